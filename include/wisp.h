@@ -247,6 +247,68 @@ wisp_status wisp_attention(const wisp_model *model, const wisp_kv *kv, const wis
                            const void *q, void *out, void *workspace, size_t workspace_bytes,
                            void *stream);
 
+/*
+ * The 8-bit KV cache (Sec. 4.5's paged KV at half the bytes; at long contexts reading it is most
+ * of a step): codes in e4m3 (OCP, largest value 448), DEVICE pools
+ *   k_pool, v_pool  [n_layers][n_blocks][n_kv_heads][page of 16 * head_dim bytes]
+ *   scale           [n_layers][n_blocks][n_kv_heads][2] fp32: the factor of K, then of V
+ * A page's value is code * scale.  Inside one page (slot s, dim e) sits at
+ *   K:  (((e / 32) * 4 + (e % 32) / 8) * 8 + (s / 8) * 4 + s % 4) * 16 + ((s / 4) % 2) * 8 + e % 8
+ *   V:  ((e / 32) * 2 + s / 8) * 256 + (e % 16) * 16 + ((e / 16) % 2) * 8 + s % 8
+ * (a lane's K or V operands of two matrix products are one 16-byte load).  The three pointers are
+ * 16-byte aligned.  Scales of pages in use are positive and finite, their V codes no NaN; both
+ * hold for whatever wisp_kv8_append writes.  One layer's operators take that layer's pools.
+ */
+typedef struct {
+  void *k_pool, *v_pool;
+  float *scale;
+  int32_t n_blocks;
+  int32_t page_size;  /* must be WISP_PAGE                                                     */
+} wisp_kv8;
+
+/*
+ * A batch planned for the 8-bit cache, shared by the calls of all layers of a step: made by
+ * wisp_kv8_plan (its fields are the library's own), copied freely, valid while its workspace
+ * and page table are.  wisp_kv8_plan uploads the batch's work lists and a table of rotations
+ * into the workspace (DEVICE, 256-byte aligned, at least wisp_kv8_workspace_size bytes; its first
+ * 256 bytes are the fault record of wisp_check, zero before the first use) and keeps
+ * desc->kv_page_table and pt_stride.  It reads model's shape, dtype and rope_base (head_dim as
+ * for wisp_attention), and desc's ctx_len, gamma, prefill_len: rows are ordered as in
+ * wisp_verify.  While `stream` is being captured the lists travel as kernel arguments.
+ * The calls below only launch kernels: they may be captured, on any stream ordered after the
+ * plan's.  They use the workspace's scratch, so calls on one plan must not overlap.
+ */
+typedef struct { uint64_t opaque[32]; } wisp_kv8_batch;
+
+size_t wisp_kv8_workspace_size(const wisp_model *model, const wisp_batch_desc *desc);
+wisp_status wisp_kv8_plan(const wisp_model *model, const wisp_batch_desc *desc, void *workspace, size_t workspace_bytes,
+                          wisp_kv8_batch *batch, void *stream);
+
+/*
+ * Rotate the new rows' Q and K (rotate-half pairing, angle position * rope_base^(-2i/head_dim))
+ * and append K and V to one layer's pages at positions ctx_len .. ctx_len + rows - 1:
+ *   qkv  DEVICE [rows][qkv_ld] of the model's dtype, row r's first (n_q + 2 n_kv) * head_dim
+ *        elements the Q heads, then K, then V (a projection's output); 16-byte aligned rows
+ *   q    DEVICE [rows][n_q_heads][head_dim] of the model's dtype: the rotated queries
+ * A page that gets rows gets, for K and for V of each head, the scale 2^k with the smallest
+ * k >= -100 such that every valid value of the page is at most 448 * 2^k (2^0 for a page of zeros);
+ * values are rounded once, from fp32, to the nearest code, ties to even.  The slots that were
+ * valid (positions below ctx_len) are brought to the new scale: exact where it grows, but for
+ * what falls below e4m3's smallest normal.  Slots past the last new row keep their codes.  A
+ * token with a K or V value of a head that is infinite, NaN or above 448 * 2^100 is kept as NaN
+ * K codes and zero V: rows that attend to it are NaN, others are not touched by it.
+ * Repeating a call gives the same pages.  A page that gets rows belongs to one request.
+ */
+wisp_status wisp_kv8_append(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *qkv, int64_t qkv_ld, void *q,
+                            void *stream);
+
+/*
+ * wisp_attention over one layer of the 8-bit cache: q and out DEVICE [rows][n_q_heads][head_dim]
+ * of the model's dtype, 16-byte aligned; row j of request i sees keys 0 .. ctx_len[i] + j.
+ * Contexts may be of any length (no limit for fp32 models).
+ */
+wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *q, void *out, void *stream);
+
 /* Uniform draws of the step's random stream: out[k] = draw (seed, req_id, tag, row, k),
  * k < n (DEVICE fp32).  tag 1 = acceptance, 2 = race. */
 wisp_status wisp_uniform(uint64_t rng_seed, uint32_t req_id, uint32_t tag, uint32_t row, uint32_t n,

@@ -44,7 +44,8 @@ EXPORTS = ("wisp_workspace_size", "wisp_logits_workspace_size", "wisp_accept_wor
            "wisp_profile_read", "wisp_profile_reset", "wisp_last_error", "wisp_schedule", "wisp_kvm_create",
            "wisp_kvm_destroy", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit", "wisp_kvm_release",
            "wisp_kvm_get_stats", "wisp_draft_stats_workspace_size", "wisp_draft_stats", "wisp_reject_predict",
-           "wisp_gemm_plan", "wisp_attention_plan", "wisp_verify_noalloc")
+           "wisp_gemm_plan", "wisp_attention_plan", "wisp_verify_noalloc", "wisp_kv8_workspace_size", "wisp_kv8_plan",
+           "wisp_kv8_append", "wisp_attention_kv8")
 
 
 class WispError(RuntimeError):
@@ -68,6 +69,14 @@ class wisp_model(C.Structure):
 
 class wisp_kv(C.Structure):
     _fields_ = [("k_pool", _VP), ("v_pool", _VP), ("n_blocks", C.c_int32), ("page_size", C.c_int32)]
+
+
+class wisp_kv8(C.Structure):
+    _fields_ = [("k_pool", _VP), ("v_pool", _VP), ("scale", _VP), ("n_blocks", C.c_int32), ("page_size", C.c_int32)]
+
+
+class wisp_kv8_batch(C.Structure):
+    _fields_ = [("opaque", C.c_uint64 * 32)]
 
 
 class wisp_batch_desc(C.Structure):
@@ -160,7 +169,13 @@ def _load():
     L.wisp_draft_stats_workspace_size.restype = C.c_size_t
     L.wisp_draft_stats.argtypes = [_VP, C.c_int32, C.c_int32, C.c_int64, C.c_float, _VP, _VP, C.c_size_t, _VP]
     L.wisp_reject_predict.argtypes = [C.POINTER(wisp_reject_mlp), _VP, C.c_int32, _VP, _VP]
-    for name in ("wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
+    L.wisp_kv8_workspace_size.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc)]
+    L.wisp_kv8_workspace_size.restype = C.c_size_t
+    L.wisp_kv8_plan.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc), _VP, C.c_size_t,
+                                C.POINTER(wisp_kv8_batch), _VP]
+    L.wisp_kv8_append.argtypes = [C.POINTER(wisp_kv8_batch), C.POINTER(wisp_kv8), _VP, C.c_int64, _VP, _VP]
+    L.wisp_attention_kv8.argtypes = [C.POINTER(wisp_kv8_batch), C.POINTER(wisp_kv8), _VP, _VP, _VP]
+    for name in ("wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
                  "wisp_check", "wisp_gemm_plan", "wisp_attention_plan", "wisp_profile_enable", "wisp_profile_read", "wisp_profile_reset",
                  "wisp_schedule", "wisp_kvm_create", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit",
                  "wisp_kvm_release", "wisp_kvm_get_stats", "wisp_draft_stats", "wisp_reject_predict"):
@@ -306,6 +321,34 @@ class KVPool:
 
     def layer(self, l: int) -> "KVPool":
         return KVPool(self.k[l:l + 1], self.v[l:l + 1])
+
+
+class KV8Pool:
+    """The 8-bit cache's device tensors in the page layout of wisp_kv8: k and v
+    [n_layers][n_blocks][n_kv][16 * head_dim] torch.float8_e4m3fn, scale [n_layers][n_blocks][n_kv][2]
+    fp32 (K, V)."""
+
+    def __init__(self, k, v, scale):
+        import torch
+        if k.shape != v.shape or k.dim() != 4 or tuple(scale.shape) != tuple(k.shape[:3]) + (2,):
+            raise ValueError(f"expected k, v [layers][blocks][n_kv][16 * head_dim] and scale [layers][blocks][n_kv][2], got "
+                             f"{tuple(k.shape)}, {tuple(v.shape)}, {tuple(scale.shape)}")
+        for t, what, dt in ((k, "k", torch.float8_e4m3fn), (v, "v", torch.float8_e4m3fn), (scale, "scale", torch.float32)):
+            _dev(t, what, dtype=dt)
+            if t.device != k.device:
+                raise ValueError(f"{what}: on {t.device}, k is on {k.device}")
+        self.k, self.v, self.scale = k, v, scale
+        self.c = wisp_kv8(k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.shape[1], PAGE)
+
+    @staticmethod
+    def zeros(n_layers, n_blocks, n_kv, head_dim, device="cuda"):
+        import torch
+        shp = (n_layers, n_blocks, n_kv, PAGE * head_dim)
+        z = lambda: torch.zeros(shp, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        return KV8Pool(z(), z(), torch.ones(shp[:3] + (2,), dtype=torch.float32, device=device))
+
+    def layer(self, l: int) -> "KV8Pool":
+        return KV8Pool(self.k[l:l + 1], self.v[l:l + 1], self.scale[l:l + 1])
 
 
 class GpuModel:
@@ -457,6 +500,75 @@ def wisp_attention(model: wisp_model, kv: KVPool, desc: BatchDesc, q, out, works
     n = desc.rows * model.n_q_heads * model.head_dim
     _ok(lib.wisp_attention(C.byref(model), C.byref(kv.c), C.byref(desc.c), _dev(q, "q", n, elem=es),
                            _dev(out, "out", n, elem=es), *_ws(workspace), _stream(stream)))
+
+
+def wisp_kv8_workspace_size(model: wisp_model, desc: BatchDesc) -> int:
+    return int(lib.wisp_kv8_workspace_size(C.byref(model), C.byref(desc.c)))
+
+
+class KV8Batch:
+    """A batch planned for the 8-bit cache (wisp_kv8_plan): keeps the workspace and the page
+    table alive, and the sizes that the calls on it check their tensors against."""
+
+    def __init__(self, c, model: wisp_model, desc: BatchDesc, ws):
+        import torch
+        self.c, self.ws, self.page_table = c, ws, desc.page_table
+        self.rows, self.n_q, self.n_kv, self.head_dim = desc.rows, model.n_q_heads, model.n_kv_heads, model.head_dim
+        self.dtype = torch.bfloat16 if model.dtype == WISP_BF16 else torch.float32
+        self.device = ws.device
+
+
+def wisp_kv8_plan(model: wisp_model, desc: BatchDesc, workspace, stream=None) -> KV8Batch:
+    """Plans desc for the 8-bit cache in `workspace` (wisp_kv8_workspace_size bytes), once for
+    all layers of a step."""
+    import torch
+    _check_desc(desc)
+    wp, wn = _ws(workspace)
+    if desc.B > 0 and desc.page_table.device != workspace.device:
+        raise ValueError(f"desc.page_table: on {desc.page_table.device}, the workspace on {workspace.device}")
+    c = wisp_kv8_batch()
+    with torch.cuda.device(workspace.device):
+        _ok(lib.wisp_kv8_plan(C.byref(model), C.byref(desc.c), wp, wn, C.byref(c), _stream(stream)))
+    return KV8Batch(c, model, desc, workspace)
+
+
+def _kv8_check(batch: KV8Batch, kv: KV8Pool, tensors):
+    if kv.k.shape[2] != batch.n_kv or kv.k.shape[3] != PAGE * batch.head_dim:
+        raise ValueError(f"kv: pages of {tuple(kv.k.shape[2:])}, expected ({batch.n_kv}, {PAGE * batch.head_dim})")
+    for what, t in tensors + (("kv", kv.k),):
+        if t.device != batch.device:
+            raise ValueError(f"{what}: on {t.device}, the batch was planned on {batch.device}")
+
+
+def _on(device, stream, call):
+    """call(stream) on `device`, the current one or another."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def wisp_kv8_append(batch: KV8Batch, kv: KV8Pool, qkv, q, stream=None):
+    """qkv [rows][(n_q + 2 n_kv) * head_dim] of the model's dtype, rows of any (16-byte) stride;
+    writes q [rows][n_q][head_dim] and layer 0 of kv (kv.layer(l) for another)."""
+    n = (batch.n_q + 2 * batch.n_kv) * batch.head_dim
+    if qkv.dim() != 2 or tuple(qkv.shape) != (batch.rows, n) or (batch.rows and qkv.stride(1) != 1):
+        raise ValueError(f"qkv: expected [{batch.rows}][{n}] with unit column stride, got {tuple(qkv.shape)}")
+    pq = _dev(qkv, "qkv", dtype=batch.dtype, contiguous=False)
+    po = _dev(q, "q", batch.rows * batch.n_q * batch.head_dim, dtype=batch.dtype)
+    _kv8_check(batch, kv, (("qkv", qkv), ("q", q)))
+    ld = qkv.stride(0) if batch.rows > 1 else n
+    _on(batch.device, stream, lambda s: _ok(lib.wisp_kv8_append(C.byref(batch.c), C.byref(kv.c), pq, ld, po, s)))
+
+
+def wisp_attention_kv8(batch: KV8Batch, kv: KV8Pool, q, out, stream=None):
+    """wisp_attention over layer 0 of the 8-bit cache kv (kv.layer(l) for another): q and out
+    [rows][n_q][head_dim] of the model's dtype."""
+    n = batch.rows * batch.n_q * batch.head_dim
+    pq, po = _dev(q, "q", n, dtype=batch.dtype), _dev(out, "out", n, dtype=batch.dtype)
+    _kv8_check(batch, kv, (("q", q), ("out", out)))
+    _on(batch.device, stream, lambda s: _ok(lib.wisp_attention_kv8(C.byref(batch.c), C.byref(kv.c), pq, po, s)))
 
 
 def wisp_uniform(rng_seed: int, req_id: int, tag: int, row: int, n: int, out, stream=None):

@@ -8,6 +8,7 @@
 
 #include "../../include/wisp.h"
 #include "kernels.h"
+#include "wave_reduce.h"
 
 namespace wisp {
 wisp_status report_error(wisp_status st, const char *msg);
@@ -33,31 +34,8 @@ struct St {
 };
 using Part = St<double>;
 
-// Reductions over a wave on the VALU: lanes l ^ 1, l ^ 2 by quad permutes, the other quad and
-// the other half of a 16-lane row by mirrors (every lane of a quad, then of an octet, already
-// holds the same value), rows by lane swaps.  The same pairs as a butterfly in steps 1, 2, 4,
-// 8, 16, 32, every lane ending with the same bits.
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  const int i = __float_as_int(v);
-  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, CTRL, 0xF, 0xF, false));
-}
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+using namespace wisp;   // the wave reductions
 
-__device__ __forceinline__ float wave_sum(float v) {
-  v += dpp<kXor1>(v);
-  v += dpp<kXor2>(v);
-  v += dpp<kHalfMirror>(v);
-  v += dpp<kMirror>(v);
-  return wisp::xor32_sum(wisp::xor16_sum(v));
-}
-__device__ __forceinline__ float wave_max(float v) {
-  v = fmaxf(v, dpp<kXor1>(v));
-  v = fmaxf(v, dpp<kXor2>(v));
-  v = fmaxf(v, dpp<kHalfMirror>(v));
-  v = fmaxf(v, dpp<kMirror>(v));
-  return wisp::xor32_max(wisp::xor16_max(v));
-}
 // the two largest of the wave's pairs (v1 >= v2), as a multiset
 __device__ __forceinline__ void top2(float &v1, float &v2, float o1, float o2) {
   v2 = fmaxf(fminf(v1, o1), fmaxf(v2, o2));

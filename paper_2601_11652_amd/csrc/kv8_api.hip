@@ -1,0 +1,235 @@
+// C ABI of the operators on the 8-bit KV cache (declared in include/wisp.h): the plan of a batch
+// (pages that get rows, attention items, rotation table) and the calls that run on it.
+#include <algorithm>
+#include <cstring>
+
+#include "api.h"
+#include "host_guard.h"
+#include "kernels.h"
+#include "kv8_plan.h"
+
+using namespace wisp;
+
+namespace {
+
+constexpr uint64_t kMagic = 0x31387670736977ull;   // a planned wisp_kv8_batch
+
+size_t take(std::vector<int32_t> &host, size_t ints) {
+  const size_t at = host.size();
+  host.resize(at + (ints + 63) / 64 * 64, 0);
+  return at;
+}
+
+template <typename V>
+size_t put(std::vector<int32_t> &host, const std::vector<V> &v) {
+  const size_t at = take(host, v.size() * (sizeof(V) / 4));
+  if (!v.empty()) std::memcpy(&host[at], v.data(), v.size() * sizeof(V));
+  return at;
+}
+
+}  // namespace
+
+wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_desc *d) {
+  Kv8Plan &p = b.p;
+  p.magic = kMagic;
+  p.page_table = d->kv_page_table;
+  p.pt_stride = d->pt_stride;
+  p.dtype = m->dtype;
+  p.nq = m->n_q_heads;
+  p.nkv = m->n_kv_heads;
+  p.hd = m->head_dim;
+  p.B = d->B;
+  const int G = p.nq / p.nkv;
+  std::vector<Kv8Unit> units;
+  std::vector<int32_t> pos, nrow(p.B), row0(p.B);
+  int most = 0;
+  for (int i = 0; i < p.B; ++i) {
+    row0[i] = (int32_t)pos.size();
+    nrow[i] = (d->prefill_len ? d->prefill_len[i] : 0) + d->gamma[i] + 1;
+    most = std::max(most, nrow[i]);
+    const int c = d->ctx_len[i], end = c + nrow[i];
+    for (int t = c; t < end; ++t) pos.push_back(t);
+    for (int pg = c / kPage; pg * kPage < end; ++pg) {
+      const int first = std::max(c, pg * kPage), last = std::min(end, (pg + 1) * kPage);
+      units.push_back(Kv8Unit{i, pg, row0[i] + first - c, (first - pg * kPage) | (last - first) << 8});
+    }
+  }
+  p.rows = (int32_t)pos.size();
+  p.n_units = (int32_t)units.size();
+
+  // Rows of a row group: as many 16-row blocks as the largest request fills, up to four (the
+  // group's K and V are read once), two or one where an fp32 model's three parts and wide
+  // heads leave no registers for more.
+  const int64_t blocks = ((int64_t)most * G + 15) / 16;
+  const int cap = p.dtype == WISP_BF16 ? 4 : p.hd == 64 || p.hd == 128 ? 2 : 1;
+  p.rb = (int)std::min<int64_t>(cap, blocks);
+  const int R = 16 * p.rb;
+  // Items: equal parts of a row group's page pairs, of at most L each
+  int64_t total = 0, n_items = 0;
+  auto groups_of = [&](int i) { return ((int64_t)nrow[i] * G + R - 1) / R; };
+  auto pairs_of = [&](int i, int64_t g) {
+    const int64_t last = std::min<int64_t>((int64_t)nrow[i] * G, (g + 1) * R) - 1;
+    return (d->ctx_len[i] + last / G + 1 + 31) / 32;
+  };
+  for (int i = 0; i < p.B; ++i)
+    for (int64_t g = 0, n = groups_of(i); g < n; ++g) total += pairs_of(i, g) * p.nkv;
+  const int64_t slots = (int64_t)device_cus() * (p.rb <= 2 ? 2 : 1);
+  const int64_t L = std::min<int64_t>(64, std::max<int64_t>(8, (total + slots - 1) / slots));
+  for (int i = 0; i < p.B; ++i)
+    for (int64_t g = 0, n = groups_of(i); g < n; ++g) n_items += (pairs_of(i, g) + L - 1) / L;
+  if (n_items * p.nkv > kKv8MaxItems)
+    return fail(WISP_E_UNSUPPORTED, "the batch's contexts need %lld attention work items (at most %d)",
+                (long long)(n_items * p.nkv), kKv8MaxItems);
+  std::vector<Kv8Item> items;
+  std::vector<Kv8Group> groups;
+  items.reserve(n_items);
+  p.n_parts = 0;
+  for (int i = 0; i < p.B; ++i)
+    for (int64_t g = 0, ng = groups_of(i); g < ng; ++g) {
+      const int64_t last = std::min<int64_t>((int64_t)nrow[i] * G, (g + 1) * R) - 1;
+      const int32_t T = d->ctx_len[i] + (int32_t)(last / G) + 1;
+      const int64_t pairs = (T + 31) / 32, n = (pairs + L - 1) / L;
+      if (n > 1) groups.push_back(Kv8Group{row0[i], nrow[i], (int32_t)g, p.n_parts, (int32_t)n, {0, 0, 0}});
+      for (int64_t k = 0; k < n; ++k) {
+        const int32_t a = (int32_t)(32 * (k * pairs / n)), e = std::min<int32_t>(T, (int32_t)(32 * ((k + 1) * pairs / n)));
+        items.push_back(Kv8Item{i, a, e, d->ctx_len[i], row0[i], nrow[i], (int32_t)g, n > 1 ? p.n_parts++ : -1});
+      }
+    }
+  p.n_items = (int32_t)items.size();
+  p.n_groups = (int32_t)groups.size();
+
+  b.i_units = put(b.host, units);
+  b.i_items = put(b.host, items);
+  b.i_groups = put(b.host, groups);
+  b.i_pos = put(b.host, pos);
+  const size_t slots_of_parts = (size_t)p.n_parts * p.nkv * R;
+  b.po_bytes = align256(slots_of_parts * p.hd * 4);
+  b.pml_bytes = align256(slots_of_parts * 2 * 4);
+  b.cs_bytes = align256((size_t)p.rows * p.hd * 4);
+  return WISP_OK;
+}
+
+void wisp::kv8_place(Kv8Build &b, char *ws, size_t desc, size_t scratch) {
+  Kv8Plan &p = b.p;
+  p.ws = ws;
+  p.w_units = desc + b.i_units * 4;
+  p.w_items = desc + b.i_items * 4;
+  p.w_groups = desc + b.i_groups * 4;
+  p.w_pos = desc + b.i_pos * 4;
+  p.w_po = scratch;
+  p.w_pml = p.w_po + b.po_bytes;
+  p.w_cs = p.w_pml + b.pml_bytes;
+  p.total = p.w_cs + b.cs_bytes;
+}
+
+wisp_status wisp::kv8_cache(Kv8Cache &c, const wisp_kv8 *kv) {
+  if (!kv || !kv->k_pool || !kv->v_pool || !kv->scale) return fail(WISP_E_INVALID, "8-bit KV pools or scales are NULL");
+  if (kv->page_size != WISP_PAGE) return fail(WISP_E_UNSUPPORTED, "page_size must be %d", WISP_PAGE);
+  if (kv->n_blocks <= 0) return fail(WISP_E_INVALID, "n_blocks must be positive");
+  if (((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool | (uintptr_t)kv->scale) & 15)
+    return fail(WISP_E_INVALID, "8-bit KV pools and scales must be 16-byte aligned");
+  c = Kv8Cache{static_cast<uint8_t *>(kv->k_pool), static_cast<uint8_t *>(kv->v_pool), kv->scale, kv->n_blocks};
+  return WISP_OK;
+}
+
+namespace {
+
+static_assert(sizeof(Kv8Plan) <= sizeof(wisp_kv8_batch), "wisp_kv8_batch holds a plan");
+
+wisp_status planned(Kv8Plan &p, const wisp_kv8_batch *batch) {
+  if (!batch) return fail(WISP_E_INVALID, "batch is NULL");
+  std::memcpy(&p, batch, sizeof(p));
+  if (p.magic != kMagic) return fail(WISP_E_INVALID, "the batch has not been planned (wisp_kv8_plan)");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return fail(WISP_E_HIP, "hipGetDevice failed");
+  if (dev != p.device) return fail(WISP_E_INVALID, "the batch was planned on device %d, the current one is %d", p.device, dev);
+  return WISP_OK;
+}
+
+size_t own_size(Kv8Build &b) {
+  kv8_place(b, nullptr, 256, align256(256 + b.host.size() * 4));
+  return b.p.total;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wisp_kv8_workspace_size(const wisp_model *model, const wisp_batch_desc *desc) {
+  return guarded_size([&]() -> size_t {
+    if (check_model(model, false) != WISP_OK || check_desc(desc, false, true) != WISP_OK) return 0;
+    Kv8Build b;
+    if (kv8_build(b, model, desc) != WISP_OK) return 0;
+    return own_size(b);
+  });
+}
+
+wisp_status wisp_kv8_plan(const wisp_model *model, const wisp_batch_desc *desc, void *workspace, size_t workspace_bytes,
+                          wisp_kv8_batch *batch, void *stream) {
+  return guarded("wisp_kv8_plan", [&]() -> wisp_status {
+    wisp_status st;
+    if (!batch) return fail(WISP_E_INVALID, "batch is NULL");
+    std::memset(batch, 0, sizeof(*batch));
+    if ((st = check_model(model, false)) != WISP_OK) return st;
+    if ((st = check_desc(desc, true, true)) != WISP_OK) return st;
+    Kv8Build b;
+    if ((st = kv8_build(b, model, desc)) != WISP_OK) return st;
+    if (hipGetDevice(&b.p.device) != hipSuccess) return fail(WISP_E_HIP, "hipGetDevice failed");
+    const size_t need = own_size(b);
+    if (desc->B > 0) {
+      if (!workspace) return fail(WISP_E_INVALID, "NULL workspace");
+      if ((uintptr_t)workspace & 255) return fail(WISP_E_INVALID, "workspace must be 256-byte aligned");
+      if (workspace_bytes < need)
+        return fail(WISP_E_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+      char *ws = static_cast<char *>(workspace);
+      kv8_place(b, ws, 256, align256(256 + b.host.size() * 4));
+      const hipStream_t s = (hipStream_t)stream;
+      hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+      if (hipStreamIsCapturing(s, &cap) != hipSuccess) return fail(WISP_E_HIP, "stream query failed");
+      st = cap == hipStreamCaptureStatusNone ? upload_ints(b.host, ws + 256, s) : upload_ints_by_arguments(b.host, ws + 256, s);
+      if (st != WISP_OK) return st;
+      StepDesc sd{};
+      sd.row_pos = reinterpret_cast<const int32_t *>(ws + b.p.w_pos);
+      rope_table(sd, reinterpret_cast<float *>(ws + b.p.w_cs), b.p.rows, b.p.hd, model->rope_base, s);
+      if ((st = hip_check("plan launch")) != WISP_OK) return st;
+    }
+    std::memcpy(batch, &b.p, sizeof(b.p));
+    return WISP_OK;
+  });
+}
+
+wisp_status wisp_kv8_append(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *qkv, int64_t qkv_ld, void *q,
+                            void *stream) {
+  return guarded("wisp_kv8_append", [&]() -> wisp_status {
+    wisp_status st;
+    Kv8Plan p;
+    if ((st = planned(p, batch)) != WISP_OK) return st;
+    if (p.B == 0) return WISP_OK;
+    Kv8Cache c;
+    if ((st = kv8_cache(c, kv)) != WISP_OK) return st;
+    if (!qkv || !q) return fail(WISP_E_INVALID, "NULL qkv / q");
+    const int64_t es = p.dtype == WISP_BF16 ? 2 : 4;
+    if (qkv_ld < (int64_t)(p.nq + 2 * p.nkv) * p.hd) return fail(WISP_E_INVALID, "qkv_ld shorter than a row");
+    if ((((uintptr_t)qkv | (uintptr_t)q) & 15) || qkv_ld * es % 16)
+      return fail(WISP_E_INVALID, "qkv, its rows and q must be 16-byte aligned");
+    kv8_append(p, c, QkvRows{qkv, qkv_ld, 0, 0}, q, reinterpret_cast<int *>(p.ws), (hipStream_t)stream);
+    return hip_check("append launch");
+  });
+}
+
+wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *q, void *out, void *stream) {
+  return guarded("wisp_attention_kv8", [&]() -> wisp_status {
+    wisp_status st;
+    Kv8Plan p;
+    if ((st = planned(p, batch)) != WISP_OK) return st;
+    if (p.B == 0) return WISP_OK;
+    Kv8Cache c;
+    if ((st = kv8_cache(c, kv)) != WISP_OK) return st;
+    if (!q || !out) return fail(WISP_E_INVALID, "NULL q / out");
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(WISP_E_INVALID, "q and out must be 16-byte aligned");
+    kv8_attention(p, c, q, out, false, reinterpret_cast<int *>(p.ws), (hipStream_t)stream);
+    return hip_check("attention launch");
+  });
+}
+
+}  // extern "C"

@@ -14,18 +14,19 @@
 
 #include "../../include/wisp.h"
 #include "common.h"
+#include "api.h"
 #include "host_guard.h"
 #include "kernels.h"
+#include "kv8.h"
 
 using namespace wisp;
 
 namespace {
-
 // the calling thread's last error message (a fixed buffer: reporting never allocates)
 thread_local char g_last_error[512] = "";
+}  // namespace
 
-wisp_status fail(wisp_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-wisp_status fail(wisp_status st, const char *fmt, ...) {
+wisp_status wisp::fail(wisp_status st, const char *fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
@@ -33,7 +34,8 @@ wisp_status fail(wisp_status st, const char *fmt, ...) {
   return st;
 }
 
-inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+namespace {
+
 
 // ------------------------------------------------------------------------------------------
 // launch plan
@@ -64,7 +66,9 @@ struct Plan {
 };
 
 
-wisp_status check_model(const wisp_model *m, bool need_weights) {
+}  // namespace
+
+wisp_status wisp::check_model(const wisp_model *m, bool need_weights) {
   if (!m) return fail(WISP_E_INVALID, "model is NULL");
   if (m->n_layers <= 0 || m->d_model <= 0 || m->n_q_heads <= 0 || m->n_kv_heads <= 0 ||
       m->head_dim <= 0 || m->d_ff <= 0 || m->vocab <= 0)
@@ -94,8 +98,7 @@ wisp_status check_model(const wisp_model *m, bool need_weights) {
   return WISP_OK;
 }
 
-// forward: the call runs the model, so prompt rows count towards the batch's rows
-wisp_status check_desc(const wisp_batch_desc *d, bool need_pages, bool forward) {
+wisp_status wisp::check_desc(const wisp_batch_desc *d, bool need_pages, bool forward) {
   if (!d) return fail(WISP_E_INVALID, "batch descriptor is NULL");
   if (d->B < 0) return fail(WISP_E_INVALID, "B < 0");
   if (d->B == 0) return WISP_OK;
@@ -125,6 +128,8 @@ wisp_status check_desc(const wisp_batch_desc *d, bool need_pages, bool forward) 
   return WISP_OK;
 }
 
+namespace {
+
 void carve(size_t &w, size_t &field, size_t bytes) {
   field = w;
   w = align256(w + bytes);
@@ -150,14 +155,17 @@ size_t attn_part_bytes(const Plan &p) {
   return p.max_group_chunks > 1 ? align256(p.items.size() * (size_t)p.hd * p.item_rows * 4) + align256(p.items.size() * (size_t)p.item_rows * 2 * 4) : 0;
 }
 
-// compute units of the current device (the attention work list is sized to them)
-int device_cus() {
+}  // namespace
+
+int wisp::device_cus() {
   int dev = 0, n = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
     n = 256;
   return n;
 }
+
+namespace {
 
 // Attention work list.  A row group (item_rows of a request's rows x G query rows of one kv
 // head) attends to a run of page pairs.  Either every item (a part of a group's pairs) has a
@@ -622,9 +630,10 @@ struct Staging {
   bool pending = false;
 };
 thread_local Staging g_stage;
+}  // namespace
 
-wisp_status upload(const Plan &p, char *ws, hipStream_t s) {
-  const size_t bytes = p.host.size() * sizeof(int32_t);
+wisp_status wisp::upload_ints(const std::vector<int32_t> &host, void *dst, hipStream_t s) {
+  const size_t bytes = host.size() * sizeof(int32_t);
   if (bytes == 0) return WISP_OK;
   if (g_stage.pending) {
     if (hipEventSynchronize(g_stage.ev) != hipSuccess) return fail(WISP_E_HIP, "staging event sync failed");
@@ -641,13 +650,23 @@ wisp_status upload(const Plan &p, char *ws, hipStream_t s) {
   }
   if (!g_stage.ev && hipEventCreateWithFlags(&g_stage.ev, hipEventDisableTiming) != hipSuccess)
     return fail(WISP_E_HIP, "event creation failed");
-  std::memcpy(g_stage.buf, p.host.data(), bytes);
-  if (hipMemcpyAsync(ws + p.w_desc, g_stage.buf, bytes, hipMemcpyHostToDevice, s) != hipSuccess)
+  std::memcpy(g_stage.buf, host.data(), bytes);
+  if (hipMemcpyAsync(dst, g_stage.buf, bytes, hipMemcpyHostToDevice, s) != hipSuccess)
     return fail(WISP_E_HIP, "descriptor upload failed");
   if (hipEventRecord(g_stage.ev, s) != hipSuccess) return fail(WISP_E_HIP, "event record failed");
   g_stage.pending = true;
   return WISP_OK;
 }
+
+wisp_status wisp::hip_check(const char *what) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(WISP_E_HIP, "%s: %s", what, hipGetErrorString(e));
+  return WISP_OK;
+}
+
+namespace {
+
+wisp_status upload(const Plan &p, char *ws, hipStream_t s) { return upload_ints(p.host, ws + p.w_desc, s); }
 
 SamplerScratch sampler_scratch(const Plan &p, char *ws) {
   SamplerScratch sc;
@@ -682,12 +701,6 @@ int gemm_class(const Plan &p, const GemmCfg &c) {
   if (!p.bf16) return WISP_PROF_GEMM_TILED;
   if (c.kind == 4) return WISP_PROF_GEMM_TILE;
   return c.kind == 2 ? WISP_PROF_GEMM_RING2 : WISP_PROF_GEMM_RING1;
-}
-
-wisp_status hip_check(const char *what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(WISP_E_HIP, "%s: %s", what, hipGetErrorString(e));
-  return WISP_OK;
 }
 
 template <typename T>
@@ -899,19 +912,19 @@ __global__ void put_desc_kernel(DescChunk c, int32_t *__restrict__ dst) {
   for (int i = threadIdx.x; i < c.n; i += blockDim.x) dst[i] = c.v[i];
 }
 
-wisp_status upload_by_arguments(const Plan &p, char *ws, hipStream_t s) {
-  int32_t *dst = reinterpret_cast<int32_t *>(ws + p.w_desc);
-  const size_t n = p.host.size();
+}  // namespace
+
+wisp_status wisp::upload_ints_by_arguments(const std::vector<int32_t> &host, void *to, hipStream_t s) {
+  int32_t *dst = static_cast<int32_t *>(to);
+  const size_t n = host.size();
   DescChunk c;
   for (size_t o = 0; o < n; o += kDescChunkInts) {
     c.n = (int32_t)std::min<size_t>(kDescChunkInts, n - o);
-    std::memcpy(c.v, p.host.data() + o, (size_t)c.n * sizeof(int32_t));
+    std::memcpy(c.v, host.data() + o, (size_t)c.n * sizeof(int32_t));
     launch(put_desc_kernel, 1, 256, 0, s, c, dst + o);
   }
   return hip_check("descriptor upload");
 }
-
-}  // namespace
 
 namespace wisp {
 // lets the host-only sources (the scheduler, the KV manager) report through wisp_last_error
@@ -1043,7 +1056,7 @@ wisp_status wisp_verify_noalloc(const wisp_model *model, const wisp_kv *kv, cons
     if ((st = noalloc_scratch(&ws)) != WISP_OK) return st;
     hipStream_t s = (hipStream_t)stream;
     if (!target_logits) target_logits = reinterpret_cast<float *>(ws + p.total);
-    if ((st = upload_by_arguments(p, ws, s)) != WISP_OK) return st;
+    if ((st = upload_ints_by_arguments(p.host, ws + p.w_desc, s)) != WISP_OK) return st;
     return run_verify(p, model, kv, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
                       ws, fault, s);
   });

@@ -1,0 +1,316 @@
+"""GPU parity of the 8-bit KV cache's operators (wisp_kv8_append, wisp_attention_kv8) against the
+fp64 oracle: head layouts and dims, lengths from one token on, pages that end inside a tile, stale
+slots and unused pages full of NaN, rows that are not finite, replayed graphs, other streams."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_11652_amd as W
+from gpu_harness import log
+from kv8_harness import Case, attention_bound, dev, host_pool
+from oracle import kv8
+
+pytestmark = pytest.mark.gpu
+
+#          ctx, rows per request, query heads, kv heads, head_dim, bf16
+APPEND = [
+    ([0], [1], 4, 4, 64, True),
+    ([0], [1], 1, 1, 32, False),
+    ([15, 16, 17, 31], [1, 1, 2, 2], 32, 8, 128, True),
+    ([5, 0, 1300], [6, 40, 17], 32, 8, 128, True),
+    ([13, 2], [19, 1], 64, 8, 128, True),
+    ([100, 7], [9, 33], 6, 2, 64, True),
+    ([100, 7], [9, 33], 4, 4, 64, False),
+    ([3, 60], [30, 5], 6, 3, 96, False),
+    ([1, 20], [15, 16], 5, 1, 160, False),
+    ([47, 0], [3, 16], 2, 2, 256, False),
+    ([9], [100], 3, 1, 224, False),
+]
+
+
+def _append(case, x, pad=0):
+    kv = case.pool()
+    qkv = torch.zeros(case.M, x.shape[1] + pad, dtype=torch.bfloat16 if case.bf16 else torch.float32, device="cuda")
+    qkv.fill_(float("nan"))
+    qkv[:, :x.shape[1]] = dev(x, case.bf16)
+    q = torch.full((case.M, case.n_q, case.hd), 7.0, dtype=qkv.dtype, device="cuda")
+    plan = case.plan()
+    W.wisp_kv8_append(plan, kv, qkv[:, :x.shape[1]], q)
+    W.wisp_check(plan.ws)
+    return kv, q, plan
+
+
+def _check_append(case, x, kv, q):
+    k, v, scale = case.k.copy(), case.v.copy(), case.scale.astype(np.float64)
+    wq, wk, wv = kv8.append(k, v, scale, case.pt, case.ctx, case.nrow, x, case.n_q, case.n_kv, case.hd, case.base)
+    gk, gv, gs = host_pool(kv)
+    # a rotated value: two products and a sum, the table's cosine and sine each rounded once, in fp32
+    xs = x.reshape(case.M, -1, case.hd)
+    h2 = case.hd // 2
+    pair = np.abs(xs[..., :h2]) + np.abs(xs[..., h2:])
+    err = 4 * 2.0 ** -24 * np.concatenate([pair, pair], -1)
+    tol = err[:, :case.n_q] + (2.0 ** -8 if case.bf16 else 2.0 ** -24) * np.abs(wq)
+    assert np.all(np.abs(q.double().cpu().numpy() - wq) <= tol)
+    np.testing.assert_array_equal(gs, scale)
+    # codes: the oracle's, but where fp32's error reaches a border between two codes
+    for g, w, new, sc, order, e in ((gk, k, wk, 0, kv8.k_order(case.hd), err[:, case.n_q:case.n_q + case.n_kv]),
+                                    (gv, v, wv, 1, kv8.v_order(case.hd), 0 * wv)):
+        written = np.zeros(g.shape, bool)
+        r = 0
+        for b in range(len(case.ctx)):
+            for t in range(int(case.ctx[b]), int(case.ctx[b] + case.nrow[b])):
+                blk, s = case.pt[b, t // 16], t % 16
+                written[blk][:, order[s]] = True
+                got = kv8.VALUES[g[blk][:, order[s]]]
+                x_s = new[r] / scale[blk, :, sc][:, None]
+                step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(np.abs(x_s), 1e-300))), -6) - 3)
+                assert np.all(np.abs(got - x_s) <= 0.5 * step * (1 + 1e-9) + e[r] / scale[blk, :, sc][:, None]), (b, t)
+                r += 1
+        np.testing.assert_array_equal(g[~written], w[~written])   # old slots rescaled, all else untouched
+        assert np.mean(g[written] != w[written]) < 1e-3
+
+
+@pytest.mark.parametrize("case", range(len(APPEND)))
+def test_append_matches_oracle(case):
+    log(f"append {APPEND[case]}")
+    c = Case(*APPEND[case], seed=100 + case)
+    x = c.qkv()
+    kv, q, plan = _append(c, x, pad=24 if case % 2 else 0)
+    _check_append(c, x, kv, q)
+    # once more: the same pages
+    before = host_pool(kv)
+    W.wisp_kv8_append(plan, kv, dev(x, c.bf16), q)
+    for a, b in zip(before, host_pool(kv)):
+        np.testing.assert_array_equal(a, b)
+
+
+def test_append_with_scales_that_are_no_powers_of_two():
+    c = Case([13, 40, 7], [4, 9, 5], 8, 2, 64, True, seed=9, pow2=False)
+    x = c.qkv()
+    kv, q, _ = _append(c, x)
+    _check_append(c, x, kv, q)
+
+
+def test_append_of_large_small_and_zero_values():
+    """Pages whose values span fp32: scales at the lower end, zeros, and a page whose old slots
+    vanish beside a new row that is far larger."""
+    c = Case([5, 0, 0, 0], [3, 16, 16, 4], 2, 2, 64, False, seed=11)
+    x = c.qkv()
+    x[3:19] *= 1e-36
+    x[19:35] = 0.0
+    x[:3] *= 1e30
+    kv, q, _ = _append(c, x.astype(np.float32).astype(np.float64))
+    _check_append(c, x.astype(np.float32).astype(np.float64), kv, q)
+
+
+def test_rows_that_are_not_finite_stay_theirs():
+    """A NaN or an infinity in K or V: the rows that attend to it are NaN, the ones before it are
+    what they are without it."""
+    for where, bad in ((0, np.nan), (1, np.inf), (1, np.nan), (0, -np.inf)):
+        c = Case([20, 30], [5, 5], 8, 2, 64, True, seed=21)
+        x = c.qkv()
+        x[3, (8 + 2 * where) * 64 + 7] = bad          # request 0's fourth row, K or V of kv head 0
+        kv, q, plan = _append(c, x)
+        ok = np.ones((c.M, c.n_q), bool)
+        ok[3:5, :4] = False
+        clean = c.queries()
+        out = torch.empty(c.M, 8, 64, dtype=torch.bfloat16, device="cuda")
+        W.wisp_attention_kv8(plan, kv, dev(clean, True), out)
+        got = out.double().cpu().numpy()
+        assert np.isnan(got[~ok]).all() and np.isfinite(got[ok]).all()
+        k, v, s = host_pool(kv)
+        assert not np.isnan(kv8.VALUES[v[c.pt[0, 1]][:, kv8.v_order(64)[:9]]]).any()
+        ref, mag, big = kv8.attention(clean, k, v, s, c.pt, c.ctx, c.nrow, 2)
+        assert np.all((np.abs(got - ref) <= attention_bound(ref, mag, big, 64, 40, True))[ok])
+
+
+ATTENTION = [
+    ([0], [1], 4, 4, 64, True),
+    ([0], [1], 1, 1, 32, False),
+    ([0, 1, 15, 16, 31, 32], [1, 1, 1, 1, 1, 1], 32, 8, 128, True),
+    ([15, 40, 0, 129], [2, 5, 1, 4], 32, 8, 128, True),
+    ([700, 33, 2500], [9, 17, 3], 32, 8, 128, True),
+    ([1000, 17], [17, 6], 64, 8, 128, True),
+    ([300, 64, 5], [4, 8, 2], 8, 8, 64, True),
+    ([64, 900], [3, 10], 16, 2, 64, True),
+    ([12000, 900], [7, 4], 32, 8, 128, True),
+    ([40, 3], [2, 1], 64, 1, 128, True),         # 64 query heads on one kv head
+    ([0, 250], [150, 90], 8, 2, 128, True),      # prompts
+    ([513], [3], 6, 2, 64, True),                # three query heads per kv head
+    ([700, 33], [9, 17], 8, 2, 128, False),
+    ([300, 64, 5], [4, 40, 2], 4, 4, 64, False),
+    ([5000], [6], 4, 4, 64, False),
+    ([100, 7], [9, 3], 6, 3, 96, False),
+    ([31, 200], [4, 17], 5, 1, 160, False),
+    ([99], [20], 2, 2, 192, False),
+    ([50], [3], 3, 1, 224, False),
+    ([47, 330], [3, 16], 2, 2, 256, False),
+]
+
+
+def _check_attention(c, q, plan=None, kv=None):
+    kv = kv or c.pool()
+    plan = plan or c.plan()
+    out = torch.full((c.M, c.n_q, c.hd), 7.0, dtype=torch.bfloat16 if c.bf16 else torch.float32, device="cuda")
+    W.wisp_attention_kv8(plan, kv, dev(q, c.bf16), out)
+    W.wisp_check(plan.ws)
+    k, v, s = host_pool(kv)
+    ref, mag, big = kv8.attention(q, k, v, s, c.pt, c.ctx, c.nrow, c.n_kv)
+    err, tol = np.abs(out.double().cpu().numpy() - ref), attention_bound(ref, mag, big, c.hd, int((c.ctx + c.nrow).max()), c.bf16)
+    log(f"  worst {np.max(err / tol):.3f} of its bound, largest error {err.max():.2e}")
+    assert np.all(err <= tol)
+    return out
+
+
+@pytest.mark.parametrize("case", range(len(ATTENTION)))
+def test_attention_matches_oracle(case):
+    log(f"attention {ATTENTION[case]}")
+    c = Case(*ATTENTION[case], seed=300 + case, pow2=case % 2 == 0).fill()
+    _check_attention(c, c.queries())
+
+
+def test_attention_of_peaked_scores():
+    """Scores of hundreds: the running maximum rises over and over, probabilities vanish."""
+    for bf16 in (True, False):
+        c = Case([1500, 3], [5, 3], 8, 2, 64, bf16, seed=77).fill()
+        _check_attention(c, c.queries(std=60.0))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_append_then_attention(bf16):
+    """The two as a layer runs them, over three steps of drafts of which some are kept."""
+    c = Case([20, 0, 333], [6, 3, 10], 8, 2, 64, bf16, seed=31)
+    kv = c.pool()
+    host = [c.k.copy(), c.v.copy(), c.scale.astype(np.float64)]
+    kept = [[2, 3, 1], [1, 1, 1], [4, 2, 1]]
+    rng = np.random.default_rng(8)
+    for step, keep in enumerate(kept):
+        x = c.qkv()
+        plan = c.plan()
+        q = torch.empty(c.M, 8, 64, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+        W.wisp_kv8_append(plan, kv, dev(x, bf16), q)
+        qh = q.double().cpu().numpy()
+        _check_attention(c, qh, plan, kv)
+        kv8.append(*host, c.pt, c.ctx, c.nrow, x, 8, 2, 64, c.base)
+        np.testing.assert_array_equal(host_pool(kv)[2], host[2])
+        c.ctx = c.ctx + np.asarray(keep, np.int32)        # rollback by length
+        c.nrow = rng.integers(1, 8, 3).astype(np.int32)
+        need = (c.ctx + c.nrow + 15) // 16
+        for b in range(3):                                # pages that the longer requests need
+            while (c.pt[b] >= 0).sum() < need[b]:
+                c.pt[b, (c.pt[b] >= 0).sum()] = max(set(range(c.k.shape[0])) - set(c.pt.reshape(-1).tolist()))
+        c.M = int(c.nrow.sum())
+        from gpu_harness import to_dev
+        c.desc = W.BatchDesc(c.ctx, c.nrow - 1, to_dev(c.pt), 1.0)
+
+
+def test_bad_block_ids_are_reported():
+    c = Case([40, 20], [3, 3], 8, 2, 64, True, seed=41).fill()
+    for bad in (-1, c.k.shape[0], 1 << 30):
+        keep = c.pt[0, 2]
+        c.pt[0, 2] = bad
+        from gpu_harness import to_dev
+        c.desc = W.BatchDesc(c.ctx, c.nrow - 1, to_dev(c.pt), 1.0)
+        kv, plan = c.pool(), c.plan()
+        before = host_pool(kv)
+        q = torch.empty(c.M, 8, 64, dtype=torch.bfloat16, device="cuda")
+        W.wisp_kv8_append(plan, kv, dev(c.qkv(), True), q)
+        with pytest.raises(W.WispError) as e:
+            W.wisp_check(plan.ws)
+        assert e.value.status == W.WISP_E_DEVICE_INPUT
+        W.wisp_attention_kv8(plan, kv, q, torch.empty_like(q))
+        with pytest.raises(W.WispError):
+            W.wisp_check(plan.ws)
+        W.wisp_check(plan.ws)                            # cleared
+        touched = {int(c.pt[0, 2]), int(c.pt[1, 1])}
+        for a, b in zip(before, host_pool(kv)):
+            for blk in range(a.shape[0]):
+                if blk not in touched:
+                    np.testing.assert_array_equal(a[blk], b[blk])
+        c.pt[0, 2] = keep
+
+
+def test_captured_and_replayed():
+    """Append and attention in a graph, replayed with new inputs between eager calls; a plan made
+    while capturing."""
+    c = Case([900, 33], [6, 3], 32, 8, 128, True, seed=51)
+    kv, plan = c.pool(), c.plan()
+    qkv = dev(c.qkv(), True)
+    q = torch.empty(c.M, 32, 128, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    ws = W.workspace(W.wisp_kv8_workspace_size(c.model, c.desc))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        inner = W.wisp_kv8_plan(c.model, c.desc, ws)
+        W.wisp_kv8_append(inner, kv, qkv, q)
+        W.wisp_attention_kv8(inner, kv, q, out)
+    for step in range(4):
+        qkv.copy_(dev(c.qkv(), True))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        W.wisp_check(ws)
+        kv2, q2 = c.pool(), torch.empty_like(q)
+        out2 = torch.empty_like(q)
+        W.wisp_kv8_append(plan, kv2, qkv, q2)
+        W.wisp_attention_kv8(plan, kv2, q2, out2)
+        torch.cuda.synchronize()
+        assert torch.equal(q, q2) and torch.equal(out, out2), step
+
+
+def test_two_plans_on_two_streams():
+    c = [Case([900, 33], [6, 3], 32, 8, 128, True, seed=61 + k).fill() for k in range(2)]
+    q = [dev(x.queries(), True) for x in c]
+    kv = [x.pool() for x in c]
+    plans = [x.plan() for x in c]
+    alone = []
+    for p, k, x in zip(plans, kv, q):
+        alone.append(torch.empty_like(x))
+        W.wisp_attention_kv8(p, k, x, alone[-1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in c]
+    outs = [torch.empty_like(x) for x in q]
+    for _ in range(20):
+        for p, k, x, o, s in zip(plans, kv, q, outs, streams):
+            W.wisp_attention_kv8(p, k, x, o, s)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, outs):
+        assert torch.equal(a, b)
+
+
+def test_wrapper_refuses_tensors_that_do_not_fit():
+    c = Case([40, 20], [3, 3], 8, 2, 64, True, seed=71).fill()
+    kv, plan = c.pool(), c.plan()
+    q = torch.empty(c.M, 8, 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros(c.M, 12 * 64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: W.wisp_attention_kv8(plan, kv, q.float(), q),
+                 lambda: W.wisp_attention_kv8(plan, kv, q[1:], q),
+                 lambda: W.wisp_attention_kv8(plan, kv, q.cpu(), q),
+                 lambda: W.wisp_attention_kv8(plan, kv, q.transpose(1, 2), q),
+                 lambda: W.wisp_kv8_append(plan, kv, x[:, 1:], q),
+                 lambda: W.wisp_kv8_append(plan, kv, x[1:], q),
+                 lambda: W.wisp_kv8_append(plan, W.KV8Pool.zeros(1, 4, 2, 128), x, q),
+                 lambda: W.KV8Pool(kv.k, kv.v, kv.scale[..., 0]),
+                 lambda: W.KV8Pool(kv.k.view(torch.uint8), kv.v, kv.scale)):
+        with pytest.raises(ValueError):
+            call()
+    wide = torch.zeros(c.M, 12 * 64 + 8, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(W.WispError):                      # rows not 16-byte aligned
+        W.wisp_kv8_append(plan, kv, wide[:, 4:4 + 12 * 64], q)
+    with pytest.raises(W.WispError):
+        W.wisp_kv8_append(plan, kv, x[:1].expand(c.M, -1), q)
+    with pytest.raises(W.WispError):
+        W.wisp_kv8_plan(c.model, c.desc, W.workspace(256))
+    W.wisp_attention_kv8(plan, kv, q, torch.empty_like(q))
+    W.wisp_check(plan.ws)
+
+
+def test_an_empty_batch_does_nothing():
+    m = Case([3], [1], 8, 2, 64, True, seed=1).model
+    d = W.BatchDesc([], [], torch.zeros(0, 1, dtype=torch.int32, device="cuda"), 1.0)
+    plan = W.wisp_kv8_plan(m, d, W.workspace(256))
+    e = torch.empty(0, 8, 64, dtype=torch.bfloat16, device="cuda")
+    W.wisp_attention_kv8(plan, W.KV8Pool.zeros(1, 2, 2, 64), e, e)
+    W.wisp_kv8_append(plan, W.KV8Pool.zeros(1, 2, 2, 64), torch.empty(0, 12 * 64, dtype=torch.bfloat16, device="cuda"), e)
