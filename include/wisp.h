@@ -512,6 +512,31 @@ wisp_status wisp_draft_stats(const float *logits, int32_t rows, int32_t vocab, i
 wisp_status wisp_reject_predict(const wisp_reject_mlp *mlp, const float *features, int32_t rows, float *p_accept,
                                 void *stream);
 
+/*
+ * What an answer says about its tokens (the rows that the step scored, Sec. 2.4's p): for each of
+ * `rows` rows of DEVICE logits of dtype (WISP_F32 or WISP_BF16; row r at logits + r * ld, `vocab`
+ * entries, ld >= vocab), with p = softmax(logits / temperature):
+ *   tokens       DEVICE int32 [rows] or NULL: the row's token; -1 (as after wisp_verify's emitted
+ *                tokens): the row is passed over, its outputs left as they were
+ *   logprob      DEVICE fp32 [rows] or NULL: ln p of the token
+ *   entropy      DEVICE fp32 [rows] or NULL: -sum p ln p
+ *   top_tokens, top_logprobs  DEVICE int32 / fp32 [rows][n_top]: the n_top most probable tokens
+ *                in falling order, equal ones by index, and their ln p; n_top <= WISP_TOP_MAX,
+ *                0: none (the pointers may be NULL)
+ * A logit of -infinity has p = 0: its ln p is -infinity, and it is not listed (places that no
+ * entry fills hold -1 and -infinity).  A row of nothing else has ln p = -infinity and entropy 0.
+ * A NaN or +infinity among a row's logits makes its ln p and entropy NaN.  A token outside -1 ..
+ * vocab - 1 gets NaN and is reported by wisp_check(workspace): workspace is DEVICE scratch of
+ * wisp_token_logprobs_workspace_size bytes, 16-byte aligned, its first 256 bytes zero before the
+ * first use.
+ */
+#define WISP_TOP_MAX 32
+size_t wisp_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t n_top);
+wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld,
+                                float temperature, const int32_t *tokens, int32_t n_top, float *logprob, float *entropy,
+                                int32_t *top_tokens, float *top_logprobs, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char *wisp_last_error(void);
 

@@ -45,7 +45,7 @@ EXPORTS = ("wisp_workspace_size", "wisp_logits_workspace_size", "wisp_accept_wor
            "wisp_kvm_destroy", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit", "wisp_kvm_release",
            "wisp_kvm_get_stats", "wisp_draft_stats_workspace_size", "wisp_draft_stats", "wisp_reject_predict",
            "wisp_gemm_plan", "wisp_attention_plan", "wisp_verify_noalloc", "wisp_kv8_workspace_size", "wisp_kv8_plan",
-           "wisp_kv8_append", "wisp_attention_kv8")
+           "wisp_kv8_append", "wisp_attention_kv8", "wisp_token_logprobs_workspace_size", "wisp_token_logprobs")
 
 
 class WispError(RuntimeError):
@@ -175,7 +175,11 @@ def _load():
                                 C.POINTER(wisp_kv8_batch), _VP]
     L.wisp_kv8_append.argtypes = [C.POINTER(wisp_kv8_batch), C.POINTER(wisp_kv8), _VP, C.c_int64, _VP, _VP]
     L.wisp_attention_kv8.argtypes = [C.POINTER(wisp_kv8_batch), C.POINTER(wisp_kv8), _VP, _VP, _VP]
-    for name in ("wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
+    L.wisp_token_logprobs_workspace_size.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+    L.wisp_token_logprobs_workspace_size.restype = C.c_size_t
+    L.wisp_token_logprobs.argtypes = [_VP, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, _VP, C.c_int32, _VP, _VP,
+                                      _VP, _VP, _VP, C.c_size_t, _VP]
+    for name in ("wisp_token_logprobs", "wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
                  "wisp_check", "wisp_gemm_plan", "wisp_attention_plan", "wisp_profile_enable", "wisp_profile_read", "wisp_profile_reset",
                  "wisp_schedule", "wisp_kvm_create", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit",
                  "wisp_kvm_release", "wisp_kvm_get_stats", "wisp_draft_stats", "wisp_reject_predict"):
@@ -603,6 +607,47 @@ def wisp_draft_stats(logits, vocab: int, temperature: float, stats, ws=None, str
         ws = workspace(lib.wisp_draft_stats_workspace_size(rows, vocab))
     _ok(lib.wisp_draft_stats(_dev(logits, "logits", dtype=_f32(), contiguous=False), rows, vocab, logits.stride(0),
                              temperature, _dev(stats, "stats", rows * 4, dtype=_f32()), *_ws(ws), _stream(stream)))
+
+
+def wisp_token_logprobs_workspace_size(rows: int, vocab: int, n_top: int) -> int:
+    return int(lib.wisp_token_logprobs_workspace_size(rows, vocab, n_top))
+
+
+def wisp_token_logprobs(logits, vocab: int, tokens, temperature: float, logprob, entropy=None, top_tokens=None,
+                        top_logprobs=None, ws=None, stream=None):
+    """ln p of `tokens` (int32 [rows], -1: row passed over), the entropy and the most probable
+    tokens (top_tokens int32, top_logprobs fp32, both [rows][n_top]) of logits rows [rows][ld],
+    fp32 or bf16, of which the first `vocab` entries of a row count.  tokens, logprob, entropy and
+    the top outputs may be None.  `ws` (a device byte tensor of wisp_token_logprobs_workspace_size bytes,
+    as workspace() makes it) is allocated when not given."""
+    import torch
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or logits.shape[1] < vocab:
+        raise ValueError(f"logits: expected [rows][>= {vocab}] with unit column stride")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"logits: dtype {logits.dtype}, expected float32 or bfloat16")
+    rows = logits.shape[0]
+    if (top_tokens is None) != (top_logprobs is None):
+        raise ValueError("top_tokens and top_logprobs come together")
+    n_top = 0
+    if top_tokens is not None:
+        if top_tokens.dim() != 2 or top_tokens.shape[0] != rows or top_tokens.shape != top_logprobs.shape:
+            raise ValueError(f"top_tokens, top_logprobs: expected [{rows}][n_top], got {tuple(top_tokens.shape)}, "
+                             f"{tuple(top_logprobs.shape)}")
+        n_top = top_tokens.shape[1]
+    opt = lambda t, what, n, dt: None if t is None else _dev(t, what, n, dtype=dt)
+    px = _dev(logits, "logits", contiguous=False)
+    ptrs = (opt(tokens, "tokens", rows, _i32()), opt(logprob, "logprob", rows, _f32()), opt(entropy, "entropy", rows, _f32()),
+            opt(top_tokens, "top_tokens", rows * n_top, _i32()), opt(top_logprobs, "top_logprobs", rows * n_top, _f32()))
+    if ws is None:
+        ws = workspace(wisp_token_logprobs_workspace_size(rows, vocab, n_top), logits.device)
+    for what, t in (("tokens", tokens), ("logprob", logprob), ("entropy", entropy), ("top_tokens", top_tokens),
+                    ("top_logprobs", top_logprobs), ("ws", ws)):
+        if t is not None and t.device != logits.device:
+            raise ValueError(f"{what}: on {t.device}, logits on {logits.device}")
+    ld = logits.stride(0) if rows > 1 else max(logits.shape[1], vocab)
+    code = WISP_F32 if logits.dtype == torch.float32 else WISP_BF16
+    _on(logits.device, stream, lambda s: _ok(lib.wisp_token_logprobs(
+        px, code, rows, vocab, ld, temperature, ptrs[0], n_top, ptrs[1], ptrs[2], ptrs[3], ptrs[4], *_ws(ws), s)))
 
 
 class RejectMLP:

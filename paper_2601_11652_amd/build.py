@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwisp.so")
 SOURCES = ["wisp_api.hip", "gemm.hip", "gemm_tile.hip", "attention.hip", "layers.hip", "sampler.hip", "draft_stats.hip",
-           "kv8_api.hip", "kv8_append.hip", "attention_kv8.hip", "scheduler.cpp", "kv_manager.cpp"]
+           "kv8_api.hip", "kv8_append.hip", "attention_kv8.hip", "token_logprobs.hip", "scheduler.cpp", "kv_manager.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,366 @@
+// What a server tells about the tokens of its answer (the rows that wisp_verify scored): the log
+// probability of each given token, the entropy of its distribution and the most probable tokens.
+// Declared in include/wisp.h.
+//
+// One pass over the logits: a workgroup holds a chunk of a row in registers, takes its maximum m
+// and the sums s = sum e^((x - m) / T) and c = sum (x - m) e^((x - m) / T), x - m formed first, so that
+// large logits lose nothing.  With the chunks joined, ln p(t) = (x_t - m) / T - ln s and the entropy is
+// ln s - c / (s T).  For the most probable tokens the pass also leaves the largest of each group of 32
+// entries: the k-th largest of those bounds the k-th largest entry from below, and only the
+// few groups that reach it are read again.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "api.h"
+#include "host_guard.h"
+#include "kernels.h"
+#include "wave_reduce.h"
+
+using namespace wisp;
+
+namespace {
+
+constexpr int kChunk = 8192, kThreads = 256, kGroup = kChunk / kThreads;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Part {   // of one chunk: the maximum, and the sums about it (0 where nothing is above -inf)
+  double s, c;
+  float m, pad;
+};
+
+// Entry j of thread t's group sits at entry_at(t, j) of its chunk: a group is what one thread loads
+template <int W>   // consecutive entries of a load
+__device__ __forceinline__ int entry_at(int t, int j) { return ((j / W) * kThreads + t) * W + j % W; }
+
+template <typename T> __device__ __forceinline__ float logit(const T *x, int64_t i);
+template <> __device__ __forceinline__ float logit<float>(const float *x, int64_t i) { return x[i]; }
+template <> __device__ __forceinline__ float logit<uint16_t>(const uint16_t *x, int64_t i) { return bf2f(x[i]); }
+
+// of the row of a workgroup; false: the row has no token, and is left as it was
+__device__ __forceinline__ bool row_counts(const int32_t *tokens, int64_t row) { return !tokens || tokens[row] != -1; }
+
+__device__ __forceinline__ Part join(const Part &a, const Part &b, double sc) {
+  // about the larger maximum; a side without entries (s = 0) adds nothing, a NaN stays
+  Part r;
+  r.m = fmaxf(a.m, b.m);
+  r.pad = 0.f;
+  auto side = [&](const Part &p, double &s, double &c) {
+    const double d = p.m == r.m ? 0.0 : (double)p.m - (double)r.m, w = exp2(d * sc);
+    s = p.s == 0.0 ? 0.0 : p.s * w;
+    c = p.s == 0.0 ? 0.0 : w * (p.c + d * p.s);
+  };
+  double s1, c1, s2, c2;
+  side(a, s1, c1);
+  side(b, s2, c2);
+  r.s = s1 + s2;
+  r.c = c1 + c2;
+  return r;
+}
+
+// grid rows x chunks, chunks fastest
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
+                                                                 float sc, const int32_t *__restrict__ tokens,
+                                                                 Part *__restrict__ parts, float *__restrict__ gmax) {
+  constexpr int W = VEC ? 16 / (int)sizeof(T) : 1;
+  const int64_t row = blockIdx.x / nch;
+  const int ch = blockIdx.x % nch, t = threadIdx.x;
+  if (!row_counts(tokens, row)) return;
+  const int base = ch * kChunk, n = min(V - base, kChunk);
+  const T *x = logits + row * ld + base;
+  float v[kGroup];
+  if constexpr (VEC) {
+    uint4 raw[kGroup / W];
+#pragma unroll
+    for (int k = 0; k < kGroup / W; ++k) {   // all loads of the thread in flight at once
+      const int e = (k * kThreads + t) * W;
+      raw[k] = make_uint4(0, 0, 0, 0);
+      if (e + W <= n) raw[k] = ld16_stream(x + e);
+    }
+#pragma unroll
+    for (int k = 0; k < kGroup / W; ++k) {
+      const int e = (k * kThreads + t) * W;
+      const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        float f;
+        if constexpr (sizeof(T) == 4) f = __uint_as_float(w[i]);
+        else f = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        if (e + W > n) f = e + i < n ? logit(x, e + i) : -INFINITY;
+        v[k * W + i] = f;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) {
+      const int e = entry_at<1>(t, k);
+      v[k] = e < n ? logit(x, e) : -INFINITY;
+    }
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kGroup; ++k) m = fmaxf(m, v[k]);
+  if (gmax) gmax[(row * nch + ch) * kThreads + t] = m;
+  // sums about the wave's maximum; in a wave of nothing but -inf about 0, where they are 0
+  const float mw = wave_max(m), mc = mw == -INFINITY ? 0.f : mw;
+  float s = 0.f, c = 0.f;
+#pragma unroll
+  for (int k = 0; k < kGroup; ++k) {
+    const float d = v[k] - mc, e = __builtin_amdgcn_exp2f(d * sc);
+    s += e;
+    c = fmaf(fmaxf(d, -3.4e38f), e, c);   // -inf x 0 stays out; a NaN enters through e
+  }
+  s = wave_sum(s);
+  c = wave_sum(c);
+  __shared__ Part sh[kThreads / 64];
+  if ((t & 63) == 0) sh[t >> 6] = Part{s, c, mw, 0.f};
+  __syncthreads();
+  if (t == 0) parts[row * nch + ch] = join(join(sh[0], sh[1], sc), join(sh[2], sh[3], sc), sc);
+}
+
+// order-preserving key of a float; -inf is the least
+__device__ __forceinline__ uint32_t key_of(float f) {
+  const uint32_t u = __float_as_uint(f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int kCand = 1024;   // candidates, and groups read again, that the quick way takes
+
+struct Best {
+  float v[kCand];
+  int32_t i[kCand];
+};
+
+// The n candidates' ranks (by value, then index): those below k are written out.
+__device__ void write_ranked(const Best &b, int n, int k, const double m, double T, double lse, int32_t *ids, float *lps) {
+  for (int a = threadIdx.x; a < n; a += kThreads) {
+    const float v = b.v[a];
+    const int id = b.i[a];
+    int rank = 0;
+    for (int o = 0; o < n; ++o) rank += b.v[o] > v || (b.v[o] == v && b.i[o] < id);
+    if (rank < k) {
+      ids[rank] = id;
+      lps[rank] = (float)(((double)v - m) / T - lse);
+    }
+  }
+}
+
+// One workgroup per row.
+template <typename T, int W>
+__global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
+                                                               float temperature, const int32_t *__restrict__ tokens,
+                                                               const Part *__restrict__ parts, const float *__restrict__ gmax,
+                                                               int top, float *__restrict__ logprob,
+                                                               float *__restrict__ entropy, int32_t *__restrict__ top_ids,
+                                                               float *__restrict__ top_lps, int *__restrict__ err) {
+  const int64_t row = blockIdx.x;
+  const int t = threadIdx.x;
+  if (!row_counts(tokens, row)) return;
+  const T *x = logits + row * ld;
+  const double sc = (double)(kLog2e / temperature), Td = temperature;
+  __shared__ Part sh_part;
+  if (t < 64) {
+    Part p{0.0, 0.0, -INFINITY, 0.f};
+    for (int c = t; c < nch; c += 64) p = join(p, parts[row * nch + c], sc);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const Part q{__shfl_xor(p.s, o), __shfl_xor(p.c, o), __shfl_xor(p.m, o), 0.f};
+      p = t & o ? join(q, p, sc) : join(p, q, sc);   // the same order in both lanes
+    }
+    if (t == 0) sh_part = p;
+  }
+  __syncthreads();
+  const Part p = sh_part;
+  const bool none = p.s == 0.0;                // every logit is -inf
+  const double lse = log(p.s), m = p.m;
+  if (t == 0) {
+    if (logprob) {
+      const int tok = tokens[row];
+      float lp = NAN;
+      if (tok < 0 || tok >= V) {
+        flag_error(err, kErrToken);
+      } else {
+        const float xt = logit(x, tok);
+        lp = none || xt == -INFINITY ? (p.s != p.s ? NAN : -INFINITY) : (float)(((double)xt - m) / Td - lse);
+      }
+      logprob[row] = lp;
+    }
+    if (entropy) entropy[row] = none ? 0.f : (float)(lse - p.c / p.s / Td);
+  }
+  if (top == 0) return;
+
+  int32_t *ids = top_ids + row * top;
+  float *lps = top_lps + row * top;
+  const float *gm = gmax + row * nch * kThreads;
+  const int groups = nch * kThreads;
+  __shared__ float sh_max[kThreads];
+  __shared__ Best best;
+  __shared__ int32_t sh_group[kCand];
+  __shared__ int sh_n, sh_groups;
+  __shared__ float sh_tau;
+  if (t == 0) {
+    sh_n = 0;
+    sh_groups = 0;
+    sh_tau = -INFINITY;
+  }
+  for (int r = t; r < top; r += kThreads) {    // places that no entry fills
+    ids[r] = -1;
+    lps[r] = p.s != p.s ? NAN : -INFINITY;
+  }
+  // the top-th largest of the threads' maxima: at least `top` entries reach it
+  float mine = -INFINITY;
+  for (int g = t; g < groups; g += kThreads) mine = fmaxf(mine, gm[g]);
+  sh_max[t] = mine;
+  __syncthreads();
+  int rank = 0;
+  for (int o = 0; o < kThreads; ++o) rank += sh_max[o] > mine || (sh_max[o] == mine && o < t);
+  if (rank == top - 1) sh_tau = mine;
+  __syncthreads();
+  const float tau = sh_tau;
+  for (int g = t; g < groups; g += kThreads) {
+    const float v = gm[g];
+    if (v >= tau && v > -INFINITY) {
+      const int at = atomicAdd(&sh_groups, 1);   // the order does not matter: candidates are ranked
+      if (at < kCand) sh_group[at] = g;
+    }
+  }
+  __syncthreads();
+  const int ng = sh_groups;
+  if (ng <= kCand) {
+    for (int u = t; u < ng * kGroup; u += kThreads) {
+      const int g = sh_group[u / kGroup], e = g / kThreads * kChunk + entry_at<W>(g % kThreads, u % kGroup);
+      if (e >= V) continue;
+      const float v = logit(x, e);
+      if (v >= tau && v > -INFINITY) {
+        const int at = atomicAdd(&sh_n, 1);
+        if (at < kCand) {
+          best.v[at] = v;
+          best.i[at] = e;
+        }
+      }
+    }
+    __syncthreads();
+    if (sh_n <= kCand) {
+      write_ranked(best, sh_n, top, m, Td, lse, ids, lps);
+      return;
+    }
+  }
+
+  // Too many reach the bound (a mask's lowest value in most places, say): the top-th largest
+  // key by four passes over its bytes, then one pass in order for what is above it and for the
+  // first that equal it.
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t sh_prefix, sh_left;
+  uint32_t prefix = 0, left = top;               // keys wanted among those with this prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    __syncthreads();
+    hist[t] = 0;
+    __syncthreads();
+    for (int e = t; e < (V + 63) / 64 * 64; e += kThreads) {   // whole waves
+      const float v = e < V ? logit(x, e) : -INFINITY;
+      const uint32_t key = key_of(v);
+      const bool in = e < V && v > -INFINITY && (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8));
+      const int bin = key >> shift & 255;
+      uint64_t todo = __builtin_amdgcn_ballot_w64(in);
+      if (todo == 0) continue;
+      const int lead = __builtin_ctzll(todo), one = __shfl(bin, lead);
+      const uint64_t same = __builtin_amdgcn_ballot_w64(in && bin == one);   // equal values: one count
+      if ((t & 63) == lead) atomicAdd(&hist[one], (uint32_t)__popcll(same));
+      if (in && bin != one) atomicAdd(&hist[bin], 1u);
+    }
+    __syncthreads();
+    if (t == 0) {
+      uint32_t seen = 0;
+      int b = 255;
+      while (b > 0 && seen + hist[b] < left) seen += hist[b--];
+      sh_prefix = prefix | (uint32_t)b << shift;
+      sh_left = left - min(seen, left);
+    }
+    __syncthreads();
+    prefix = sh_prefix;
+    left = sh_left;
+  }
+  // fewer entries than places: the key ends at the smallest there is, and all are taken
+  if (t == 0) sh_n = 0;
+  __shared__ uint32_t sh_count[kThreads / 64];
+  uint32_t equal_before = 0;
+  __syncthreads();
+  for (int e0 = 0; e0 < V; e0 += kThreads) {
+    const int e = e0 + t;
+    const float v = e < V ? logit(x, e) : -INFINITY;
+    const uint32_t key = key_of(v);
+    const bool here = e < V && v > -INFINITY;
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(here && key == prefix);
+    if ((t & 63) == 0) sh_count[t >> 6] = __popcll(eq);
+    __syncthreads();
+    uint32_t at = equal_before + __popcll(eq & ((1ull << (t & 63)) - 1));
+    for (int w = 0; w < (t >> 6); ++w) at += sh_count[w];
+    if (here && (key > prefix || (key == prefix && at < left))) {
+      const int k = atomicAdd(&sh_n, 1);
+      if (k < kCand) {
+        best.v[k] = v;
+        best.i[k] = e;
+      }
+    }
+    for (int w = 0; w < kThreads / 64; ++w) equal_before += sh_count[w];
+    __syncthreads();
+  }
+  write_ranked(best, min(sh_n, kCand), top, m, Td, lse, ids, lps);
+}
+
+int chunks_of(int32_t vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
+
+}  // namespace
+
+extern "C" size_t wisp_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t n_top) {
+  if (rows < 0 || vocab < 1 || n_top < 0 || n_top > WISP_TOP_MAX) return 0;
+  const size_t n = (size_t)rows * chunks_of(vocab);
+  return 256 + align256(n * sizeof(Part)) + (n_top ? align256(n * kThreads * 4) : 0);
+}
+
+extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t ld,
+                                           float temperature, const int32_t *tokens, int32_t n_top, float *logprob,
+                                           float *entropy, int32_t *top_tokens, float *top_logprobs, void *workspace,
+                                           size_t workspace_bytes, void *stream) {
+  return guarded("wisp_token_logprobs", [&]() -> wisp_status {
+    if (rows < 0 || vocab < 1 || ld < vocab) return fail(WISP_E_INVALID, "rows < 0, vocab < 1 or ld < vocab");
+    if (!(temperature > 0.f) || isinf(temperature)) return fail(WISP_E_INVALID, "temperature must be finite and > 0");
+    if (n_top < 0 || n_top > WISP_TOP_MAX) return fail(WISP_E_INVALID, "n_top = %d outside 0..%d", n_top, WISP_TOP_MAX);
+    if (dtype != WISP_F32 && dtype != WISP_BF16) return fail(WISP_E_UNSUPPORTED, "dtype %d", dtype);
+    if (logprob && !tokens) return fail(WISP_E_INVALID, "logprob without tokens");
+    if (n_top > 0 && (!top_tokens || !top_logprobs)) return fail(WISP_E_INVALID, "NULL top_tokens / top_logprobs");
+    if (vocab > 1 << 30) return fail(WISP_E_UNSUPPORTED, "vocab > 2^30");
+    if (rows == 0) return WISP_OK;
+    const int nch = chunks_of(vocab);
+    if ((int64_t)rows * nch > INT32_MAX) return fail(WISP_E_UNSUPPORTED, "more than 2^31 - 1 chunks of 8192 logits in one call");
+    if (!logits || !workspace) return fail(WISP_E_INVALID, "NULL logits / workspace");
+    if ((uintptr_t)workspace & 15) return fail(WISP_E_INVALID, "workspace must be 16-byte aligned");
+    if ((uintptr_t)logits & (dtype == WISP_F32 ? 3 : 1)) return fail(WISP_E_INVALID, "logits not aligned to their type");
+    const size_t need = wisp_token_logprobs_workspace_size(rows, vocab, n_top);
+    if (workspace_bytes < need) return fail(WISP_E_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    char *ws = static_cast<char *>(workspace);
+    Part *parts = reinterpret_cast<Part *>(ws + 256);
+    float *gmax = n_top ? reinterpret_cast<float *>(ws + 256 + align256((size_t)rows * nch * sizeof(Part))) : nullptr;
+    int *err = reinterpret_cast<int *>(ws);
+    const hipStream_t s = (hipStream_t)stream;
+    const float sc = kLog2e / temperature;
+    auto go = [&](auto *x, auto chunk, auto row) {
+      launch(chunk, (uint32_t)(rows * nch), kThreads, 0, s, x, (int)vocab, ld, nch, sc, tokens, parts, gmax);
+      launch(row, (uint32_t)rows, kThreads, 0, s, x, (int)vocab, ld, nch, temperature, tokens, (const Part *)parts,
+             (const float *)gmax, (int)n_top, logprob, entropy, top_tokens, top_logprobs, err);
+    };
+    const int es = dtype == WISP_F32 ? 4 : 2;
+    const bool vec = ((uintptr_t)logits & 15) == 0 && ld * es % 16 == 0;
+    if (dtype == WISP_F32) {
+      const float *x = static_cast<const float *>(logits);
+      vec ? go(x, logprobs_chunk_kernel<float, true>, logprobs_row_kernel<float, 4>)
+          : go(x, logprobs_chunk_kernel<float, false>, logprobs_row_kernel<float, 1>);
+    } else {
+      const uint16_t *x = static_cast<const uint16_t *>(logits);
+      vec ? go(x, logprobs_chunk_kernel<uint16_t, true>, logprobs_row_kernel<uint16_t, 8>)
+          : go(x, logprobs_chunk_kernel<uint16_t, false>, logprobs_row_kernel<uint16_t, 1>);
+    }
+    return hip_check("wisp_token_logprobs");
+  });
+}
