@@ -255,8 +255,8 @@ wisp_status wisp_attention(const wisp_model *model, const wisp_kv *kv, const wis
  * A page's value is code * scale.  Inside one page (slot s, dim e) sits at
  *   K:  (((e / 32) * 4 + (e % 32) / 8) * 8 + (s / 8) * 4 + s % 4) * 16 + ((s / 4) % 2) * 8 + e % 8
  *   V:  ((e / 32) * 2 + s / 8) * 256 + (e % 16) * 16 + ((e / 16) % 2) * 8 + s % 8
- * (a lane's K or V operands of two matrix products are one 16-byte load).  The three pointers are
- * 16-byte aligned.  Scales of pages in use are positive and finite, their V codes no NaN; both
+ * (a lane's K or V operands of two matrix products are one 16-byte load).  The pools are 16-byte
+ * aligned, the scales 8-byte.  Scales of pages in use are positive and finite, their V codes no NaN; both
  * hold for whatever wisp_kv8_append writes.  One layer's operators take that layer's pools.
  */
 typedef struct {
@@ -308,6 +308,19 @@ wisp_status wisp_kv8_append(const wisp_kv8_batch *batch, const wisp_kv8 *kv, con
  * Contexts may be of any length (no limit for fp32 models).
  */
 wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *q, void *out, void *stream);
+
+/*
+ * wisp_verify on the 8-bit cache: the same step, its K and V appended and read by the two
+ * operators above (a step's plan is its own).  Inputs, outputs, errors and the rollback by length as
+ * wisp_verify's; the workspace holds wisp_verify_kv8_workspace_size bytes, plus
+ * wisp_logits_workspace_size when target_logits is NULL.  An fp32 model's contexts have no limit
+ * of their own.
+ */
+size_t wisp_verify_kv8_workspace_size(const wisp_model *model, const wisp_batch_desc *desc);
+wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const wisp_batch_desc *desc,
+                            const int32_t *tokens, const float *draft_probs, uint64_t rng_seed, int32_t *accept_len,
+                            int32_t *out_tokens, float *target_logits, void *workspace, size_t workspace_bytes,
+                            void *stream);
 
 /* Uniform draws of the step's random stream: out[k] = draw (seed, req_id, tag, row, k),
  * k < n (DEVICE fp32).  tag 1 = acceptance, 2 = race. */

@@ -45,7 +45,8 @@ EXPORTS = ("wisp_workspace_size", "wisp_logits_workspace_size", "wisp_accept_wor
            "wisp_kvm_destroy", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit", "wisp_kvm_release",
            "wisp_kvm_get_stats", "wisp_draft_stats_workspace_size", "wisp_draft_stats", "wisp_reject_predict",
            "wisp_gemm_plan", "wisp_attention_plan", "wisp_verify_noalloc", "wisp_kv8_workspace_size", "wisp_kv8_plan",
-           "wisp_kv8_append", "wisp_attention_kv8", "wisp_token_logprobs_workspace_size", "wisp_token_logprobs")
+           "wisp_kv8_append", "wisp_attention_kv8", "wisp_verify_kv8_workspace_size", "wisp_verify_kv8",
+           "wisp_token_logprobs_workspace_size", "wisp_token_logprobs")
 
 
 class WispError(RuntimeError):
@@ -179,7 +180,11 @@ def _load():
     L.wisp_token_logprobs_workspace_size.restype = C.c_size_t
     L.wisp_token_logprobs.argtypes = [_VP, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, _VP, C.c_int32, _VP, _VP,
                                       _VP, _VP, _VP, C.c_size_t, _VP]
-    for name in ("wisp_token_logprobs", "wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
+    L.wisp_verify_kv8_workspace_size.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc)]
+    L.wisp_verify_kv8_workspace_size.restype = C.c_size_t
+    L.wisp_verify_kv8.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_kv8), C.POINTER(wisp_batch_desc),
+                                  _VP, _VP, C.c_uint64, _VP, _VP, _VP, _VP, C.c_size_t, _VP]
+    for name in ("wisp_verify_kv8", "wisp_token_logprobs", "wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
                  "wisp_check", "wisp_gemm_plan", "wisp_attention_plan", "wisp_profile_enable", "wisp_profile_read", "wisp_profile_reset",
                  "wisp_schedule", "wisp_kvm_create", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit",
                  "wisp_kvm_release", "wisp_kvm_get_stats", "wisp_draft_stats", "wisp_reject_predict"):
@@ -573,6 +578,27 @@ def wisp_attention_kv8(batch: KV8Batch, kv: KV8Pool, q, out, stream=None):
     pq, po = _dev(q, "q", n, dtype=batch.dtype), _dev(out, "out", n, dtype=batch.dtype)
     _kv8_check(batch, kv, (("q", q), ("out", out)))
     _on(batch.device, stream, lambda s: _ok(lib.wisp_attention_kv8(C.byref(batch.c), C.byref(kv.c), pq, po, s)))
+
+
+def wisp_verify_kv8_workspace_size(model: wisp_model, desc: BatchDesc) -> int:
+    return int(lib.wisp_verify_kv8_workspace_size(C.byref(model), C.byref(desc.c)))
+
+
+def wisp_verify_kv8(model: wisp_model, kv: KV8Pool, desc: BatchDesc, tokens, draft_probs, rng_seed: int,
+                    accept_len, out_tokens, target_logits, workspace, stream=None):
+    """wisp_verify on the 8-bit cache (workspace: wisp_verify_kv8_workspace_size bytes)."""
+    _check_desc(desc)
+    if tuple(kv.k.shape[2:]) != (model.n_kv_heads, PAGE * model.head_dim) or kv.k.shape[0] < model.n_layers:
+        raise ValueError(f"kv: {tuple(kv.k.shape)}, expected [>= {model.n_layers}][blocks][{model.n_kv_heads}]"
+                         f"[{PAGE * model.head_dim}]")
+    V = model.vocab
+    probs = _dev(draft_probs, "draft_probs", desc.S * V, dtype=_f32()) if desc.S > 0 else _ptr(draft_probs)
+    logits = None if target_logits is None else _dev(target_logits, "target_logits", desc.M * V, dtype=_f32())
+    _ok(lib.wisp_verify_kv8(C.byref(model), C.byref(kv.c), C.byref(desc.c),
+                            _dev(tokens, "tokens", desc.rows, dtype=_i32()), probs, rng_seed & ((1 << 64) - 1),
+                            _dev(accept_len, "accept_len", desc.B, dtype=_i32()),
+                            _dev(out_tokens, "out_tokens", desc.M, dtype=_i32()), logits, *_ws(workspace),
+                            _stream(stream)))
 
 
 def wisp_uniform(rng_seed: int, req_id: int, tag: int, row: int, n: int, out, stream=None):

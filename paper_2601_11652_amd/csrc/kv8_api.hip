@@ -126,8 +126,8 @@ wisp_status wisp::kv8_cache(Kv8Cache &c, const wisp_kv8 *kv) {
   if (!kv || !kv->k_pool || !kv->v_pool || !kv->scale) return fail(WISP_E_INVALID, "8-bit KV pools or scales are NULL");
   if (kv->page_size != WISP_PAGE) return fail(WISP_E_UNSUPPORTED, "page_size must be %d", WISP_PAGE);
   if (kv->n_blocks <= 0) return fail(WISP_E_INVALID, "n_blocks must be positive");
-  if (((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool | (uintptr_t)kv->scale) & 15)
-    return fail(WISP_E_INVALID, "8-bit KV pools and scales must be 16-byte aligned");
+  if ((((uintptr_t)kv->k_pool | (uintptr_t)kv->v_pool) & 15) || ((uintptr_t)kv->scale & 7))
+    return fail(WISP_E_INVALID, "8-bit KV pools must be 16-byte aligned, their scales 8-byte");
   c = Kv8Cache{static_cast<uint8_t *>(kv->k_pool), static_cast<uint8_t *>(kv->v_pool), kv->scale, kv->n_blocks};
   return WISP_OK;
 }

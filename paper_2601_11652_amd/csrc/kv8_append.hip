@@ -268,7 +268,7 @@ void append(const Kv8Plan &p, const Kv8Cache &c, const QkvRows &src, T *q, int *
   else if (src.splits == 1) go(kv8_append_kernel<T, 1>);
   else if (src.splits == 2) go(kv8_append_kernel<T, 2>);
   else if (src.splits <= 4) src.splits == 3 ? go(kv8_append_kernel<T, 3>) : go(kv8_append_kernel<T, 4>);
-  else go(kv8_append_kernel<T, 16>);
+  else src.splits <= 8 ? go(kv8_append_kernel<T, 8>) : go(kv8_append_kernel<T, 16>);
 }
 
 }  // namespace

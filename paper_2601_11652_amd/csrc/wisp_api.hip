@@ -17,7 +17,7 @@
 #include "api.h"
 #include "host_guard.h"
 #include "kernels.h"
-#include "kv8.h"
+#include "kv8_plan.h"
 
 using namespace wisp;
 
@@ -63,6 +63,7 @@ struct Plan {
          w_rR = 0, w_vtok = 0, total = 0;
   int max_group_chunks = 0;          // most chunks any attention group combines
   int race_chunk = 0;                // vocabulary entries per workgroup of the acceptance's race
+  bool kv8 = false;                  // the step runs on the 8-bit cache, which has a plan of its own
 };
 
 
@@ -441,7 +442,7 @@ wisp_status make_plan(Plan &p, const wisp_model *m, const wisp_batch_desc *d, bo
       p.g_lm = gemm_bf16_plan(p.Mv, p.V, p.d);
       p.g_lm.splits = 1;
       p.g_lm.kf_per_split = p.d / 16;
-      wisp_status st = plan_attention(p, d, nrow, SIZE_MAX);
+      wisp_status st = p.kv8 ? WISP_OK : plan_attention(p, d, nrow, SIZE_MAX);
       if (st != WISP_OK) return st;
     }
   }
@@ -703,8 +704,15 @@ int gemm_class(const Plan &p, const GemmCfg &c) {
   return c.kind == 2 ? WISP_PROF_GEMM_RING2 : WISP_PROF_GEMM_RING1;
 }
 
+// the step's 8-bit cache, its pools and the batch's plan for it
+struct Kv8Step {
+  Kv8Cache cache;   // layer 0's
+  const Kv8Plan *plan;
+};
+
+// kv, or the 8-bit cache k8
 template <typename T>
-wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, const StepDesc &sd,
+wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, const Kv8Step *k8, const StepDesc &sd,
                         char *ws, const int32_t *tokens, float *logits, hipStream_t s) {
   const bool packed = p.bf16;
   float *cs = reinterpret_cast<float *>(ws + p.w_rope);
@@ -714,7 +722,7 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
   T *af = reinterpret_cast<T *>(ws + p.w_af);
   T *qb = reinterpret_cast<T *>(ws + p.w_q);
   float *part = reinterpret_cast<float *>(ws + p.w_part);
-  const int64_t layer_elems = (int64_t)kv->n_blocks * p.nkv * WISP_PAGE * p.hd;
+  const int64_t layer_pages = (int64_t)sd.n_blocks * p.nkv, layer_elems = layer_pages * WISP_PAGE * p.hd;
   const AttnItem *items = reinterpret_cast<const AttnItem *>(ws + p.w_desc + p.i_items * 4);
   const AttnGroup *groups = reinterpret_cast<const AttnGroup *>(ws + p.w_desc + p.i_groups * 4);
   const int32_t *first = p.first.empty() ? nullptr : reinterpret_cast<const int32_t *>(ws + p.w_desc) + p.i_first;
@@ -735,6 +743,12 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
     if (rbg == 0) attn_bytes += (double)tokens * kv_tok / p.nkv;
     attn_flops += 4.0 * p.hd * nr * tokens;
   }
+  if (k8)   // a byte per element and the pages' two scales
+    for (int i = 0; i < p.B; ++i) {
+      const double rows = p.host[p.i_nrow + i], ctx = p.host[p.i_ctx + i];
+      attn_bytes += 2.0 * p.nkv * (ctx + rows) * (p.hd + 4.0 / WISP_PAGE);
+      attn_flops += 4.0 * p.hd * p.nq * rows * (ctx + (rows + 1) / 2);
+    }
   {
     ProfScope ps(WISP_PROF_ROWS, 0, 0, s);
     rope_table(sd, cs, p.M, p.hd, m->rope_base, s);
@@ -742,8 +756,8 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
                   p.V, m->rms_eps, s);
   }
   for (int l = 0; l < m->n_layers; ++l) {
-    T *kl = (T *)kv->k_pool + l * layer_elems;
-    T *vl = (T *)kv->v_pool + l * layer_elems;
+    T *kl = k8 ? nullptr : (T *)kv->k_pool + l * layer_elems;
+    T *vl = k8 ? nullptr : (T *)kv->v_pool + l * layer_elems;
     // one dense projection: C = act . W^T (fp32 partials over cfg.splits K ranges)
     auto gemm = [&](const T *act, const void *w, float *out, int N, int K, const GemmCfg &cfg) {
       ProfScope ps(gemm_class(p, cfg), gemm_bytes(N, K), gemm_flops(N, K), s);
@@ -754,11 +768,21 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
       return p.bf16 ? cfg.splits : 1;
     };
     const int sq = gemm(xn, m->w_qkv[l], part, p.qkvN, p.d, p.g_qkv);
-    {
+    if (k8) {
+      const Kv8Cache c{k8->cache.k + l * layer_elems, k8->cache.v + l * layer_elems, k8->cache.scale + l * layer_pages * 2,
+                       k8->cache.n_blocks};
+      {
+        ProfScope ps(WISP_PROF_ROWS, 0, 0, s);
+        kv8_append(*k8->plan, c, QkvRows{part, p.qkvN, (int64_t)p.M * p.qkvN, sq}, qb, sd.err, s);
+      }
+      ProfScope ps(WISP_PROF_ATTN, attn_bytes, attn_flops, s);
+      kv8_attention(*k8->plan, c, qb, ao, packed, sd.err, s);
+    } else {
       ProfScope ps(WISP_PROF_ROWS, 0, 0, s);
       qkv_rope_append<T>(sd, part, sq, cs, qb, kl, vl, p.M, p.nq, p.nkv, p.hd, s);
     }
-    if (p.bf16) {
+    if (k8) {
+    } else if (p.bf16) {
       float *po = reinterpret_cast<float *>(ws + p.w_attn_o);
       float *pml = reinterpret_cast<float *>(ws + p.w_attn_ml);
       {
@@ -819,14 +843,20 @@ namespace {
 
 // validation shared by the two verification entry points
 wisp_status check_verify(const wisp_model *model, const wisp_kv *kv, const wisp_batch_desc *desc,
-                         const int32_t *tokens, const int32_t *accept_len, const int32_t *out_tokens) {
+                         const int32_t *tokens, const int32_t *accept_len, const int32_t *out_tokens,
+                         const wisp_kv8 *kv8 = nullptr) {
   wisp_status st;
   if ((st = check_model(model, true)) != WISP_OK) return st;
   if ((st = check_desc(desc, true, true)) != WISP_OK) return st;
   if (desc->B == 0) return WISP_OK;
-  if (!kv || !kv->k_pool || !kv->v_pool) return fail(WISP_E_INVALID, "KV pools are NULL");
-  if (kv->page_size != WISP_PAGE) return fail(WISP_E_UNSUPPORTED, "page_size must be %d", WISP_PAGE);
-  if (kv->n_blocks <= 0) return fail(WISP_E_INVALID, "n_blocks must be positive");
+  Kv8Cache c;
+  if (kv8) {
+    if ((st = kv8_cache(c, kv8)) != WISP_OK) return st;
+  } else {
+    if (!kv || !kv->k_pool || !kv->v_pool) return fail(WISP_E_INVALID, "KV pools are NULL");
+    if (kv->page_size != WISP_PAGE) return fail(WISP_E_UNSUPPORTED, "page_size must be %d", WISP_PAGE);
+    if (kv->n_blocks <= 0) return fail(WISP_E_INVALID, "n_blocks must be positive");
+  }
   if (!tokens || !accept_len || !out_tokens) return fail(WISP_E_INVALID, "NULL tokens / outputs");
   return WISP_OK;
 }
@@ -836,21 +866,40 @@ wisp_status plan_verify(Plan &p, const wisp_model *model, const wisp_batch_desc 
   wisp_status st;
   if ((st = make_plan(p, model, desc, true, 0, limit)) != WISP_OK) return st;
   if (p.S > 0 && !draft_probs) return fail(WISP_E_INVALID, "draft_probs is NULL");
-  if (!p.bf16 && p.max_tokens > 32768) return fail(WISP_E_UNSUPPORTED, "fp32 path supports <= 32768 tokens per request");
+  if (!p.bf16 && !p.kv8 && p.max_tokens > 32768)
+    return fail(WISP_E_UNSUPPORTED, "fp32 path supports <= 32768 tokens per request");
+  return WISP_OK;
+}
+
+// A step on the 8-bit cache: the step's plan without its attention, and the cache's own, whose
+// lists travel in the step's descriptor block and whose partial results follow its workspace.
+wisp_status plan_kv8_step(Plan &p, Kv8Build &b, const wisp_model *model, const wisp_batch_desc *desc) {
+  wisp_status st;
+  p.kv8 = true;
+  if ((st = make_plan(p, model, desc, true)) != WISP_OK || (st = kv8_build(b, model, desc)) != WISP_OK) return st;
+  const size_t at = p.host.size();
+  p.host.insert(p.host.end(), b.host.begin(), b.host.end());
+  // the descriptor block has grown: everything behind it moves
+  const size_t grown = align256(p.host.size() * 4) - align256(at * 4);
+  for (size_t *w : {&p.w_rope, &p.w_h, &p.w_xn, &p.w_ao, &p.w_af, &p.w_q, &p.w_part, &p.w_sm, &p.w_si, &p.w_ss, &p.w_rk,
+                    &p.w_ri, &p.w_rR, &p.w_vtok, &p.total})
+    *w += grown;
+  kv8_place(b, nullptr, p.w_desc + at * 4, p.total);
+  b.p.w_cs = p.w_rope;   // the step's own table of rotations
   return WISP_OK;
 }
 
 // the step's kernel sequence on a planned, uploaded workspace `ws`; `err` (or NULL: the
 // workspace's own record) receives the device-side input faults
-wisp_status run_verify(const Plan &p, const wisp_model *model, const wisp_kv *kv, const wisp_batch_desc *desc,
-                       const int32_t *tokens, const float *draft_probs, uint64_t rng_seed, int32_t *accept_len,
+wisp_status run_verify(const Plan &p, const wisp_model *model, const wisp_kv *kv, const Kv8Step *k8,
+                       const wisp_batch_desc *desc, const int32_t *tokens, const float *draft_probs, uint64_t rng_seed, int32_t *accept_len,
                        int32_t *out_tokens, float *target_logits, char *ws, int *err, hipStream_t s) {
   wisp_status st;
-  StepDesc sd = step_desc(p, ws, desc, kv->n_blocks, err);
+  StepDesc sd = step_desc(p, ws, desc, k8 ? k8->cache.n_blocks : kv->n_blocks, err);
   if (p.bf16)
-    st = run_forward<uint16_t>(p, model, kv, sd, ws, tokens, target_logits, s);
+    st = run_forward<uint16_t>(p, model, kv, k8, sd, ws, tokens, target_logits, s);
   else
-    st = run_forward<float>(p, model, kv, sd, ws, tokens, target_logits, s);
+    st = run_forward<float>(p, model, kv, k8, sd, ws, tokens, target_logits, s);
   if (st != WISP_OK) return st;
   // the acceptance sees the verification rows only: row offsets over them, and (with
   // prompt rows present) their tokens gathered into a compact array
@@ -1029,7 +1078,45 @@ wisp_status wisp_verify(const wisp_model *model, const wisp_kv *kv, const wisp_b
     char *ws = (char *)workspace;
     if (!target_logits) target_logits = reinterpret_cast<float *>(ws + p.total);
     if ((st = upload(p, ws, s)) != WISP_OK) return st;
-    return run_verify(p, model, kv, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
+    return run_verify(p, model, kv, nullptr, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
+                      ws, nullptr, s);
+  });
+}
+
+size_t wisp_verify_kv8_workspace_size(const wisp_model *model, const wisp_batch_desc *desc) {
+  return guarded_size([&]() -> size_t {
+    if (check_model(model, false) != WISP_OK || check_desc(desc, false, true) != WISP_OK) return 0;
+    Plan p;
+    Kv8Build b;
+    return plan_kv8_step(p, b, model, desc) == WISP_OK ? b.p.total : 0;
+  });
+}
+
+wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const wisp_batch_desc *desc,
+                            const int32_t *tokens, const float *draft_probs, uint64_t rng_seed, int32_t *accept_len,
+                            int32_t *out_tokens, float *target_logits, void *workspace, size_t workspace_bytes,
+                            void *stream) {
+  return guarded("wisp_verify_kv8", [&]() -> wisp_status {
+    wisp_status st;
+    if (!kv) return fail(WISP_E_INVALID, "8-bit KV cache is NULL");
+    if ((st = check_verify(model, nullptr, desc, tokens, accept_len, out_tokens, kv)) != WISP_OK) return st;
+    if (desc->B == 0) return WISP_OK;
+    if (!workspace) return fail(WISP_E_INVALID, "NULL workspace");
+    Plan p;
+    Kv8Build b;
+    if ((st = plan_kv8_step(p, b, model, desc)) != WISP_OK) return st;
+    if (p.S > 0 && !draft_probs) return fail(WISP_E_INVALID, "draft_probs is NULL");
+    const size_t need = b.p.total + (target_logits ? 0 : logits_bytes(p.Mv, p.V));
+    if (workspace_bytes < need)
+      return fail(WISP_E_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    const hipStream_t s = (hipStream_t)stream;
+    char *ws = (char *)workspace;
+    if (!target_logits) target_logits = reinterpret_cast<float *>(ws + b.p.total);
+    b.p.ws = ws;
+    if ((st = upload(p, ws, s)) != WISP_OK) return st;
+    Kv8Step k8{{}, &b.p};
+    if ((st = kv8_cache(k8.cache, kv)) != WISP_OK) return st;
+    return run_verify(p, model, nullptr, &k8, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
                       ws, nullptr, s);
   });
 }
@@ -1057,7 +1144,7 @@ wisp_status wisp_verify_noalloc(const wisp_model *model, const wisp_kv *kv, cons
     hipStream_t s = (hipStream_t)stream;
     if (!target_logits) target_logits = reinterpret_cast<float *>(ws + p.total);
     if ((st = upload_ints_by_arguments(p.host, ws + p.w_desc, s)) != WISP_OK) return st;
-    return run_verify(p, model, kv, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
+    return run_verify(p, model, kv, nullptr, desc, tokens, draft_probs, rng_seed, accept_len, out_tokens, target_logits,
                       ws, fault, s);
   });
 }
