@@ -1,15 +1,17 @@
 // Ragged multi-query causal attention over the 8-bit paged KV cache: the attention of Sec. 4.5's
 // batched one-step verification on e4m3 pages with one K and one V scale per page and kv head.
 //
-// A workgroup of four waves runs one item: a row group (16 RB of a request's rows x query heads of
-// one kv head) over a range of the request's tokens, each wave a quarter of the range's page
-// pairs.  Per pair a wave computes S^T = K Q^T and O^T += V^T P^T with 16x16x32 matrix products in
+// A workgroup of four waves runs a share of one kv head's work, items one after another: an item is
+// up to four row groups (16 RB of a request's rows x query heads each) over a range of the request's
+// tokens.  One row group's tokens are split over the four waves, two row groups have two waves
+// each, three or four one each: waves that share tokens read the same lines at the same time.  Per
+// page pair (32 tokens) a wave computes S^T = K Q^T and O^T += V^T P^T with 16x16x32 matrix products in
 // bf16, which holds every e4m3 value exactly: the codes are converted between load and product,
-// the K scale multiplies the scores and the V scale the probabilities (a lane's eight
-// tokens of a pair lie in one page, so each is one factor per lane).  Every query row stays in one
-// lane column (lane % 16), so the online softmax needs two cross-row steps, and the
-// probabilities leave the first product in the order that the second consumes.  The waves' partial
-// results are joined through LDS, those of a context cut into several items by a second kernel.
+// the K scale multiplies the scores and the V scale the probabilities (a lane's eight tokens of
+// a pair lie in one page, so each is one factor per lane).  Every query row stays in one lane column
+// (lane % 16), so the online softmax needs two cross-row steps, and the probabilities leave the
+// first product in the order that the second consumes.  The waves of a row group are joined
+// through LDS, the parts of a context that several items share by a second kernel.
 //
 // An fp32 model's queries and probabilities enter the products as three bf16 parts each (8 bits
 // of the significand per part: 24 in all), so its results are fp32's.
@@ -34,8 +36,20 @@ __device__ __forceinline__ bf16x8_t to_bf16(uint32_t lo, uint32_t hi) {
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
+// a barrier that orders LDS only: the loads ahead and the results' stores stay in flight
+// (__syncthreads waits for them too: 4 us at the end of every item)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// x, its value unknown to the compiler: what is computed from it at the end of an item stays there
+// (hoisted out of the loop over items, such offsets filled the registers that the codes ahead need)
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 struct Kv8Args {
   const Kv8Item *items;
+  const int32_t *first;   // share s runs items first[s] .. first[s + 1] - 1
   const int32_t *page_table;
   const uint8_t *k, *v;
   const float2 *scale;
@@ -49,237 +63,424 @@ struct Kv8Args {
 };
 
 template <int HD, int RB, bool F32>
-__global__ __launch_bounds__(256, RB <= 2 && HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Args a) {
-  constexpr int ROWS = 16 * RB;
+__global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Args a) {
+  constexpr int ROWS = 16 * RB;         // of a row group
   constexpr int KC = HD / 32;           // 32-wide chunks of the contraction; 16-byte loads of K and of V
   constexpr int MB = HD / 16;           // 16-wide blocks of the output dims
   constexpr int NP = F32 ? 3 : 1;       // bf16 parts of a query and of a probability
-  constexpr int kQBytes = NP * RB * KC * 64 * 16, kJoinBytes = 4 * RB * MB * 64 * 16;
-  __shared__ __attribute__((aligned(16))) char smem[kQBytes > kJoinBytes ? kQBytes : kJoinBytes];
-  __shared__ float sh_m[4][ROWS], sh_l[4][ROWS];
+  constexpr int LDJ = HD + 4;           // a row of a wave's accumulators in LDS, in floats: 16 bytes apart in banks
+  constexpr int kQueries = 4 * NP * RB * KC * 64, kJoin = 4 * ROWS * LDJ / 4;   // 16-byte units
+  // the row groups' queries in operand order while an item runs, the accumulators when it ends
+  __shared__ uint4 smem[kQueries > kJoin ? kQueries : kJoin];
+  __shared__ float2 sh_ml[4][ROWS];
+  uint4(*qs)[NP][RB][KC][64] = reinterpret_cast<uint4(*)[NP][RB][KC][64]>(smem);
+  float(*jo)[ROWS][LDJ] = reinterpret_cast<float(*)[ROWS][LDJ]>(smem);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lc = lane & 15, lg = lane >> 4;
-  const int kvh = blockIdx.x % a.nkv;   // neighbouring workgroups (other XCDs): other kv heads
-  const Kv8Item it = a.items[blockIdx.x / a.nkv];
-  const int G = a.nq / a.nkv, rows = it.nrow * G;
+  const int kvh = blockIdx.x % a.nkv;   // neighbouring workgroups, on other XCDs: other kv heads
+  const int G = a.nq / a.nkv;
+  int k = a.first[blockIdx.x / a.nkv];
+  const int k_end = a.first[blockIdx.x / a.nkv + 1];
+  if (k >= k_end) return;
 
-  // this wave's page pairs, their block ids (lane l: its l-th page) and scales
-  const int pairs = (it.t1 - it.t0 + 31) / 32;
-  const int pa = pairs * wave / 4, n = pairs * (wave + 1) / 4 - pa;
-  const int tok0 = it.t0 + 32 * pa;
-  int blk = 0;
-  float ks = 0.f, vs = 0.f, vs_inv = 0.f;
-  if (n > 0) {
-    const int pg = min((tok0 >> 4) + lane, (min(it.t1, tok0 + 32 * n) - 1) >> 4);
-    blk = a.page_table[(int64_t)it.req * a.pt_stride + pg];
-    if (blk < 0 || blk >= a.n_blocks) {
-      flag_error(a.err, kErrBlock);
-      blk = min(max(blk, 0), a.n_blocks - 1);
-    }
-  }
+  // What a wave does of an item: row group rg, tokens tok .. end - 1 in n page quads (64 tokens)
+  struct Share {
+    int rg, part, parts, tok, end, n;
+  };
+  auto share_of = [&](const Kv8Item &it) __attribute__((always_inline)) {
+    Share s;
+    const int groups = kv8_groups(it.groups), quads = (it.t1 - it.t0 + 63) / 64;
+    s.parts = groups == 1 ? 4 : groups == 2 ? 2 : 1;
+    s.rg = wave % groups;
+    s.part = wave / groups;              // of three groups' waves the fourth is idle: part 1 of 1
+    const int p = min(s.part, s.parts), from = quads * p / s.parts;
+    const int n = p < s.parts ? quads * (p + 1) / s.parts - from : 0;
+    s.tok = it.t0 + 64 * from;
+    s.end = min(it.t1, s.tok + 64 * n);
+    s.n = max(1, n);                     // with nothing to do one quad, all of it masked
+    return s;
+  };
+  auto item_at = [&](int i) __attribute__((always_inline)) { return a.items[min(i, k_end - 1)]; };
+  // block ids of up to 64 pages from token tok on, one per lane
+  auto ids_at = [&](const Kv8Item &it, int tok) __attribute__((always_inline)) {
+    return a.page_table[(int64_t)it.req * a.pt_stride + min((tok >> 4) + lane, (it.t1 - 1) >> 4)];
+  };
+  auto clamped = [&](int b) { return min(max(b, 0), a.n_blocks - 1); };
 
-  // the row group's queries in operand order, loaded by all four waves
-  uint4(*qs)[RB][KC][64] = reinterpret_cast<uint4(*)[RB][KC][64]>(smem);
-  for (int u = threadIdx.x; u < RB * KC * 64; u += 256) {
-    const int l = u & 63, kc = (u >> 6) % KC, rb = (u >> 6) / KC;
-    const int lr = min(it.rbg * ROWS + rb * 16 + (l & 15), rows - 1);   // padding rows reuse a real row
-    const int64_t at = ((int64_t)(it.row0 + lr / G) * a.nq + kvh * G + lr % G) * HD + kc * 32 + 8 * (l >> 4);
-    if constexpr (F32) {
-      const float *p = reinterpret_cast<const float *>(a.q) + at;
-      uint32_t w[3][4];
+  // the queries of an item, by all threads: asked for, then stored in operand order (when nobody
+  // reads what is there any more)
+  constexpr int QN = RB * KC;            // 16-byte operands of a thread for four row groups
+  struct Queries {
+    uint4 w[QN][F32 ? 2 : 1];
+  };
+  auto load_queries = [&](const Kv8Item &it, Queries &q) __attribute__((always_inline)) {
+    const int rows = it.nrow * G, count = kv8_groups(it.groups) * RB * KC * 64, tid = opaque(threadIdx.x);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = p[2 * e], y = p[2 * e + 1];
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          w[k][e] = pack2bf_rne(x, y);
-          x -= low(w[k][e]);
-          y -= high(w[k][e]);
+    for (int x = 0; x < QN; ++x) {
+      const int u = x * 256 + tid;
+      q.w[x][0] = q.w[x][F32 ? 1 : 0] = make_uint4(0, 0, 0, 0);
+      if (u < count) {
+        const int l = u & 63, kc = (u >> 6) % KC, r16 = (u >> 6) / KC;   // 16-row block of the item
+        const int lr = min(kv8_first(it.groups) * ROWS + r16 * 16 + (l & 15), rows - 1);   // padding rows: a real one
+        const int64_t at = ((int64_t)(it.row0 + lr / G) * a.nq + kvh * G + lr % G) * HD + kc * 32 + 8 * (l >> 4);
+        if constexpr (F32) {
+          q.w[x][0] = ld16(reinterpret_cast<const float *>(a.q) + at);
+          q.w[x][1] = ld16(reinterpret_cast<const float *>(a.q) + at + 4);
+        } else {
+          q.w[x][0] = ld16(reinterpret_cast<const uint16_t *>(a.q) + at);
         }
       }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) qs[k][rb][kc][l] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-    } else {
-      qs[0][rb][kc][l] = ld16(reinterpret_cast<const uint16_t *>(a.q) + at);
     }
+  };
+  auto store_queries = [&](const Kv8Item &it, const Queries &q) __attribute__((always_inline)) {
+    const int count = kv8_groups(it.groups) * RB * KC * 64, tid = opaque(threadIdx.x);
+#pragma unroll
+    for (int x = 0; x < QN; ++x) {
+      const int u = x * 256 + tid;
+      if (u < count) {
+        const int l = u & 63, kc = (u >> 6) % KC, r16 = (u >> 6) / KC;
+        if constexpr (F32) {
+          const uint32_t in[8] = {q.w[x][0].x, q.w[x][0].y, q.w[x][0].z, q.w[x][0].w,
+                                  q.w[x][1].x, q.w[x][1].y, q.w[x][1].z, q.w[x][1].w};
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(in[e]);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              h[e] = pack2bf_rne(f[2 * e], f[2 * e + 1]);
+              f[2 * e] -= low(h[e]);
+              f[2 * e + 1] -= high(h[e]);
+            }
+            qs[r16 / RB][p % NP][r16 % RB][kc][l] = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+        } else {
+          qs[r16 / RB][0][r16 % RB][kc][l] = q.w[x][0];
+        }
+      }
+    }
+  };
+
+  // A segment: up to 16 quads of the wave's share, whose block ids sit in the lanes (lane l its l-th
+  // page).  The next segment's, of this item or the next, are asked for while it runs.
+  Kv8Item it = item_at(k), nx = item_at(k + 1);
+  Share sh = share_of(it);
+  int tok = sh.tok, n = min(sh.n, 16), left = sh.n - n;   // first token and quads of the segment; quads after it
+  int blk = ids_at(it, tok), nblk = 0;   // nblk: once they are here
+  auto check = [&](int b) __attribute__((always_inline)) {
+    if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
+  };
+  {
+    Queries q;
+    load_queries(it, q);
+    check(blk);
+    store_queries(it, q);
   }
-  if (n > 0) {
-    const float2 s2 = a.scale[(int64_t)blk * a.nkv + kvh];
-    ks = s2.x * a.c_log2;
-    vs = s2.y;
-    vs_inv = 1.0f / vs;
-  }
-  __syncthreads();
+  lds_barrier();
 
   float m_run[RB], l_run[RB];
   floatx4 o[RB][MB];
   int jrow[RB];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    jrow[rb] = min(it.rbg * ROWS + rb * 16 + lc, rows - 1) / G;
-    m_run[rb] = -INFINITY;
-    l_run[rb] = 0.f;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) o[rb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  auto lane_of = [](float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); };
-  const int k_off = lg * 128 + (lc & 7) * 16, v_off = (lg & 1) * 256 + lc * 16;
-  for (int i = 0; i < n; ++i) {
-    const int tp = tok0 + 32 * i;
-    const int64_t p0 = ((int64_t)__builtin_amdgcn_readlane(blk, 2 * i) * a.nkv + kvh) * (kPage * HD);
-    const int64_t p1 = ((int64_t)__builtin_amdgcn_readlane(blk, 2 * i + 1) * a.nkv + kvh) * (kPage * HD);
-    const uint8_t *kp = a.k + (lc >= 8 ? p1 : p0) + k_off, *vp = a.v + (lg >= 2 ? p1 : p0) + v_off;
-    uint4 kr[KC], vr[KC];
-#pragma unroll
-    for (int c = 0; c < KC; ++c) kr[c] = ld16_stream(kp + c * 512);
-#pragma unroll
-    for (int c = 0; c < KC; ++c) vr[c] = ld16_stream(vp + c * 512);
-    const float ks_l = lg >= 2 ? lane_of(ks, 2 * i + 1) : lane_of(ks, 2 * i);
-    const float vs_l = lg >= 2 ? lane_of(vs, 2 * i + 1) : lane_of(vs, 2 * i);
-    const float vi_l = lg >= 2 ? lane_of(vs_inv, 2 * i + 1) : lane_of(vs_inv, 2 * i);
-    floatx4 s[RB][2];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) s[rb][0] = s[rb][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const bf16x8_t k0 = to_bf16(kr[c].x, kr[c].y), k1 = to_bf16(kr[c].z, kr[c].w);
-#pragma unroll
-      for (int k = NP - 1; k >= 0; --k)   // small parts first
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          const bf16x8_t qf = as_bf16x8(qs[k][rb][c][lane]);
-          s[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf, s[rb][0], 0, 0, 0);
-          s[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf, s[rb][1], 0, 0, 0);
-        }
-    }
-    // slots past the range may hold anything: zero probability is not enough against a NaN
-    if (tp + 32 > it.t1) {
-      const int left = min(max(it.t1 - (tp + 8 * lg), 0), 8);
-      const uint32_t mlo = left >= 4 ? ~0u : (1u << (8 * left)) - 1u, mhi = left <= 4 ? 0u : left == 8 ? ~0u : (1u << (8 * (left - 4))) - 1u;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        vr[c].x &= mlo;
-        vr[c].y &= mhi;
-        vr[c].z &= mlo;
-        vr[c].w &= mhi;
-      }
-    }
-    const bool unmasked = tp + 32 <= min(it.t1, it.ctx + 1);
-    uint4 pb[NP][RB];
+  auto begin_item = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      // s[rb][h][e]: token tp + 8 lg + 4 h + e, query row rb * 16 + lc of the group
+      jrow[rb] = min((kv8_first(it.groups) + sh.rg) * ROWS + rb * 16 + lc, it.nrow * G - 1) / G;
+      m_run[rb] = -INFINITY;
+      l_run[rb] = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s[rb][h] *= ks_l;
-      if (!unmasked) {
-        const int lim = min(it.t1, it.ctx + jrow[rb] + 1);
+      for (int mb = 0; mb < MB; ++mb) o[rb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  begin_item();
+
+  const int k_off = lg * 128 + (lc & 7) * 16, v_off = (lg & 1) * 256 + lc * 16;
+  bool more = true;                      // a segment follows this one
+  // The codes of quad i of this segment, or past its end the first of the next one.  With none to
+  // follow every lane asks for the start of a page (one cache line): the loads are issued on every
+  // path, so that the waits stay exact.
+  struct Pages {
+    int64_t p[4];
+  };
+  auto pages_of = [&](int i) __attribute__((always_inline)) {
+    int b[4];
+    if (i < n) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) b[x] = __builtin_amdgcn_readlane(blk, 4 * i + x);
+    } else {
+      asm volatile("" ::: "memory");     // a branch: a select would wait for the ids on either side
+#pragma unroll
+      for (int x = 0; x < 4; ++x) b[x] = __builtin_amdgcn_readlane(nblk, x);
+    }
+    Pages p;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p.p[x] = (int64_t)clamped(b[x]) * a.nkv + kvh;
+    return p;
+  };
+  auto load = [&](int i, const uint8_t *pool, int off, int64_t page, uint4 (&r)[KC]) __attribute__((always_inline)) {
+    const uint8_t *p = pool + page * (kPage * HD) + (i < n || more ? off : 0);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) r[c] = ld16(p + c * 512);
+  };
+  uint4 kr[2][KC], vr[2][KC];            // pair h of the quad
+  float2 sc[2];                          // scales of the lane's page of pair h: lane groups 0 and 1 its first
+  auto load_k = [&](int i) __attribute__((always_inline)) {
+    const Pages p = pages_of(i);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      load(i, a.k, k_off, lc >= 8 ? p.p[2 * h + 1] : p.p[2 * h], kr[h]);
+      sc[h] = a.scale[lg >= 2 ? p.p[2 * h + 1] : p.p[2 * h]];
+    }
+  };
+  auto load_v = [&](int i) __attribute__((always_inline)) {
+    const Pages p = pages_of(i);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load(i, a.v, v_off, lg >= 2 ? p.p[2 * h + 1] : p.p[2 * h], vr[h]);
+  };
+
+  // One quad in three phases; each operand's registers are filled again as soon as its phase is over:
+  // K is in flight during the softmax and the second product, V during the first product and the
+  // softmax.
+  auto step = [&](int i) __attribute__((always_inline)) {
+    const int tp = tok + 64 * i;
+    float ks[2], lv[2], vi[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ks[h] = sc[h].x * a.c_log2;
+      lv[h] = __builtin_amdgcn_logf(sc[h].y);
+      vi[h] = __builtin_amdgcn_exp2f(-lv[h]);
+    }
+    floatx4 s[RB][2][2];                 // [row block][pair][half of its pages' slots]
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s[rb][h][0] = s[rb][h][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) { // small parts first
+        bf16x8_t qf[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) qf[rb] = as_bf16x8(qs[sh.rg][p][rb][c][lane]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8_t k0 = to_bf16(kr[h][c].x, kr[h][c].y), k1 = to_bf16(kr[h][c].z, kr[h][c].w);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            s[rb][h][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[rb], s[rb][h][0], 0, 0, 0);
+            s[rb][h][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[rb], s[rb][h][1], 0, 0, 0);
+          }
+        }
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(i + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // s[rb][h][x][e]: token tp + 32 h + 8 lg + 4 x + e, query row rb * 16 + lc of the group, without K's scale
+    if (tp + 64 > min(sh.end, it.ctx + 1)) {
+      const int t = opaque(tp + 8 * lg);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int lim = min(sh.end, it.ctx + jrow[rb] + 1) - t;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (tp + 8 * lg + 4 * h + e >= lim) s[rb][h][e] = -INFINITY;
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (32 * h + 4 * x + e >= lim) s[rb][h][x][e] = -INFINITY;
       }
-      float mx = fmaxf(fmaxf(fmaxf(s[rb][0][0], s[rb][0][1]), fmaxf(s[rb][0][2], s[rb][0][3])),
-                       fmaxf(fmaxf(s[rb][1][0], s[rb][1][1]), fmaxf(s[rb][1][2], s[rb][1][3])));
-      mx = xor32_max(xor16_max(mx));
-      // the running maximum (base 2) rises only by more than 8: p stays below 2^8, and the
-      // accumulators are rescaled on few pairs; numerator and denominator share the reference
-      const bool grow = mx > m_run[rb] + 8.0f;
+    }
+    uint4 pb[NP][RB][2];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float mx[2];                       // scores in base 2
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        mx[h] = ks[h] * fmaxf(fmaxf(fmaxf(s[rb][h][0][0], s[rb][h][0][1]), fmaxf(s[rb][h][0][2], s[rb][h][0][3])),
+                              fmaxf(fmaxf(s[rb][h][1][0], s[rb][h][1][1]), fmaxf(s[rb][h][1][2], s[rb][h][1][3])));
+      const float top = xor32_max(xor16_max(fmaxf(mx[0], mx[1])));
+      // the running maximum rises only by more than 8: p stays below 2^8, and the accumulators
+      // are rescaled on few quads; numerator and denominator share the reference
+      const bool grow = top > m_run[rb] + 8.0f;
       if (__builtin_amdgcn_ballot_w64(grow)) {
-        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run[rb] - mx) : 1.0f;
-        m_run[rb] = grow ? mx : m_run[rb];
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run[rb] - top) : 1.0f;
+        m_run[rb] = grow ? top : m_run[rb];
         l_run[rb] *= alpha;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) o[rb][mb] *= alpha;
       }
-      const float mc = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-      float rs = 0.f;
-      uint32_t pw[NP][4];
+      const float m = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        // p x V's scale = 2^(s ks - m + log2 vs)
+        const float off = lv[h] - m;
+        float rs = 0.f;
+        uint32_t pw[NP][4];
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          float x = __builtin_amdgcn_exp2f(s[rb][h][e] - mc) * vs_l, y = __builtin_amdgcn_exp2f(s[rb][h][e + 1] - mc) * vs_l;
-          if constexpr (F32) rs += x + y;
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int k = 0; k < NP; ++k) {
-            const uint32_t w = pack2bf_rne(x, y);
-            pw[k][h * 2 + e / 2] = w;
-            x -= low(w);
-            y -= high(w);
+          for (int e = 0; e < 4; e += 2) {
+            float f = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e], ks[h], off));
+            float g = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e + 1], ks[h], off));
+            if constexpr (F32) rs += f + g;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+              const uint32_t w = pack2bf_rne(f, g);
+              pw[p][x * 2 + e / 2] = w;
+              f -= low(w);
+              g -= high(w);
+            }
+            // bf16: the sum adds the rounded values, as the second product does
+            if constexpr (!F32) {
+              const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+              rs = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[0][x * 2 + e / 2]), one, rs, false);
+            }
           }
-          // bf16: the sum adds the rounded values, as the second product does
-          if constexpr (!F32) rs += low(pw[0][h * 2 + e / 2]) + high(pw[0][h * 2 + e / 2]);
-        }
-      l_run[rb] += xor32_sum(xor16_sum(rs * vi_l));
+        l_run[rb] = __builtin_fmaf(rs, vi[h], l_run[rb]);   // this lane's tokens; the lanes are added up at the end
 #pragma unroll
-      for (int k = 0; k < NP; ++k) pb[k][rb] = make_uint4(pw[k][0], pw[k][1], pw[k][2], pw[k][3]);
+        for (int p = 0; p < NP; ++p) pb[p][rb][h] = make_uint4(pw[p][0], pw[p][1], pw[p][2], pw[p][3]);
+      }
+    }
+    // slots past the range may hold anything: zero probability is not enough against a NaN
+    if (tp + 64 > sh.end) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int in = min(max(sh.end - opaque(tp + 32 * h + 8 * lg), 0), 8);
+        const uint32_t mlo = in >= 4 ? ~0u : (1u << (8 * in)) - 1u, mhi = in <= 4 ? 0u : in == 8 ? ~0u : (1u << (8 * (in - 4))) - 1u;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          vr[h][c].x &= mlo;
+          vr[h][c].y &= mhi;
+          vr[h][c].z &= mlo;
+          vr[h][c].w &= mhi;
+        }
+      }
     }
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const bf16x8_t v0 = to_bf16(vr[c].x, vr[c].y), v1 = to_bf16(vr[c].z, vr[c].w);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int k = NP - 1; k >= 0; --k)
+      for (int c = 0; c < KC; ++c) {
+        const bf16x8_t v0 = to_bf16(vr[h][c].x, vr[h][c].y), v1 = to_bf16(vr[h][c].z, vr[h][c].w);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          o[rb][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(pb[k][rb]), o[rb][2 * c], 0, 0, 0);
-          o[rb][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(pb[k][rb]), o[rb][2 * c + 1], 0, 0, 0);
-        }
-    }
-  }
+        for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            o[rb][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, as_bf16x8(pb[p][rb][h]), o[rb][2 * c], 0, 0, 0);
+            o[rb][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, as_bf16x8(pb[p][rb][h]), o[rb][2 * c + 1], 0, 0, 0);
+          }
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(i + 1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
 
-  // join the waves: tile t = rb * MB + mb is added up by wave t % 4, in wave order
-  if (lg == 0)
+  // The item's end, through LDS: every wave's accumulators, then 8 dims of a row per thread, the waves
+  // that share the row's group added up in order.
+  auto put_result = [&]() __attribute__((always_inline)) {
+    const int lane = opaque(threadIdx.x) & 63, lc = lane & 15, lg = lane >> 4;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      sh_m[wave][rb * 16 + lc] = m_run[rb];
-      sh_l[wave][rb * 16 + lc] = l_run[rb];
+      const float l = xor32_sum(xor16_sum(l_run[rb]));
+      if (lg == 0) sh_ml[wave][rb * 16 + lc] = make_float2(m_run[rb], l);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) *reinterpret_cast<floatx4 *>(&jo[wave][rb * 16 + lc][mb * 16 + 4 * lg]) = o[rb][mb];
     }
-  __syncthreads();   // the queries are no longer read either
-  floatx4(*jo)[RB * MB][64] = reinterpret_cast<floatx4(*)[RB * MB][64]>(smem);
-  float m_all[RB], l_all[RB];
+  };
+  auto write_result = [&]() __attribute__((always_inline)) {
+    const int groups = kv8_groups(it.groups), lr0 = kv8_first(it.groups) * ROWS;
+    const int end = min(groups * ROWS, it.nrow * G - lr0) * (HD / 8);
+    for (int u = opaque(threadIdx.x); u < end; u += 256) {
+      const int r = u / (HD / 8), c0 = u % (HD / 8) * 8, g = r / ROWS, rr = r % ROWS;
+      float2 ml[4];
+      float m = -INFINITY;
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = rb * 16 + lc;
-    m_all[rb] = fmaxf(fmaxf(sh_m[0][r], sh_m[1][r]), fmaxf(sh_m[2][r], sh_m[3][r]));
-    auto weight = [&](float m) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_all[rb]); };
-    l_all[rb] = 0.f;
+      for (int p = 0; p < 4; ++p) {
+        if (p < sh.parts) {
+          ml[p] = sh_ml[g + p * groups][rr];
+          m = fmaxf(m, ml[p].x);
+        }
+      }
+      float l = 0.f;
+      floatx4 x{0.f, 0.f, 0.f, 0.f}, y{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) l_all[rb] += sh_l[w][r] * weight(sh_m[w][r]);
-    const float mine = weight(m_run[rb]);
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) jo[wave][rb * MB + mb][lane] = o[rb][mb] * mine;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int lr = it.rbg * ROWS + rb * 16 + lc;
-    if (lr >= rows) continue;
-    const float inv = 1.0f / l_all[rb];
-    const int64_t row = it.row0 + jrow[rb];
-    const int head = kvh * G + lr - jrow[rb] * G;
-    const int64_t slot = ((int64_t)it.part * a.nkv + kvh) * ROWS + rb * 16 + lc;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      if ((rb * MB + mb) % 4 != wave) continue;
-      const int t = rb * MB + mb;
-      const floatx4 x = jo[0][t][lane] + jo[1][t][lane] + (jo[2][t][lane] + jo[3][t][lane]);
-      if (it.part >= 0) {
-        __builtin_nontemporal_store(x, reinterpret_cast<floatx4 *>(a.part_o + slot * HD + mb * 16 + 4 * lg));
+      for (int p = 0; p < 4; ++p) {
+        if (p < sh.parts) {
+          // a wave that saw nothing has no maximum; a NaN stays one
+          const float w = ml[p].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[p].x - m);
+          const float *from = &jo[g + p * groups][rr][c0];
+          l += ml[p].y * w;
+          x += *reinterpret_cast<const floatx4 *>(from) * w;
+          y += *reinterpret_cast<const floatx4 *>(from + 4) * w;
+        }
+      }
+      if (it.part >= 0) {                // a part of the context: not divided yet
+        const int64_t slot = ((int64_t)(it.part + g) * a.nkv + kvh) * ROWS + rr;
+        float *to = a.part_o + slot * HD + c0;
+        __builtin_nontemporal_store(x, reinterpret_cast<floatx4 *>(to));
+        __builtin_nontemporal_store(y, reinterpret_cast<floatx4 *>(to + 4));
+        if (c0 == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(m, l);
         continue;
       }
-      const int64_t col = (int64_t)head * HD + mb * 16 + 4 * lg;
+      const int64_t row = it.row0 + (lr0 + r) / G, col = (int64_t)(kvh * G + (lr0 + r) % G) * HD + c0;
+      const float inv = 1.0f / l;
+      x *= inv;
+      y *= inv;
       if constexpr (F32) {
-        *reinterpret_cast<floatx4 *>(reinterpret_cast<float *>(a.out) + row * a.out_K + col) = x * inv;
+        float *to = reinterpret_cast<float *>(a.out) + row * a.out_K + col;
+        *reinterpret_cast<floatx4 *>(to) = x;
+        *reinterpret_cast<floatx4 *>(to + 4) = y;
       } else {
-        const int64_t at = a.packed ? packed_off(row, col, a.out_K) : row * a.out_K + col;
-        *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(a.out) + at) =
-            make_uint2(pack2bf_rne(x[0] * inv, x[1] * inv), pack2bf_rne(x[2] * inv, x[3] * inv));
+        uint16_t *to = reinterpret_cast<uint16_t *>(a.out) + (a.packed ? packed_off(row, col, a.out_K) : row * a.out_K + col);
+        *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(x[0], x[1]), pack2bf_rne(x[2], x[3]), pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]));
       }
     }
-    if (it.part >= 0 && lg == 0 && wave == 0)
-      *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(m_all[rb], l_all[rb]);
+  };
+
+  load_k(0);
+  load_v(0);
+  __builtin_amdgcn_sched_barrier(0);
+  while (true) {
+    const bool same = left > 0;                          // the next segment is this item's
+    more = same || k + 1 < k_end;
+    const Share ns = share_of(nx);
+    const int ntok = same ? tok + 64 * n : ns.tok;
+    const int ids = same ? ids_at(it, ntok) : ids_at(nx, ntok);   // with nothing to follow: this item's once more
+    if (n == 1) {                                        // needed at once (a branch: see pages_of)
+      asm volatile("" ::: "memory");
+      nblk = ids;
+    }
+    for (int i = 0; i < n; ++i) {
+      step(i);
+      if (i == 0) {                                      // older than a quad's loads by now
+        nblk = opaque(ids);
+        check(nblk);
+      }
+    }
+    if (same) {
+      n = min(left, 16);
+      left -= n;
+    } else {
+      lds_barrier();                                     // the queries are no longer read
+      put_result();
+      lds_barrier();
+      write_result();
+      if (!more) break;
+      Queries q;
+      load_queries(nx, q);
+      lds_barrier();
+      store_queries(nx, q);
+      ++k;
+      it = nx;
+      nx = item_at(k + 1);
+      sh = ns;
+      n = min(sh.n, 16);
+      left = sh.n - n;
+      begin_item();
+      lds_barrier();
+    }
+    tok = ntok;
+    blk = nblk;
   }
 }
 
@@ -293,7 +494,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(const Kv8Group *__restric
   const int ch = hd / 8, lr0 = g.rbg * rows_per_group, nr = min(rows_per_group, g.nrow * G - lr0);
   for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < nr * ch; u += gridDim.y * blockDim.x) {
     const int rr = u / ch, c0 = u % ch * 8;
-    auto slot = [&](int c) { return ((int64_t)(g.part + c) * nkv + kvh) * rows_per_group + rr; };
+    auto slot = [&](int c) { return ((int64_t)(g.part + c * g.stride) * nkv + kvh) * rows_per_group + rr; };
     float m = -INFINITY;
     for (int c = 0; c < g.n_parts; ++c) m = fmaxf(m, part_ml[slot(c) * 2]);
     float den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -329,6 +530,7 @@ void kv8_attention(const Kv8Plan &p, const Kv8Cache &c, const void *q, void *out
   if (p.n_items == 0) return;
   Kv8Args a;
   a.items = reinterpret_cast<const Kv8Item *>(p.ws + p.w_items);
+  a.first = reinterpret_cast<const int32_t *>(p.ws + p.w_first);
   a.page_table = p.page_table;
   a.k = c.k;
   a.v = c.v;
@@ -346,32 +548,22 @@ void kv8_attention(const Kv8Plan &p, const Kv8Cache &c, const void *q, void *out
   a.c_log2 = 1.4426950408889634f / sqrtf((float)p.hd);
   a.packed = packed;
   const bool f32 = p.dtype == 0;
-  auto go = [&](auto kernel) { launch(kernel, (uint32_t)p.n_items * p.nkv, 256, 0, s, a); };
+  auto go = [&](auto kernel) { launch(kernel, (uint32_t)p.n_shares * p.nkv, 256, 0, s, a); };
   if (f32) {
     switch (p.hd) {
       case 32: go(kv8_attn_kernel<32, 1, true>); break;
-      case 64: p.rb == 1 ? go(kv8_attn_kernel<64, 1, true>) : go(kv8_attn_kernel<64, 2, true>); break;
+      case 64: go(kv8_attn_kernel<64, 1, true>); break;
       case 96: go(kv8_attn_kernel<96, 1, true>); break;
-      case 128: p.rb == 1 ? go(kv8_attn_kernel<128, 1, true>) : go(kv8_attn_kernel<128, 2, true>); break;
+      case 128: go(kv8_attn_kernel<128, 1, true>); break;
       case 160: go(kv8_attn_kernel<160, 1, true>); break;
       case 192: go(kv8_attn_kernel<192, 1, true>); break;
       case 224: go(kv8_attn_kernel<224, 1, true>); break;
       default: go(kv8_attn_kernel<256, 1, true>); break;
     }
   } else if (p.hd == 128) {
-    switch (p.rb) {
-      case 1: go(kv8_attn_kernel<128, 1, false>); break;
-      case 2: go(kv8_attn_kernel<128, 2, false>); break;
-      case 3: go(kv8_attn_kernel<128, 3, false>); break;
-      default: go(kv8_attn_kernel<128, 4, false>); break;
-    }
+    p.rb == 1 ? go(kv8_attn_kernel<128, 1, false>) : go(kv8_attn_kernel<128, 2, false>);
   } else {
-    switch (p.rb) {
-      case 1: go(kv8_attn_kernel<64, 1, false>); break;
-      case 2: go(kv8_attn_kernel<64, 2, false>); break;
-      case 3: go(kv8_attn_kernel<64, 3, false>); break;
-      default: go(kv8_attn_kernel<64, 4, false>); break;
-    }
+    p.rb == 1 ? go(kv8_attn_kernel<64, 1, false>) : go(kv8_attn_kernel<64, 2, false>);
   }
   if (p.n_groups == 0) return;
   const int rows = 16 * p.rb, units = rows * p.hd / 8;

@@ -29,26 +29,28 @@ constexpr float kE4m3Max = 448.f;
 struct Kv8Unit {    // a page that gets new rows: `held` valid slots before, then `rows` new ones
   int32_t req, page, row, held_rows;   // page: index in the request's table; held | rows << 8
 };
-struct Kv8Item {    // attention of one row group over tokens t0 .. t1 - 1 of its request
+struct Kv8Item {    // attention of up to four row groups over tokens t0 .. t1 - 1 of their request
   int32_t req, t0, t1, ctx;
-  int32_t row0, nrow, rbg, part;       // first row and rows of the request; row group; partial, -1: none
+  int32_t row0, nrow, groups, part;    // first row and rows of the request; kv8_pack; first partial, -1: none
 };
-struct Kv8Group {   // the partials of one row group, combined in order
-  int32_t row0, nrow, rbg, part, n_parts, pad[3];
+struct Kv8Group {   // the partials of one row group, `stride` apart, combined in order
+  int32_t row0, nrow, rbg, part, n_parts, stride, pad[2];
 };
+// an item's first row group and their number
+inline int32_t kv8_pack(int first, int n) { return first | (n - 1) << 24; }
+__host__ __device__ inline int kv8_first(int32_t g) { return g & 0xFFFFFF; }
+__host__ __device__ inline int kv8_groups(int32_t g) { return (g >> 24) + 1; }
 
-constexpr int kKv8ItemPairs = 128;     // most page pairs of an item: 64 pages, one per lane, for each of 4 waves
-constexpr int kKv8MaxItems = 1 << 22;  // items of one batch
+constexpr int kKv8MaxItems = 1 << 22;  // work items of one batch
 
 struct Kv8Plan {    // a wisp_kv8_batch
   uint64_t magic;
   const int32_t *page_table;
   char *ws;
   int32_t device, dtype, nq, nkv, hd, rows, B;
-  int32_t pt_stride, n_units, n_items, n_groups, rb, n_parts;
-  uint32_t pad;
+  int32_t pt_stride, n_units, n_items, n_shares, n_groups, rb, n_parts;
   // byte offsets in the workspace
-  uint64_t w_units, w_items, w_groups, w_pos, w_cs, w_po, w_pml, total;
+  uint64_t w_units, w_items, w_first, w_groups, w_pos, w_cs, w_po, w_pml, total;
 };
 
 struct Kv8Cache {   // one layer's pools

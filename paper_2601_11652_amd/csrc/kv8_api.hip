@@ -57,46 +57,89 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   p.rows = (int32_t)pos.size();
   p.n_units = (int32_t)units.size();
 
-  // Rows of a row group: as many 16-row blocks as the largest request fills, up to four (the
-  // group's K and V are read once), two or one where an fp32 model's three parts and wide
-  // heads leave no registers for more.
-  const int64_t blocks = ((int64_t)most * G + 15) / 16;
-  const int cap = p.dtype == WISP_BF16 ? 4 : p.hd == 64 || p.hd == 128 ? 2 : 1;
-  p.rb = (int)std::min<int64_t>(cap, blocks);
+  // Row groups of 32 rows, of 16 where no request has more (and for fp32, whose three parts fill
+  // the registers); up to four of a request make a bundle that runs together.
+  p.rb = p.dtype == WISP_BF16 && (int64_t)most * G > 16 ? 2 : 1;
   const int R = 16 * p.rb;
-  // Items: equal parts of a row group's page pairs, of at most L each
-  int64_t total = 0, n_items = 0;
-  auto groups_of = [&](int i) { return ((int64_t)nrow[i] * G + R - 1) / R; };
-  auto pairs_of = [&](int i, int64_t g) {
-    const int64_t last = std::min<int64_t>((int64_t)nrow[i] * G, (g + 1) * R) - 1;
-    return (d->ctx_len[i] + last / G + 1 + 31) / 32;
+  // The cost of a page pair in quarters of a wave's turn: one row group's pairs are spread over four
+  // waves; two groups have two waves each but share what is read, three or four one.  Starting
+  // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
+  // 0.25-32k: 348 us; with pairs of 4, 4 and 7 375, of 4, 8 and 16 377.  A prompt of 4096 rows: 217
+  // us, without the cost of an item 255.
+  constexpr int64_t kPair[5] = {0, 4, 6, 10, 10}, kStart = 64;
+  struct Bundle {
+    int32_t req, first, groups, tokens;   // tokens: up to its last row's causal limit
+    int64_t pairs, cost;
   };
-  for (int i = 0; i < p.B; ++i)
-    for (int64_t g = 0, n = groups_of(i); g < n; ++g) total += pairs_of(i, g) * p.nkv;
-  const int64_t slots = (int64_t)device_cus() * (p.rb <= 2 ? 2 : 1);
-  const int64_t L = std::min<int64_t>(64, std::max<int64_t>(8, (total + slots - 1) / slots));
-  for (int i = 0; i < p.B; ++i)
-    for (int64_t g = 0, n = groups_of(i); g < n; ++g) n_items += (pairs_of(i, g) + L - 1) / L;
-  if (n_items * p.nkv > kKv8MaxItems)
-    return fail(WISP_E_UNSUPPORTED, "the batch's contexts need %lld attention work items (at most %d)",
-                (long long)(n_items * p.nkv), kKv8MaxItems);
+  std::vector<Bundle> bundles;
+  int64_t total = 0;
+  for (int i = 0; i < p.B; ++i) {
+    const int64_t groups = ((int64_t)nrow[i] * G + R - 1) / R, nb = (groups + 3) / 4;
+    for (int64_t k = 0; k < nb; ++k) {
+      const int64_t f = k * groups / nb, e = (k + 1) * groups / nb;
+      const int32_t T = d->ctx_len[i] + (int32_t)((std::min<int64_t>((int64_t)nrow[i] * G, e * R) - 1) / G) + 1;
+      const int64_t pairs = (T + 31) / 32;
+      bundles.push_back(Bundle{i, (int32_t)f, (int32_t)(e - f), T, pairs, kStart + pairs * kPair[e - f]});
+      total += bundles.back().cost;
+    }
+  }
+  // Every kv head's work, the same for all, is cut into shares of equal cost, one for each
+  // workgroup (two per CU); a bundle that a share's border cuts becomes several items.  Short shares
+  // are whole turns of all four waves.  Where both workgroups of a CU are there, the older one's
+  // waves go first and take 1.3 times the younger one's work in the same time.
+  const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
+  constexpr int64_t kTurn = 32, kOld = 57;             // cost of a turn; percent of the older half
+  int64_t size = (total + most_shares - 1) / most_shares;
+  if (size < 8 * kTurn) size = std::max<int64_t>(1, (size + kTurn - 1) / kTurn) * kTurn;
+  const int64_t shares = std::max<int64_t>(1, (total + size - 1) / size), half = shares / 2;
+  auto border = [&](int64_t s) {                       // cost before share s
+    if (size < 8 * kTurn) return s * size;
+    return s <= half ? total * kOld / 100 * s / std::max<int64_t>(1, half)
+                     : total * kOld / 100 + total * (100 - kOld) / 100 * (s - half) / (shares - half);
+  };
+  if ((int64_t)(bundles.size() + shares) * p.nkv > kKv8MaxItems)
+    return fail(WISP_E_UNSUPPORTED, "the batch needs %lld attention work items (at most %d)",
+                (long long)((bundles.size() + shares) * p.nkv), kKv8MaxItems);
   std::vector<Kv8Item> items;
   std::vector<Kv8Group> groups;
-  items.reserve(n_items);
+  std::vector<int32_t> first{0};
+  items.reserve(bundles.size() + shares);
   p.n_parts = 0;
-  for (int i = 0; i < p.B; ++i)
-    for (int64_t g = 0, ng = groups_of(i); g < ng; ++g) {
-      const int64_t last = std::min<int64_t>((int64_t)nrow[i] * G, (g + 1) * R) - 1;
-      const int32_t T = d->ctx_len[i] + (int32_t)(last / G) + 1;
-      const int64_t pairs = (T + 31) / 32, n = (pairs + L - 1) / L;
-      if (n > 1) groups.push_back(Kv8Group{row0[i], nrow[i], (int32_t)g, p.n_parts, (int32_t)n, {0, 0, 0}});
-      for (int64_t k = 0; k < n; ++k) {
-        const int32_t a = (int32_t)(32 * (k * pairs / n)), e = std::min<int32_t>(T, (int32_t)(32 * ((k + 1) * pairs / n)));
-        items.push_back(Kv8Item{i, a, e, d->ctx_len[i], row0[i], nrow[i], (int32_t)g, n > 1 ? p.n_parts++ : -1});
+  int64_t at = 0;                                      // cost before this bundle
+  for (const Bundle &u : bundles) {
+    const int64_t snap = size / 16;                    // a cut this close to the bundle's edge is left out
+    const int64_t grain = u.groups == 1 ? 8 : u.groups == 2 ? 4 : 2, unit = kPair[u.groups] * grain;   // pairs of a turn
+    const size_t item0 = items.size();
+    auto item = [&](int64_t a, int64_t e) {
+      items.push_back(Kv8Item{u.req, (int32_t)(32 * a), (int32_t)std::min<int64_t>(u.tokens, 32 * e), d->ctx_len[u.req],
+                              row0[u.req], nrow[u.req], kv8_pack(u.first, u.groups), -1});
+    };
+    int64_t done = 0;
+    while ((int64_t)first.size() < shares) {
+      const int64_t b = border((int64_t)first.size());
+      if (b >= at + u.cost - snap) break;
+      const int64_t cut = (std::max<int64_t>(b - at - kStart, 0) + unit / 2) / unit * grain;   // pairs before it
+      if (cut > done && cut < u.pairs && b > at + snap) {
+        item(done, cut);
+        done = cut;
       }
+      first.push_back((int32_t)items.size());
     }
+    item(done, u.pairs);
+    at += u.cost;
+    const int32_t n = (int32_t)(items.size() - item0);
+    if (n > 1) {
+      for (int32_t k = 0; k < n; ++k) items[item0 + k].part = p.n_parts + k * u.groups;
+      for (int32_t g = 0; g < u.groups; ++g)
+        groups.push_back(Kv8Group{row0[u.req], nrow[u.req], u.first + g, p.n_parts + g, n, u.groups, {0, 0}});
+      p.n_parts += n * u.groups;
+    }
+  }
+  while ((int64_t)first.size() <= shares) first.push_back((int32_t)items.size());
   p.n_items = (int32_t)items.size();
   p.n_groups = (int32_t)groups.size();
+  p.n_shares = (int32_t)shares;
+  b.i_first = put(b.host, first);
 
   b.i_units = put(b.host, units);
   b.i_items = put(b.host, items);
@@ -114,6 +157,7 @@ void wisp::kv8_place(Kv8Build &b, char *ws, size_t desc, size_t scratch) {
   p.ws = ws;
   p.w_units = desc + b.i_units * 4;
   p.w_items = desc + b.i_items * 4;
+  p.w_first = desc + b.i_first * 4;
   p.w_groups = desc + b.i_groups * 4;
   p.w_pos = desc + b.i_pos * 4;
   p.w_po = scratch;

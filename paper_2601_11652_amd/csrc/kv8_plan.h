@@ -10,7 +10,7 @@ namespace wisp {
 struct Kv8Build {
   Kv8Plan p{};
   std::vector<int32_t> host;      // the arrays that the device needs; the i_ are places in it
-  size_t i_units = 0, i_items = 0, i_groups = 0, i_pos = 0;
+  size_t i_units = 0, i_items = 0, i_first = 0, i_groups = 0, i_pos = 0;
   size_t po_bytes = 0, pml_bytes = 0, cs_bytes = 0;
 };
 // the plan of a checked model and batch, not yet placed in a workspace

@@ -148,6 +148,31 @@ ATTENTION = [
 ]
 
 
+# shapes that reach the plan's corners: many kv heads leave few workgroups for each
+PLANS = [
+    # long shares: a wave's share is longer than the 64 pages whose ids it holds at a time
+    ([5000, 50], [2, 1], 512, 512, 64, True),
+    ([5000], [3], 512, 512, 32, False),
+    # the same with three row groups, whose waves run alone
+    ([9000, 17000], [17, 17], 128, 32, 64, True),
+    # many short requests: a workgroup runs one item after another
+    ([(37 * k) % 101 for k in range(300)], [1 + k % 5 for k in range(300)], 32, 32, 64, True),
+    ([(37 * k) % 101 for k in range(200)], [1 + k % 20 for k in range(200)], 64, 16, 128, True),
+    # row groups of 16 rows, all kinds of bundles next to each other
+    ([500, 3, 2000, 64, 1], [1, 4, 2, 3, 4], 16, 4, 128, True),
+    ([100, 3, 0, 64, 1, 700], [50, 4, 33, 17, 9, 100], 16, 4, 64, True),
+    ([100, 3, 0, 64, 1, 700], [50, 4, 33, 17, 9, 100], 16, 4, 64, False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(PLANS)))
+def test_attention_at_the_corners_of_the_plan(case):
+    ctx, nrow = PLANS[case][:2]
+    log(f"attention of {len(ctx)} requests, ctx {min(ctx)}-{max(ctx)}, rows {min(nrow)}-{max(nrow)}, {PLANS[case][2:]}")
+    c = Case(*PLANS[case], seed=500 + case, pow2=case % 2 == 1).fill()
+    _check_attention(c, c.queries())
+
+
 def _check_attention(c, q, plan=None, kv=None):
     kv = kv or c.pool()
     plan = plan or c.plan()
