@@ -12,6 +12,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "api.h"
 #include "host_guard.h"
 #include "kernels.h"
@@ -146,8 +148,10 @@ __device__ void write_ranked(const Best &b, int n, int k, const double m, double
   }
 }
 
-// One workgroup per row.
-template <typename T, int W>
+// One workgroup per row, N chunks at most (0: any number), so that a thread holds the group maxima
+// that it needs: those of its own groups, one a chunk.  Bound by latency (a handful of rows) or by
+// starting a workgroup for each: everything that depends on no other load is asked for first.
+template <typename T, int W, int N>
 __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
                                                                float temperature, const int32_t *__restrict__ tokens,
                                                                const Part *__restrict__ parts, const float *__restrict__ gmax,
@@ -155,45 +159,57 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
                                                                float *__restrict__ entropy, int32_t *__restrict__ top_ids,
                                                                float *__restrict__ top_lps, int *__restrict__ err) {
   const int64_t row = blockIdx.x;
-  const int t = threadIdx.x;
-  if (!row_counts(tokens, row)) return;
+  const int t = threadIdx.x, lane = t & 63;
+  const int tok = tokens ? tokens[row] : -1;
+  if (tokens && tok == -1) return;
   const T *x = logits + row * ld;
-  const double sc = (double)(kLog2e / temperature), Td = temperature;
-  __shared__ Part sh_part;
-  if (t < 64) {
-    Part p{0.0, 0.0, -INFINITY, 0.f};
-    for (int c = t; c < nch; c += 64) p = join(p, parts[row * nch + c], sc);
+  const float *gm = gmax + row * nch * kThreads;
+  float gv[N ? N : 1];
+  if (N && top > 0) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const Part q{__shfl_xor(p.s, o), __shfl_xor(p.c, o), __shfl_xor(p.m, o), 0.f};
-      p = t & o ? join(q, p, sc) : join(p, q, sc);   // the same order in both lanes
-    }
-    if (t == 0) sh_part = p;
+    for (int c = 0; c < N; ++c) gv[c] = c < nch ? gm[c * kThreads + t] : -INFINITY;
   }
-  __syncthreads();
-  const Part p = sh_part;
-  const bool none = p.s == 0.0;                // every logit is -inf
-  const double lse = log(p.s), m = p.m;
+  const bool tok_ok = tok >= 0 && tok < V;
+  const float xt = tok_ok ? logit(x, tok) : 0.f;
+  // the chunks joined, by every wave: a lane's chunks in order, then the lanes
+  const float sc = kLog2e / temperature;
+  float m = -INFINITY;
+  double s = 0.0, cs = 0.0;
+  for (int c = lane; c < nch; c += 64) {
+    const Part p = parts[row * nch + c];
+    const float hi = fmaxf(m, p.m);
+    const double d0 = m == hi ? 0.0 : (double)m - hi, d1 = p.m == hi ? 0.0 : (double)p.m - hi;
+    const float w0 = __builtin_amdgcn_exp2f((float)d0 * sc), w1 = __builtin_amdgcn_exp2f((float)d1 * sc);
+    // a side without entries adds nothing, a NaN stays
+    cs = (s == 0.0 ? 0.0 : w0 * (cs + d0 * s)) + (p.s == 0.0 ? 0.0 : w1 * (p.c + d1 * p.s));
+    s = (s == 0.0 ? 0.0 : w0 * s) + (p.s == 0.0 ? 0.0 : w1 * p.s);
+    m = hi;
+  }
+  const float mw = wave_max(m);
+  {
+    const double d = m == mw ? 0.0 : (double)m - mw;
+    const float w = __builtin_amdgcn_exp2f((float)d * sc);
+    cs = s == 0.0 ? 0.0 : w * (cs + d * s);
+    s = s == 0.0 ? 0.0 : w * s;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o);
+    cs += __shfl_xor(cs, o);
+  }
+  const double Td = temperature, lse = log(s), md = mw;
+  const bool none = s == 0.0;                  // every logit is -inf
   if (t == 0) {
     if (logprob) {
-      const int tok = tokens[row];
-      float lp = NAN;
-      if (tok < 0 || tok >= V) {
-        flag_error(err, kErrToken);
-      } else {
-        const float xt = logit(x, tok);
-        lp = none || xt == -INFINITY ? (p.s != p.s ? NAN : -INFINITY) : (float)(((double)xt - m) / Td - lse);
-      }
-      logprob[row] = lp;
+      if (!tok_ok) flag_error(err, kErrToken);
+      logprob[row] = !tok_ok || s != s ? NAN : none || xt == -INFINITY ? -INFINITY : (float)(((double)xt - md) / Td - lse);
     }
-    if (entropy) entropy[row] = none ? 0.f : (float)(lse - p.c / p.s / Td);
+    if (entropy) entropy[row] = none ? 0.f : (float)(lse - cs / s / Td);
   }
   if (top == 0) return;
 
   int32_t *ids = top_ids + row * top;
   float *lps = top_lps + row * top;
-  const float *gm = gmax + row * nch * kThreads;
-  const int groups = nch * kThreads;
   __shared__ float sh_max[kThreads];
   __shared__ Best best;
   __shared__ int32_t sh_group[kCand];
@@ -202,47 +218,78 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
   if (t == 0) {
     sh_n = 0;
     sh_groups = 0;
-    sh_tau = -INFINITY;
   }
-  for (int r = t; r < top; r += kThreads) {    // places that no entry fills
-    ids[r] = -1;
-    lps[r] = p.s != p.s ? NAN : -INFINITY;
+  if (t < top) {                               // places that no entry fills
+    ids[t] = -1;
+    lps[t] = s != s ? NAN : -INFINITY;
   }
-  // the top-th largest of the threads' maxima: at least `top` entries reach it
   float mine = -INFINITY;
-  for (int g = t; g < groups; g += kThreads) mine = fmaxf(mine, gm[g]);
+  if constexpr (N > 0) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) mine = fmaxf(mine, gv[c]);
+  } else {
+    for (int c = 0; c < nch; ++c) mine = fmaxf(mine, gm[c * kThreads + t]);
+  }
   sh_max[t] = mine;
   __syncthreads();
-  int rank = 0;
-  for (int o = 0; o < kThreads; ++o) rank += sh_max[o] > mine || (sh_max[o] == mine && o < t);
-  if (rank == top - 1) sh_tau = mine;
+  // the top-th largest of 64 maxima, each of four threads' groups: at least `top` entries reach it
+  static_assert(WISP_TOP_MAX <= 64, "a bound from 64 maxima");
+  if (t < 64) {
+    mine = fmaxf(fmaxf(sh_max[t], sh_max[t + 64]), fmaxf(sh_max[t + 128], sh_max[t + 192]));
+    int rank = 0;
+#pragma unroll 16
+    for (int o = 0; o < 64; ++o) {
+      const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), o));
+      rank += v > mine || (v == mine && o < t);
+    }
+    if (rank == top - 1) sh_tau = mine;
+  }
   __syncthreads();
   const float tau = sh_tau;
-  for (int g = t; g < groups; g += kThreads) {
-    const float v = gm[g];
+  auto list = [&](float v, int c) {
     if (v >= tau && v > -INFINITY) {
       const int at = atomicAdd(&sh_groups, 1);   // the order does not matter: candidates are ranked
-      if (at < kCand) sh_group[at] = g;
+      if (at < kCand) sh_group[at] = c * kThreads + t;
     }
+  };
+  if constexpr (N > 0) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) list(gv[c], c);
+  } else {
+    for (int c = 0; c < nch; ++c) list(gm[c * kThreads + t], c);
   }
   __syncthreads();
   const int ng = sh_groups;
   if (ng <= kCand) {
-    for (int u = t; u < ng * kGroup; u += kThreads) {
-      const int g = sh_group[u / kGroup], e = g / kThreads * kChunk + entry_at<W>(g % kThreads, u % kGroup);
-      if (e >= V) continue;
-      const float v = logit(x, e);
-      if (v >= tau && v > -INFINITY) {
-        const int at = atomicAdd(&sh_n, 1);
-        if (at < kCand) {
-          best.v[at] = v;
-          best.i[at] = e;
+    constexpr int P = kGroup / W;                // loads of a group
+    for (int u = t; u < ng * P; u += kThreads) {
+      const int g = sh_group[u / P], e0 = g / kThreads * kChunk + entry_at<W>(g % kThreads, u % P * W);
+      float v[W];
+      if (W > 1 && e0 + W <= V) {
+        const uint4 r = ld16(x + e0);
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i % 4]);
+          else v[i] = __uint_as_float(i & 1 ? w[i / 2 % 4] & 0xFFFF0000u : w[i / 2 % 4] << 16);
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = e0 + i < V ? logit(x, e0 + i) : -INFINITY;
       }
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+        if (v[i] >= tau && v[i] > -INFINITY) {
+          const int at = atomicAdd(&sh_n, 1);
+          if (at < kCand) {
+            best.v[at] = v[i];
+            best.i[at] = e0 + i;
+          }
+        }
     }
     __syncthreads();
     if (sh_n <= kCand) {
-      write_ranked(best, sh_n, top, m, Td, lse, ids, lps);
+      write_ranked(best, sh_n, top, md, Td, lse, ids, lps);
       return;
     }
   }
@@ -306,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
     for (int w = 0; w < kThreads / 64; ++w) equal_before += sh_count[w];
     __syncthreads();
   }
-  write_ranked(best, min(sh_n, kCand), top, m, Td, lse, ids, lps);
+  write_ranked(best, min(sh_n, kCand), top, md, Td, lse, ids, lps);
 }
 
 int chunks_of(int32_t vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
@@ -350,16 +397,23 @@ extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, in
       launch(row, (uint32_t)rows, kThreads, 0, s, x, (int)vocab, ld, nch, temperature, tokens, (const Part *)parts,
              (const float *)gmax, (int)n_top, logprob, entropy, top_tokens, top_logprobs, err);
     };
+    // the row kernel that holds the chunks' group maxima (V <= 131072: 16, twice that: 32)
+    auto rows_of = [&](auto *x, auto w) {
+      using T = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
+      constexpr int W = decltype(w)::value;
+      return nch <= 16 ? logprobs_row_kernel<T, W, 16> : nch <= 32 ? logprobs_row_kernel<T, W, 32> : logprobs_row_kernel<T, W, 0>;
+    };
+    using One = std::integral_constant<int, 1>;
     const int es = dtype == WISP_F32 ? 4 : 2;
     const bool vec = ((uintptr_t)logits & 15) == 0 && ld * es % 16 == 0;
     if (dtype == WISP_F32) {
       const float *x = static_cast<const float *>(logits);
-      vec ? go(x, logprobs_chunk_kernel<float, true>, logprobs_row_kernel<float, 4>)
-          : go(x, logprobs_chunk_kernel<float, false>, logprobs_row_kernel<float, 1>);
+      vec ? go(x, logprobs_chunk_kernel<float, true>, rows_of(x, std::integral_constant<int, 4>{}))
+          : go(x, logprobs_chunk_kernel<float, false>, rows_of(x, One{}));
     } else {
       const uint16_t *x = static_cast<const uint16_t *>(logits);
-      vec ? go(x, logprobs_chunk_kernel<uint16_t, true>, logprobs_row_kernel<uint16_t, 8>)
-          : go(x, logprobs_chunk_kernel<uint16_t, false>, logprobs_row_kernel<uint16_t, 1>);
+      vec ? go(x, logprobs_chunk_kernel<uint16_t, true>, rows_of(x, std::integral_constant<int, 8>{}))
+          : go(x, logprobs_chunk_kernel<uint16_t, false>, rows_of(x, One{}));
     }
     return hip_check("wisp_token_logprobs");
   });
