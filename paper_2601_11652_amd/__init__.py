@@ -193,8 +193,10 @@ def _load():
 
 
 class _Lazy:
-    def __getattr__(self, name):
-        return getattr(load_library(), name)
+    def __getattr__(self, name):   # once a name: the function stays as the object's own
+        f = getattr(load_library(), name)
+        setattr(self, name, f)
+        return f
 
 
 lib = _Lazy()
@@ -262,8 +264,20 @@ def _check_desc(desc: "BatchDesc"):
 def _stream(stream) -> int | None:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(torch)(torch.cuda.current_device())
     return getattr(stream, "cuda_stream", stream)
+
+
+_raw = None
+
+
+def _raw_stream(torch):
+    """device index -> handle of its current stream.  The handle alone where torch gives it (0.1 us
+    a call; by way of a Stream object 2.8, more than a small call's launch takes)."""
+    global _raw
+    if _raw is None:
+        _raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw
 
 
 # ------------------------------------------------------------------------------------------
@@ -347,6 +361,7 @@ class KV8Pool:
             if t.device != k.device:
                 raise ValueError(f"{what}: on {t.device}, k is on {k.device}")
         self.k, self.v, self.scale = k, v, scale
+        self.page, self.device = tuple(k.shape[2:]), k.device
         self.c = wisp_kv8(k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.shape[1], PAGE)
 
     @staticmethod
@@ -522,7 +537,8 @@ class KV8Batch:
     def __init__(self, c, model: wisp_model, desc: BatchDesc, ws):
         import torch
         self.c, self.ws, self.page_table = c, ws, desc.page_table
-        self.rows, self.n_q, self.n_kv, self.head_dim = desc.rows, model.n_q_heads, model.n_kv_heads, model.head_dim
+        self.rows, n_q, n_kv, hd = desc.rows, model.n_q_heads, model.n_kv_heads, model.head_dim
+        self.q_numel, self.qkv_shape, self.page = self.rows * n_q * hd, (self.rows, (n_q + 2 * n_kv) * hd), (n_kv, PAGE * hd)
         self.dtype = torch.bfloat16 if model.dtype == WISP_BF16 else torch.float32
         self.device = ws.device
 
@@ -530,54 +546,59 @@ class KV8Batch:
 def wisp_kv8_plan(model: wisp_model, desc: BatchDesc, workspace, stream=None) -> KV8Batch:
     """Plans desc for the 8-bit cache in `workspace` (wisp_kv8_workspace_size bytes), once for
     all layers of a step."""
-    import torch
     _check_desc(desc)
     wp, wn = _ws(workspace)
     if desc.B > 0 and desc.page_table.device != workspace.device:
         raise ValueError(f"desc.page_table: on {desc.page_table.device}, the workspace on {workspace.device}")
     c = wisp_kv8_batch()
-    with torch.cuda.device(workspace.device):
+    with _On(workspace.device):
         _ok(lib.wisp_kv8_plan(C.byref(model), C.byref(desc.c), wp, wn, C.byref(c), _stream(stream)))
     return KV8Batch(c, model, desc, workspace)
 
 
-def _kv8_check(batch: KV8Batch, kv: KV8Pool, tensors):
-    if kv.k.shape[2] != batch.n_kv or kv.k.shape[3] != PAGE * batch.head_dim:
-        raise ValueError(f"kv: pages of {tuple(kv.k.shape[2:])}, expected ({batch.n_kv}, {PAGE * batch.head_dim})")
-    for what, t in tensors + (("kv", kv.k),):
-        if t.device != batch.device:
-            raise ValueError(f"{what}: on {t.device}, the batch was planned on {batch.device}")
+def _kv8_check(batch: KV8Batch, kv: KV8Pool, a, b):
+    if kv.page != batch.page:
+        raise ValueError(f"kv: pages of {kv.page}, expected {batch.page}")
+    if not a.device == b.device == kv.device == batch.device:
+        raise ValueError(f"tensors on {a.device} and {b.device}, kv on {kv.device}, the batch was planned on {batch.device}")
 
 
-def _on(device, stream, call):
-    """call(stream) on `device`, the current one or another."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(device):
-        return call(_stream(stream))
+class _On:
+    """Makes a device current for a call on its tensors, if it is not."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
 
 
 def wisp_kv8_append(batch: KV8Batch, kv: KV8Pool, qkv, q, stream=None):
     """qkv [rows][(n_q + 2 n_kv) * head_dim] of the model's dtype, rows of any (16-byte) stride;
     writes q [rows][n_q][head_dim] and layer 0 of kv (kv.layer(l) for another)."""
-    n = (batch.n_q + 2 * batch.n_kv) * batch.head_dim
-    if qkv.dim() != 2 or tuple(qkv.shape) != (batch.rows, n) or (batch.rows and qkv.stride(1) != 1):
-        raise ValueError(f"qkv: expected [{batch.rows}][{n}] with unit column stride, got {tuple(qkv.shape)}")
+    if qkv.shape != batch.qkv_shape or (batch.rows and qkv.stride(1) != 1):
+        raise ValueError(f"qkv: expected {list(batch.qkv_shape)} with unit column stride, got {list(qkv.shape)}")
     pq = _dev(qkv, "qkv", dtype=batch.dtype, contiguous=False)
-    po = _dev(q, "q", batch.rows * batch.n_q * batch.head_dim, dtype=batch.dtype)
-    _kv8_check(batch, kv, (("qkv", qkv), ("q", q)))
-    ld = qkv.stride(0) if batch.rows > 1 else n
-    _on(batch.device, stream, lambda s: _ok(lib.wisp_kv8_append(C.byref(batch.c), C.byref(kv.c), pq, ld, po, s)))
+    po = _dev(q, "q", batch.q_numel, dtype=batch.dtype)
+    _kv8_check(batch, kv, qkv, q)
+    ld = qkv.stride(0) if batch.rows > 1 else batch.qkv_shape[1]
+    with _On(batch.device):
+        _ok(lib.wisp_kv8_append(C.byref(batch.c), C.byref(kv.c), pq, ld, po, _stream(stream)))
 
 
 def wisp_attention_kv8(batch: KV8Batch, kv: KV8Pool, q, out, stream=None):
     """wisp_attention over layer 0 of the 8-bit cache kv (kv.layer(l) for another): q and out
     [rows][n_q][head_dim] of the model's dtype."""
-    n = batch.rows * batch.n_q * batch.head_dim
-    pq, po = _dev(q, "q", n, dtype=batch.dtype), _dev(out, "out", n, dtype=batch.dtype)
-    _kv8_check(batch, kv, (("q", q), ("out", out)))
-    _on(batch.device, stream, lambda s: _ok(lib.wisp_attention_kv8(C.byref(batch.c), C.byref(kv.c), pq, po, s)))
+    pq, po = _dev(q, "q", batch.q_numel, dtype=batch.dtype), _dev(out, "out", batch.q_numel, dtype=batch.dtype)
+    _kv8_check(batch, kv, q, out)
+    with _On(batch.device):
+        _ok(lib.wisp_attention_kv8(C.byref(batch.c), C.byref(kv.c), pq, po, _stream(stream)))
 
 
 def wisp_verify_kv8_workspace_size(model: wisp_model, desc: BatchDesc) -> int:
@@ -660,20 +681,23 @@ def wisp_token_logprobs(logits, vocab: int, tokens, temperature: float, logprob,
             raise ValueError(f"top_tokens, top_logprobs: expected [{rows}][n_top], got {tuple(top_tokens.shape)}, "
                              f"{tuple(top_logprobs.shape)}")
         n_top = top_tokens.shape[1]
-    opt = lambda t, what, n, dt: None if t is None else _dev(t, what, n, dtype=dt)
+    f32, i32 = torch.float32, torch.int32
     px = _dev(logits, "logits", contiguous=False)
-    ptrs = (opt(tokens, "tokens", rows, _i32()), opt(logprob, "logprob", rows, _f32()), opt(entropy, "entropy", rows, _f32()),
-            opt(top_tokens, "top_tokens", rows * n_top, _i32()), opt(top_logprobs, "top_logprobs", rows * n_top, _f32()))
+    pt = None if tokens is None else _dev(tokens, "tokens", rows, dtype=i32)
+    pl = None if logprob is None else _dev(logprob, "logprob", rows, dtype=f32)
+    pe = None if entropy is None else _dev(entropy, "entropy", rows, dtype=f32)
+    pi = None if top_tokens is None else _dev(top_tokens, "top_tokens", dtype=i32)
+    pv = None if top_logprobs is None else _dev(top_logprobs, "top_logprobs", dtype=f32)
     if ws is None:
         ws = workspace(wisp_token_logprobs_workspace_size(rows, vocab, n_top), logits.device)
-    for what, t in (("tokens", tokens), ("logprob", logprob), ("entropy", entropy), ("top_tokens", top_tokens),
-                    ("top_logprobs", top_logprobs), ("ws", ws)):
+    for t in (tokens, logprob, entropy, top_tokens, top_logprobs, ws):
         if t is not None and t.device != logits.device:
-            raise ValueError(f"{what}: on {t.device}, logits on {logits.device}")
+            raise ValueError(f"a tensor on {t.device}, logits on {logits.device}")
     ld = logits.stride(0) if rows > 1 else max(logits.shape[1], vocab)
-    code = WISP_F32 if logits.dtype == torch.float32 else WISP_BF16
-    _on(logits.device, stream, lambda s: _ok(lib.wisp_token_logprobs(
-        px, code, rows, vocab, ld, temperature, ptrs[0], n_top, ptrs[1], ptrs[2], ptrs[3], ptrs[4], *_ws(ws), s)))
+    code = WISP_F32 if logits.dtype == f32 else WISP_BF16
+    with _On(logits.device):
+        _ok(lib.wisp_token_logprobs(px, code, rows, vocab, ld, temperature, pt, n_top, pl, pe, pi, pv, *_ws(ws),
+                                    _stream(stream)))
 
 
 class RejectMLP:

@@ -73,11 +73,15 @@ def test_plan_refusals():
     assert _plan(m, _desc([250], [8])) == W.WISP_E_CAPACITY
     L = W.load_library()
     assert L.wisp_kv8_plan(C.byref(m), C.byref(_desc([1], [1]).c), FAKE, 1 << 40, None, None) == W.WISP_E_INVALID
-    # contexts that would pass the work list's 2^22 items
-    ctx = 1 << 29
-    big = _desc([ctx] * 64, [0] * 64, stride=(ctx >> 4) + 1)
-    assert W.wisp_kv8_workspace_size(W.GpuModel.shape_only(shape(8, 8, 64, True)), big) == 0
+    # a batch that would pass the work list's 2^22 items: every request one on each of 32 kv heads
+    n = 1 << 17
+    big = _desc([5] * n, [0] * n)
+    assert W.wisp_kv8_workspace_size(W.GpuModel.shape_only(shape(32, 32, 64, True)), big) == 0
     assert "work items" in W.wisp_last_error()
+    # long contexts do not: 64 requests of 2^29 tokens
+    ctx = 1 << 29
+    far = _desc([ctx] * 64, [0] * 64, stride=(ctx >> 4) + 1)
+    assert W.wisp_kv8_workspace_size(W.GpuModel.shape_only(shape(8, 8, 64, True)), far) > 0
 
 
 def test_calls_need_a_planned_batch():
