@@ -47,6 +47,11 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
+// The larger of two scores, as their median with the largest float: fmaxf quiets its operands
+// first, an instruction for each.  A NaN is passed over; of two, what comes out does not matter, as
+// their row's result is NaN.
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, 3.402823466e38f); }
+
 struct Kv8Args {
   const Kv8Item *items;
   const int32_t *first;   // share s runs items first[s] .. first[s + 1] - 1
@@ -297,8 +302,8 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
       float mx[2];                       // scores in base 2
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        mx[h] = ks[h] * fmaxf(fmaxf(fmaxf(s[rb][h][0][0], s[rb][h][0][1]), fmaxf(s[rb][h][0][2], s[rb][h][0][3])),
-                              fmaxf(fmaxf(s[rb][h][1][0], s[rb][h][1][1]), fmaxf(s[rb][h][1][2], s[rb][h][1][3])));
+        mx[h] = ks[h] * max2(max2(max2(s[rb][h][0][0], s[rb][h][0][1]), max2(s[rb][h][0][2], s[rb][h][0][3])),
+                             max2(max2(s[rb][h][1][0], s[rb][h][1][1]), max2(s[rb][h][1][2], s[rb][h][1][3])));
       const float top = xor32_max(xor16_max(fmaxf(mx[0], mx[1])));
       // the running maximum rises only by more than 8: p stays below 2^8, and the accumulators
       // are rescaled on few quads; numerator and denominator share the reference
@@ -484,7 +489,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
   }
 }
 
-// Joins a row group's partials in order: one thread per (row, 8 dims)
+// Joins a row group's partials in order, in rounds of kRound whose loads are all issued before the
+// first is used: one thread per (row, 8 dims).  Bound by latency: a launch and two dependent loads.
+constexpr int kRound = 8;
 template <bool F32>
 __global__ __launch_bounds__(256) void kv8_join_kernel(const Kv8Group *__restrict__ groups, int rows_per_group, int hd,
                                                        const float *__restrict__ part_o, const float *__restrict__ part_ml,
@@ -494,18 +501,36 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(const Kv8Group *__restric
   const int ch = hd / 8, lr0 = g.rbg * rows_per_group, nr = min(rows_per_group, g.nrow * G - lr0);
   for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < nr * ch; u += gridDim.y * blockDim.x) {
     const int rr = u / ch, c0 = u % ch * 8;
-    auto slot = [&](int c) { return ((int64_t)(g.part + c * g.stride) * nkv + kvh) * rows_per_group + rr; };
-    float m = -INFINITY;
-    for (int c = 0; c < g.n_parts; ++c) m = fmaxf(m, part_ml[slot(c) * 2]);
-    float den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < g.n_parts; ++c) {
-      const float2 ml = *reinterpret_cast<const float2 *>(part_ml + slot(c) * 2);
-      const float4 x = *reinterpret_cast<const float4 *>(part_o + slot(c) * hd + c0);
-      const float4 y = *reinterpret_cast<const float4 *>(part_o + slot(c) * hd + c0 + 4);
-      const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-      den += ml.y * w;
-      acc[0] += x.x * w; acc[1] += x.y * w; acc[2] += x.z * w; acc[3] += x.w * w;
-      acc[4] += y.x * w; acc[5] += y.y * w; acc[6] += y.z * w; acc[7] += y.w * w;
+    float m = -INFINITY, den = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < g.n_parts; r += kRound) {
+      float2 ml[kRound];
+      float4 x[kRound], y[kRound];
+#pragma unroll
+      for (int c = 0; c < kRound; ++c) {
+        ml[c] = make_float2(-INFINITY, 0.f);
+        x[c] = y[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r + c < g.n_parts) {   // the same for the whole workgroup
+          const int64_t slot = ((int64_t)(g.part + (r + c) * g.stride) * nkv + kvh) * rows_per_group + rr;
+          ml[c] = *reinterpret_cast<const float2 *>(part_ml + slot * 2);
+          x[c] = *reinterpret_cast<const float4 *>(part_o + slot * hd + c0);
+          y[c] = *reinterpret_cast<const float4 *>(part_o + slot * hd + c0 + 4);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int c = 0; c < kRound; ++c) top = fmaxf(top, ml[c].x);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      den *= keep;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= keep;
+      m = top;
+#pragma unroll
+      for (int c = 0; c < kRound; ++c) {
+        const float w = ml[c].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[c].x - m);
+        den += ml[c].y * w;
+        acc[0] += x[c].x * w; acc[1] += x[c].y * w; acc[2] += x[c].z * w; acc[3] += x[c].w * w;
+        acc[4] += y[c].x * w; acc[5] += y[c].y * w; acc[6] += y[c].z * w; acc[7] += y[c].w * w;
+      }
     }
     const float inv = 1.0f / den;
 #pragma unroll
