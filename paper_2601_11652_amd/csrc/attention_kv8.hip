@@ -67,7 +67,7 @@ struct Kv8Args {
   bool packed;
 };
 
-template <int HD, int RB, bool F32>
+template <int HD, int RB, bool F32, bool STREAM = false>
 __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Args a) {
   constexpr int ROWS = 16 * RB;         // of a row group
   constexpr int KC = HD / 32;           // 32-wide chunks of the contraction; 16-byte loads of K and of V
@@ -223,10 +223,22 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
     for (int x = 0; x < 4; ++x) p.p[x] = (int64_t)clamped(b[x]) * a.nkv + kvh;
     return p;
   };
+  // STREAM, a batch larger than the last-level cache: non-temporal where no other wave reads the same
+  // codes.  Pages in any order stream at 6.8 TB/s then, 6.0 otherwise; waves that share codes find
+  // them in L2 only without it (of 1.77 GB 1.23 times as much was read).  128 requests of 0.25-32k: 350
+  // -> 330 us; 32 requests of 0.5-2k 25.6 without and 28.3 with it.
+  bool alone = STREAM && kv8_groups(it.groups) == 1, next_alone = false;
   auto load = [&](int i, const uint8_t *pool, int off, int64_t page, uint4 (&r)[KC]) __attribute__((always_inline)) {
     const uint8_t *p = pool + page * (kPage * HD) + (i < n || more ? off : 0);
+    if (STREAM && (i < n ? alone : next_alone)) {
+      asm volatile("" ::: "memory");     // keeps the two branches two
 #pragma unroll
-    for (int c = 0; c < KC; ++c) r[c] = ld16(p + c * 512);
+      for (int c = 0; c < KC; ++c) r[c] = ld16_stream(p + c * 512);
+      asm volatile("" ::: "memory");
+    } else {
+#pragma unroll
+      for (int c = 0; c < KC; ++c) r[c] = ld16(p + c * 512);
+    }
   };
   uint4 kr[2][KC], vr[2][KC];            // pair h of the quad
   float2 sc[2];                          // scales of the lane's page of pair h: lane groups 0 and 1 its first
@@ -449,6 +461,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
     const bool same = left > 0;                          // the next segment is this item's
     more = same || k + 1 < k_end;
     const Share ns = share_of(nx);
+    next_alone = same ? alone : STREAM && kv8_groups(nx.groups) == 1;
     const int ntok = same ? tok + 64 * n : ns.tok;
     const int ids = same ? ids_at(it, ntok) : ids_at(nx, ntok);   // with nothing to follow: this item's once more
     if (n == 1) {                                        // needed at once (a branch: see pages_of)
@@ -486,6 +499,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
     }
     tok = ntok;
     blk = nblk;
+    alone = next_alone;
   }
 }
 
@@ -585,10 +599,12 @@ void kv8_attention(const Kv8Plan &p, const Kv8Cache &c, const void *q, void *out
       case 224: go(kv8_attn_kernel<224, 1, true>); break;
       default: go(kv8_attn_kernel<256, 1, true>); break;
     }
-  } else if (p.hd == 128) {
-    p.rb == 1 ? go(kv8_attn_kernel<128, 1, false>) : go(kv8_attn_kernel<128, 2, false>);
+  } else if (p.stream) {
+    if (p.hd == 128) p.rb == 1 ? go(kv8_attn_kernel<128, 1, false, true>) : go(kv8_attn_kernel<128, 2, false, true>);
+    else p.rb == 1 ? go(kv8_attn_kernel<64, 1, false, true>) : go(kv8_attn_kernel<64, 2, false, true>);
   } else {
-    p.rb == 1 ? go(kv8_attn_kernel<64, 1, false>) : go(kv8_attn_kernel<64, 2, false>);
+    if (p.hd == 128) p.rb == 1 ? go(kv8_attn_kernel<128, 1, false>) : go(kv8_attn_kernel<128, 2, false>);
+    else p.rb == 1 ? go(kv8_attn_kernel<64, 1, false>) : go(kv8_attn_kernel<64, 2, false>);
   }
   if (p.n_groups == 0) return;
   const int rows = 16 * p.rb, units = rows * p.hd / 8;

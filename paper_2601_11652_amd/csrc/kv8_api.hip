@@ -66,13 +66,15 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
   // 0.25-32k: 348 us; with pairs of 4, 4 and 7 375, of 4, 8 and 16 377.  A prompt of 4096 rows: 217
   // us, without the cost of an item 255.
-  constexpr int64_t kPair[5] = {0, 4, 6, 10, 10}, kStart = 64;
+  constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
   struct Bundle {
     int32_t req, first, groups, tokens;   // tokens: up to its last row's causal limit
     int64_t pairs, cost;
   };
   std::vector<Bundle> bundles;
-  int64_t total = 0;
+  int64_t total = 0, bytes = 0;
+  for (int i = 0; i < p.B; ++i) bytes += 2 * ((int64_t)d->ctx_len[i] + nrow[i]) * p.nkv * p.hd;
+  p.stream = bytes > (256 << 20);                      // more than the last-level cache holds
   for (int i = 0; i < p.B; ++i) {
     const int64_t groups = ((int64_t)nrow[i] * G + R - 1) / R, nb = (groups + 3) / 4;
     for (int64_t k = 0; k < nb; ++k) {
@@ -88,7 +90,7 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   // are whole turns of all four waves.  Where both workgroups of a CU are there, the older one's
   // waves go first and take 1.3 times the younger one's work in the same time.
   const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
-  constexpr int64_t kTurn = 32, kOld = 57;             // cost of a turn; percent of the older half
+  constexpr int64_t kTurn = 32, kOld = 55;             // cost of a turn; percent of the older half
   int64_t size = (total + most_shares - 1) / most_shares;
   if (size < 8 * kTurn) size = std::max<int64_t>(1, (size + kTurn - 1) / kTurn) * kTurn;
   const int64_t shares = std::max<int64_t>(1, (total + size - 1) / size), half = shares / 2;

@@ -7,7 +7,7 @@ import torch
 
 import paper_2601_11652_amd as W
 from gpu_harness import log
-from kv8_harness import Case, attention_bound, dev, host_pool
+from kv8_harness import Case, attention_bound, dev, host_pool, shape
 from oracle import kv8
 
 pytestmark = pytest.mark.gpu
@@ -192,6 +192,58 @@ def test_attention_matches_oracle(case):
     log(f"attention {ATTENTION[case]}")
     c = Case(*ATTENTION[case], seed=300 + case, pow2=case % 2 == 0).fill()
     _check_attention(c, c.queries())
+
+
+@pytest.mark.parametrize("n_q,n_kv,hd,lo,hi", [(64, 16, 128, 200, 6000), (16, 16, 128, 1000, 5000), (64, 32, 64, 200, 6000), (32, 32, 64, 10, 6000)])
+def test_attention_of_more_codes_than_the_caches_hold(n_q, n_kv, hd, lo, hi):
+    """Over 256 MB of codes (they are read past the caches then), one to five row groups a request;
+    the reference in fp64 on the device."""
+    rng = np.random.default_rng(n_q + hd)
+    B = 4 + (300 << 20) // (2 * n_kv * hd) // ((lo + hi) // 2)
+    ctx, nrow = rng.integers(lo, hi, B).astype(np.int32), rng.integers(1, 18, B).astype(np.int32)
+    nrow[0] = 40
+    tokens = ctx + nrow
+    log(f"{B} requests, {int(tokens.sum()) * 2 * n_kv * hd >> 20} MB of codes")
+    assert int(tokens.sum()) * 2 * n_kv * hd > 256 << 20
+    need = (tokens + 15) // 16
+    nb = int(need.sum())
+    pt, perm, o = np.full((B, int(need.max())), -1, np.int32), rng.permutation(nb).astype(np.int32), 0
+    for b in range(B):
+        pt[b, :need[b]] = perm[o:o + need[b]]
+        o += need[b]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(hd)
+    pool = lambda: (90.0 * torch.randn(nb, n_kv, 16 * hd, device="cuda", generator=g)).clamp_(-448, 448).to(torch.float8_e4m3fn)
+    k, v = pool(), pool()
+    scale = torch.exp2(torch.randint(-8, -4, (nb, n_kv, 2), device="cuda", generator=g).float())
+    M = int(nrow.sum())
+    q = torch.randn(M, n_q, hd, device="cuda", generator=g).to(torch.bfloat16)
+    m = W.GpuModel.shape_only(shape(n_q, n_kv, hd, True))
+    gamma = np.minimum(nrow - 1, 16)
+    desc = W.BatchDesc(ctx, gamma, torch.from_numpy(pt).cuda(), 1.0, None, nrow - 1 - gamma)
+    plan = W.wisp_kv8_plan(m, desc, W.workspace(W.wisp_kv8_workspace_size(m, desc)))
+    out = torch.empty_like(q)
+    W.wisp_attention_kv8(plan, W.KV8Pool(k[None], v[None], scale[None]), q, out)
+    W.wisp_check(plan.ws)
+    order = [torch.from_numpy(f(hd)).cuda() for f in (kv8.k_order, kv8.v_order)]
+    off, G, worst = np.concatenate([[0], np.cumsum(nrow)]), n_q // n_kv, 0.0
+    for b in range(B):
+        T = int(tokens[b])
+        blk = torch.from_numpy(pt[b, :need[b]].astype(np.int64)).cuda()
+        kd, vd = [(p[blk].double() * scale[blk][..., w, None].double())[:, :, order[w]].transpose(0, 1).reshape(n_kv, -1, hd)[:, :T]
+                  for w, p in enumerate((k, v))]
+        qq = q[off[b]:off[b + 1]].double().view(-1, n_kv, G, hd).permute(1, 0, 2, 3).reshape(n_kv, -1, hd)
+        s = torch.bmm(qq, kd.transpose(1, 2).contiguous()).view(n_kv, -1, G, T) / hd ** 0.5
+        seen = torch.arange(T, device="cuda") <= int(ctx[b]) + torch.arange(int(nrow[b]), device="cuda")[:, None]
+        p = torch.softmax(s.masked_fill(~seen[None, :, None], -np.inf), -1).view(n_kv, -1, T)
+        ref, mag = torch.bmm(p, vd.contiguous()), torch.bmm(p, vd.abs().contiguous())
+        big = torch.bmm(qq.abs(), kd.abs().transpose(1, 2).contiguous()).amax(-1) / hd ** 0.5
+        got = out[off[b]:off[b + 1]].double().view(-1, n_kv, G, hd).permute(1, 0, 2, 3).reshape(n_kv, -1, hd)
+        tol = attention_bound(*[t.cpu().numpy() for t in (ref, mag, big)], hd, T, True)
+        ratio = np.abs((got - ref).cpu().numpy()) / tol
+        worst = max(worst, ratio.max())
+        assert worst <= 1.0, (b, worst)
+    log(f"  worst {worst:.3f} of its bound")
 
 
 def test_attention_of_peaked_scores():
