@@ -18,43 +18,49 @@ namespace wisp {
 
 namespace {
 
-// 8 or 2 consecutive columns of a row; S = 0: stored as T, else S fp32 partials (a bound above 4)
-template <typename T, int S, int N>
-__device__ __forceinline__ void load_cols(const QkvRows &src, int64_t row, int col, float (&v)[N]) {
-  if constexpr (S == 0 && std::is_same<T, uint16_t>::value) {
-    const uint16_t *p = reinterpret_cast<const uint16_t *>(src.p) + row * src.ld + col;
-    uint32_t w[N / 2];
-    if constexpr (N == 8) {
-      const uint4 x = ld16(p);
-      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-    } else {
-      w[0] = *reinterpret_cast<const uint32_t *>(p);
-    }
-#pragma unroll
-    for (int e = 0; e < N / 2; ++e) {
-      v[2 * e] = __uint_as_float(w[e] << 16);
-      v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-    }
-  } else {
-    constexpr int MAX = S == 0 ? 1 : S;
-    const float *p = reinterpret_cast<const float *>(src.p) + row * src.ld + col;
-#pragma unroll
-    for (int z = 0; z < MAX; ++z) {
-      const float *pz = p + (MAX <= 4 ? z : min(z, src.splits - 1)) * src.stride;
-      float w[N];
+// 8 or 2 consecutive columns of a row, read once; S = 0: stored as T, else S fp32 partials (a bound
+// above 4).  bf16 words are kept as they come: widening them is the use that waits for the load.
+template <typename T, int S>
+struct Cols {
+  static constexpr bool kWords = S == 0 && std::is_same<T, uint16_t>::value;
+  static constexpr int kPer = kWords ? 2 : 1;   // values per word
+  using Word = std::conditional_t<kWords, uint32_t, float>;
+
+  template <int N>
+  static __device__ __forceinline__ void load(const QkvRows &src, int64_t row, int col, Word *w) {
+    if constexpr (kWords) {
+      const uint16_t *p = reinterpret_cast<const uint16_t *>(src.p) + row * src.ld + col;
       if constexpr (N == 8) {
-        const float4 a = *reinterpret_cast<const float4 *>(pz), b = *reinterpret_cast<const float4 *>(pz + 4);
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        const uint4 x = ld16_stream(p);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
       } else {
-        const float2 a = *reinterpret_cast<const float2 *>(pz);
-        w[0] = a.x; w[1] = a.y;
+        w[0] = *reinterpret_cast<const uint32_t *>(p);
       }
+    } else {
+      constexpr int MAX = S == 0 ? 1 : S;
+      const float *p = reinterpret_cast<const float *>(src.p) + row * src.ld + col;
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = z == 0 ? w[e] : MAX <= 4 || z < src.splits ? v[e] + w[e] : v[e];
+      for (int z = 0; z < MAX; ++z) {
+        const float *pz = p + (MAX <= 4 ? z : min(z, src.splits - 1)) * src.stride;
+        float x[N];
+        if constexpr (N == 8) {
+          const float4 a = *reinterpret_cast<const float4 *>(pz), b = *reinterpret_cast<const float4 *>(pz + 4);
+          x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+          x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
+          const float2 a = *reinterpret_cast<const float2 *>(pz);
+          x[0] = a.x; x[1] = a.y;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = z == 0 ? x[e] : MAX <= 4 || z < src.splits ? w[e] + x[e] : w[e];
+      }
     }
   }
-}
+  static __device__ __forceinline__ float value(const Word *w, int e) {
+    if constexpr (kWords) return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    else return w[e];
+  }
+};
 
 __device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
   *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -64,19 +70,24 @@ __device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
   *reinterpret_cast<uint4 *>(p) = make_uint4(pack2bf_rne(v[0], v[1]), pack2bf_rne(v[2], v[3]), pack2bf_rne(v[4], v[5]), pack2bf_rne(v[6], v[7]));
 }
 
-// (x_i, x_{i + hd/2}) rotated by the angle of dim i; cs: (cos, sin) of 8 consecutive dims
-__device__ __forceinline__ void rotate8(float (&lo)[8], float (&hi)[8], const float2 *__restrict__ cs) {
+// (cos, sin) of 8 consecutive dims of a row
+struct Angles {
   float4 t[4];
+  __device__ __forceinline__ void load(const float2 *__restrict__ cs) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) t[e] = reinterpret_cast<const float4 *>(cs)[e];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float c = e & 1 ? t[e / 2].z : t[e / 2].x, s = e & 1 ? t[e / 2].w : t[e / 2].y;
-    const float a = lo[e], b = hi[e];
-    lo[e] = a * c - b * s;
-    hi[e] = b * c + a * s;
+    for (int e = 0; e < 4; ++e) t[e] = reinterpret_cast<const float4 *>(cs)[e];
   }
-}
+  // (x_i, x_{i + hd/2}) rotated by the angle of dim i
+  __device__ __forceinline__ void rotate8(float (&lo)[8], float (&hi)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float c = e & 1 ? t[e / 2].z : t[e / 2].x, s = e & 1 ? t[e / 2].w : t[e / 2].y;
+      const float a = lo[e], b = hi[e];
+      lo[e] = a * c - b * s;
+      hi[e] = b * c + a * s;
+    }
+  }
+};
 
 typedef float float2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void decode8(uint2 w, float scale, float (&v)[8]) {
@@ -112,116 +123,159 @@ __device__ __forceinline__ int scale_exp(float most) {
 }
 __device__ __forceinline__ float exp2i(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-// a value that the cache holds: at most 448 x 2^100 (infinities and NaN are not), so that the
+// a magnitude that the cache holds: at most 448 x 2^100 (infinity and NaN are not), so that the
 // probabilities x scale stay finite
-__device__ __forceinline__ bool holds(float v) { return fabsf(v) <= kE4m3Max * 1.2676506002282294e30f; }
+__device__ __forceinline__ bool holds(float v) { return v <= kE4m3Max * 1.2676506002282294e30f; }
+// largest magnitude of both; a NaN stays
+__device__ __forceinline__ float most_of(float m, float a, float b) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, fabsf(a)), fabsf(b));
+}
 
 constexpr uint32_t kNan4 = 0x7F7F7F7Fu;   // four e4m3 NaN
 
-constexpr int kQHeads = 4;   // q heads of a thread
+constexpr int kQHeads = 2;   // q heads of a thread
 
-// Workgroups 0 .. n_units * nkv - 1: one page of one kv head, 2 * hd threads.  The first hd hold
-// K, thread (slot, i) the dims 8i .. 8i + 7 and their rotation partners; the others V, thread
-// (half, p) the dims 2p, 2p + 1 of 8 slots: each thread's values make whole 8-byte pieces of the
-// page.  The other workgroups: Q, a thread 8 + 8 dims of kQHeads heads of one row.
+// Two kinds of workgroups, interleaved over the grid in one even pattern.  A page's chain of loads
+// (unit, page table, old codes) would leave the memory idle by itself: all pages first, 12922 rows of
+// 32 + 2 x 8 heads of 128 took 58 us, interleaved 52 us (283 MB, 5.4 TB/s: near a copy's rate, so the
+// memory bounds it; 32 requests of 2 to 9 rows 4.7 us, the chain's latency).
+// One page of one kv head, 2 * hd threads: the first hd hold K, thread (slot, i) the dims 8i .. 8i + 7
+// and their rotation partners; the others V, thread (half, p) the dims 2p, 2p + 1 of 8 slots: each
+// thread's values make whole 8-byte pieces of the page.  Or Q, a thread 8 + 8 dims of kQHeads heads of
+// one row (1 head: 50 us, 4: 53 us where 2 took 48).  Q is stored through the caches: past them this
+// kernel took 47 us, but the attention that reads Q next 11 us more.
 template <typename T, int S>
 __global__ __launch_bounds__(512) void kv8_append_kernel(const Kv8Unit *__restrict__ units, int n_units,
                                                          const int32_t *__restrict__ page_table, int pt_stride,
                                                          const float2 *__restrict__ cs, QkvRows src, T *__restrict__ q,
                                                          uint8_t *__restrict__ k_pool, uint8_t *__restrict__ v_pool,
                                                          float2 *__restrict__ scales, int n_blocks, int rows, int nq,
-                                                         int nkv, int hd, int *__restrict__ err) {
+                                                         int nkv, int hd, uint32_t q_share, int *__restrict__ err) {
+  using C = Cols<T, S>;
   const int tid = threadIdx.x, half = hd / 2;
-  if ((int)blockIdx.x >= n_units * nkv) {
+  // workgroup b is Q's next one where floor(b q_share / 2^32) steps up
+  const uint32_t q_at = __umulhi(blockIdx.x, q_share);
+  if (__umulhi(blockIdx.x + 1, q_share) > q_at) {
     const int per = half / 8, groups = (nq + kQHeads - 1) / kQHeads;   // threads of a head; of a row: per * groups
-    const uint32_t t = (blockIdx.x - n_units * nkv) * blockDim.x + tid, per_row = per * groups;
+    const uint32_t t = q_at * blockDim.x + tid, per_row = per * groups;
     const int64_t row = t / per_row;
     if (row >= rows) return;
     const int u = t % per_row, i = (u % per) * 8, h0 = u / per;
-    float lo[kQHeads][8], hi[kQHeads][8];
+    typename C::Word w[kQHeads][16 / C::kPer];
+    Angles turn;
+    turn.load(cs + row * half + i);
 #pragma unroll
     for (int k = 0; k < kQHeads; ++k) {
       const int h = min(h0 + k * groups, nq - 1);
-      load_cols<T, S>(src, row, h * hd + i, lo[k]);
-      load_cols<T, S>(src, row, h * hd + half + i, hi[k]);
+      C::template load<8>(src, row, h * hd + i, w[k]);
+      C::template load<8>(src, row, h * hd + half + i, w[k] + 8 / C::kPer);
     }
 #pragma unroll
     for (int k = 0; k < kQHeads; ++k) {
       const int h = h0 + k * groups;
       if (h >= nq) break;
-      rotate8(lo[k], hi[k], cs + row * half + i);
+      float lo[8], hi[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        lo[e] = C::value(w[k], e);
+        hi[e] = C::value(w[k], 8 + e);
+      }
+      turn.rotate8(lo, hi);
       T *o = q + (row * nq + h) * hd + i;
-      store8(o, lo[k]);
-      store8(o + half, hi[k]);
+      store8(o, lo);
+      store8(o + half, hi);
     }
     return;
   }
-  __shared__ uint32_t sh_bad, sh_most[2];
-  const int unit = blockIdx.x / nkv, kvh = blockIdx.x % nkv;
+  __shared__ uint32_t sh_bad[8], sh_most[2];   // 512 threads
+  const int page_block = blockIdx.x - q_at, unit = (uint32_t)page_block / nkv, kvh = (uint32_t)page_block % nkv;
   const Kv8Unit un = units[unit];
   const int blk = page_table[(int64_t)un.req * pt_stride + un.page];
+  const int held = un.held_rows & 255, filled = held + (un.held_rows >> 8);
+  if (tid < 2) sh_most[tid] = 0;
+  const bool is_k = tid < hd;
+  // K: slot, dims i .. i + 7 (a) and half + i .. (b); V: dims i (a) and i + 1 (b) of slots slot .. slot + 7
+  const uint32_t u = is_k ? tid : tid - hd, per = is_k ? half / 8 : half, at = u / per;
+  const int slot = is_k ? at : at * 8, i = (u - at * per) * (is_k ? 8 : 2);
+  const int col = (nq + kvh + (is_k ? 0 : nkv)) * hd + i;
+  // The new rows, asked for before the page's place in the pool is known.  Slots without a new row
+  // take the nearest one's: no branch stands between these loads, and none waits for another.
+  typename C::Word raw[16 / C::kPer];
+  Angles turn;
+  auto row_of = [&](int sl) { return (int64_t)un.row + min(max(sl - held, 0), filled - held - 1); };
+  if (is_k) {
+    turn.load(cs + row_of(slot) * half + i);
+    C::template load<8>(src, row_of(slot), col, raw);
+    C::template load<8>(src, row_of(slot), col + half, raw + 8 / C::kPer);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) C::template load<2>(src, row_of(slot + e), col, raw + 2 * e / C::kPer);
+  }
   if (blk < 0 || blk >= n_blocks) {
     if (tid == 0) flag_error(err, kErrBlock);
     return;
   }
-  const int held = un.held_rows & 255, filled = held + (un.held_rows >> 8);
   const int64_t page = (int64_t)blk * nkv + kvh;
-  const float2 old = scales[page];
-  if (tid == 0) sh_bad = 0;
-  if (tid < 2) sh_most[tid] = 0;
-  __syncthreads();
-  const bool is_k = tid < hd;
-  // K: slot, dims i .. i + 7 (a) and half + i .. (b); V: dims i (a) and i + 1 (b) of slots slot .. slot + 7
-  const int u = is_k ? tid : tid - hd;
-  const int slot = is_k ? u / (half / 8) : u / half * 8, i = is_k ? u % (half / 8) * 8 : u % half * 2;
   uint8_t *pg = (is_k ? k_pool : v_pool) + page * (kPage * hd);
   const int at_a = is_k ? k8_page_off(slot, i) : v8_page_off(slot, i);
   const int at_b = is_k ? k8_page_off(slot, half + i) : v8_page_off(slot, i + 1);
-  float a[8], b[8];
   uint2 ca{}, cb{};
-  const int col = (nq + kvh + (is_k ? 0 : nkv)) * hd + i;
+  float old = 1.f;
   // what is there: the old slots' values; for V also the codes past the last row, which stay
   if (is_k ? slot < held : slot < held || filled < slot + 8) {
     ca = *reinterpret_cast<const uint2 *>(pg + at_a);
     cb = *reinterpret_cast<const uint2 *>(pg + at_b);
+    const float2 sc = scales[page];
+    old = is_k ? sc.x : sc.y;
   }
-  decode8(ca, is_k ? old.x : old.y, a);
-  decode8(cb, is_k ? old.x : old.y, b);
+  float a[8], b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float k0 = C::value(raw, e), k1 = C::value(raw, 8 + e);
+    const float v0 = C::value(raw, 2 * e), v1 = C::value(raw, 2 * e + 1);
+    a[e] = is_k ? k0 : v0;
+    b[e] = is_k ? k1 : v1;
+  }
+  if (slot < held) {
+    float oa[8], ob[8];
+    decode8(ca, old, oa);
+    decode8(cb, old, ob);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if ((is_k ? slot : slot + e) < held) {
+        a[e] = oa[e];
+        b[e] = ob[e];
+      }
+  }
   uint32_t bad = 0;   // slots with a new value that the cache does not hold
   if (is_k) {
-    if (slot >= held && slot < filled) {
-      const int64_t row = un.row + slot - held;
-      load_cols<T, S>(src, row, col, a);
-      load_cols<T, S>(src, row, col + half, b);
-      bool ok = true;
+    if (slot >= held) {
+      float m = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ok = ok && holds(a[e]) && holds(b[e]);
-      rotate8(a, b, cs + row * half + i);
+      for (int e = 0; e < 8; ++e) m = most_of(m, a[e], b[e]);
+      turn.rotate8(a, b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ok = ok && holds(a[e]) && holds(b[e]);
-      bad = ok ? 0u : 1u << slot;
+      for (int e = 0; e < 8; ++e) m = most_of(m, a[e], b[e]);
+      bad = holds(m) || slot >= filled ? 0u : 1u << slot;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (slot + e >= held && slot + e < filled) {
-        float w[2];
-        load_cols<T, S>(src, un.row + slot + e - held, col, w);
-        a[e] = w[0];
-        b[e] = w[1];
-        if (!holds(w[0]) || !holds(w[1])) bad |= 1u << (slot + e);
-      }
+      bad |= holds(most_of(0.f, a[e], b[e])) || slot + e < held || slot + e >= filled ? 0u : 1u << (slot + e);
   }
-  if (bad) atomicOr(&sh_bad, bad);
-  __syncthreads();
-  bad = sh_bad;
+  uint32_t wave_bad = 0;
+  for (uint64_t m = __ballot(bad != 0); m != 0; m &= m - 1) wave_bad |= __builtin_amdgcn_readlane(bad, __builtin_ctzll(m));
+  if ((tid & 63) == 0) sh_bad[tid >> 6] = wave_bad;
+  __syncthreads();   // also sh_most, and everyone has read the old scales
+  bad = 0;
+  for (int w = 0; w < (int)blockDim.x >> 6; ++w) bad |= sh_bad[w];
   float most = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int sl = is_k ? slot : slot + e;
-    const bool counts = sl < filled && !(bad >> sl & 1);
-    // an old NaN (kept from an earlier row) does not count either: fmaxf passes it over
-    if (counts) most = fmaxf(most, fmaxf(fabsf(a[e]), fabsf(b[e])));
+    // an old NaN (kept from an earlier row) does not count: fmaxf passes it over
+    const float m = fmaxf(fabsf(a[e]), fabsf(b[e]));
+    most = fmaxf(most, sl < filled && !(bad >> sl & 1) ? m : 0.f);
   }
   most = half_wave_max(most);   // hd is a multiple of 32: a half wave holds K or V only
   if ((tid & 31) == 0) atomicMax(&sh_most[is_k ? 0 : 1], __float_as_uint(most));
@@ -259,10 +313,12 @@ void append(const Kv8Plan &p, const Kv8Cache &c, const QkvRows &src, T *q, int *
   const float2 *cs = reinterpret_cast<const float2 *>(p.ws + p.w_cs);
   const int threads = 2 * p.hd;
   const int64_t per_row = (int64_t)p.hd / 16 * ((p.nq + kQHeads - 1) / kQHeads);
-  const int64_t blocks = (int64_t)p.n_units * p.nkv + (p.rows * per_row + threads - 1) / threads;
+  const int64_t q_blocks = (p.rows * per_row + threads - 1) / threads, blocks = (int64_t)p.n_units * p.nkv + q_blocks;
+  // rounded up: with blocks < 2^31 (wisp_kv8_plan) the error stays below one step, and the last step is whole
+  const uint32_t q_share = (uint32_t)((((uint64_t)q_blocks << 32) + blocks - 1) / blocks);
   auto go = [&](auto kernel) {
     launch(kernel, (uint32_t)blocks, threads, 0, s, units, p.n_units, p.page_table, p.pt_stride, cs, src, q, c.k, c.v,
-           reinterpret_cast<float2 *>(c.scale), c.n_blocks, p.rows, p.nq, p.nkv, p.hd, err);
+           reinterpret_cast<float2 *>(c.scale), c.n_blocks, p.rows, p.nq, p.nkv, p.hd, q_share, err);
   };
   if (src.splits == 0) go(kv8_append_kernel<T, 0>);
   else if (src.splits == 1) go(kv8_append_kernel<T, 1>);
