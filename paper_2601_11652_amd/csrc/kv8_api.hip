@@ -64,8 +64,8 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   // The cost of a page pair in quarters of a wave's turn: one row group's pairs are spread over four
   // waves; two groups have two waves each but share what is read, three or four one.  Starting
   // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
-  // 0.25-32k: 348 us; with pairs of 4, 4 and 7 375, of 4, 8 and 16 377.  A prompt of 4096 rows: 217
-  // us, without the cost of an item 255.
+  // 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
+  // A prompt of 4096 rows: 216 us, 215, 226 and 253.
   constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
   struct Bundle {
     int32_t req, first, groups, tokens;   // tokens: up to its last row's causal limit
@@ -73,7 +73,17 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   };
   std::vector<Bundle> bundles;
   int64_t total = 0, bytes = 0;
-  for (int i = 0; i < p.B; ++i) bytes += 2 * ((int64_t)d->ctx_len[i] + nrow[i]) * p.nkv * p.hd;
+  int64_t n_bundles = 0;
+  for (int i = 0; i < p.B; ++i) {
+    bytes += 2 * ((int64_t)d->ctx_len[i] + nrow[i]) * p.nkv * p.hd;
+    n_bundles += (((int64_t)nrow[i] * G + R - 1) / R + 3) / 4;
+  }
+  // Items carry a row group's index in 24 bits, and the kernels count a request's rows x G and the
+  // threads of an append in 32: both hold for every batch of at most kKv8MaxItems bundles x kv heads.
+  auto too_many = [&](int64_t n) {
+    return fail(WISP_E_UNSUPPORTED, "the batch needs %lld attention work items (at most %d)", (long long)n, kKv8MaxItems);
+  };
+  if (n_bundles > kKv8MaxItems / p.nkv) return too_many(n_bundles * p.nkv);
   p.stream = bytes > (256 << 20);                      // more than the last-level cache holds
   for (int i = 0; i < p.B; ++i) {
     const int64_t groups = ((int64_t)nrow[i] * G + R - 1) / R, nb = (groups + 3) / 4;
@@ -88,7 +98,8 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   // Every kv head's work, the same for all, is cut into shares of equal cost, one for each
   // workgroup (two per CU); a bundle that a share's border cuts becomes several items.  Short shares
   // are whole turns of all four waves.  Where both workgroups of a CU are there, the older one's
-  // waves go first and take 1.3 times the younger one's work in the same time.
+  // waves go first: it takes 55 % of their work (128 requests of 0.25-32k: 330 us;
+  // 50 %: 334, 60 %: 349).
   const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
   constexpr int64_t kTurn = 32, kOld = 55;             // cost of a turn; percent of the older half
   int64_t size = (total + most_shares - 1) / most_shares;
@@ -99,9 +110,7 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
     return s <= half ? total * kOld / 100 * s / std::max<int64_t>(1, half)
                      : total * kOld / 100 + total * (100 - kOld) / 100 * (s - half) / (shares - half);
   };
-  if ((int64_t)(bundles.size() + shares) * p.nkv > kKv8MaxItems)
-    return fail(WISP_E_UNSUPPORTED, "the batch needs %lld attention work items (at most %d)",
-                (long long)((bundles.size() + shares) * p.nkv), kKv8MaxItems);
+  if ((n_bundles + shares) * p.nkv > kKv8MaxItems) return too_many((n_bundles + shares) * p.nkv);
   std::vector<Kv8Item> items;
   std::vector<Kv8Group> groups;
   std::vector<int32_t> first{0};
