@@ -2,6 +2,8 @@
 // (pages that get rows, attention items, rotation table) and the calls that run on it.
 #include <algorithm>
 #include <cstring>
+#include <numeric>
+#include <queue>
 
 #include "api.h"
 #include "host_guard.h"
@@ -25,6 +27,82 @@ size_t put(std::vector<int32_t> &host, const std::vector<V> &v) {
   const size_t at = take(host, v.size() * (sizeof(V) / 4));
   if (!v.empty()) std::memcpy(&host[at], v.data(), v.size() * sizeof(V));
   return at;
+}
+
+struct Bundle {
+  int32_t req, first, groups, tokens;   // row groups; tokens: up to its last row's causal limit
+  int64_t pairs, cost;
+};
+struct Piece {                          // page pairs from .. to - 1 of a bundle, in a share; a bundle's in order
+  int32_t bundle, share;
+  int64_t from, to;
+};
+
+// The cost of a page pair in quarters of a wave's turn: one row group's pairs are spread over four
+// waves; two groups have two waves each but share what is read, three or four one.  Starting
+// an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
+// 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
+// A prompt of 4096 rows: 216 us, 215, 226 and 253.
+constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
+constexpr int64_t kTurn = 32;           // cost of a turn
+// Where both workgroups of a CU are there, the older one's waves go first: percent of the work that
+// the older half of the shares takes (128 requests of 0.25-32k: 330 us; 50 %: 334, 60 %: 349).
+constexpr int64_t kOld = 55;
+int64_t grain_of(const Bundle &u) { return u.groups == 1 ? 8 : u.groups == 2 ? 4 : 2; }   // pairs of a turn
+
+// Shares of equal cost, the bundles one after another: one that a share's border cuts becomes several
+// pieces.  Short shares are whole turns of all four waves.
+std::vector<Piece> by_borders(const std::vector<Bundle> &bundles, int64_t shares, int64_t size, int64_t total) {
+  const int64_t half = shares / 2, snap = size / 16;   // a cut this close to the bundle's edge is left out
+  auto border = [&](int64_t s) {                       // cost before share s
+    if (size < 8 * kTurn) return s * size;
+    return s <= half ? total * kOld / 100 * s / std::max<int64_t>(1, half)
+                     : total * kOld / 100 + total * (100 - kOld) / 100 * (s - half) / (shares - half);
+  };
+  std::vector<Piece> pieces;
+  pieces.reserve(bundles.size() + shares);
+  int64_t at = 0, share = 0;                           // cost before this bundle
+  for (size_t k = 0; k < bundles.size(); ++k) {
+    const Bundle &u = bundles[k];
+    const int64_t grain = grain_of(u), unit = kPair[u.groups] * grain;
+    int64_t done = 0;
+    for (; share + 1 < shares; ++share) {
+      const int64_t b = border(share + 1);
+      if (b >= at + u.cost - snap) break;
+      const int64_t cut = (std::max<int64_t>(b - at - kStart, 0) + unit / 2) / unit * grain;   // pairs before it
+      if (cut > done && cut < u.pairs && b > at + snap) {
+        pieces.push_back(Piece{(int32_t)k, (int32_t)share, done, cut});
+        done = cut;
+      }
+    }
+    pieces.push_back(Piece{(int32_t)k, (int32_t)share, done, u.pairs});
+    at += u.cost;
+  }
+  return pieces;
+}
+
+// Whole bundles, the longest first, each to the share that ends first with it.  `end`: when the last
+// share ends, in the cost of a share at the mean speed.
+std::vector<Piece> by_length(const std::vector<Bundle> &bundles, int64_t shares, int64_t &end) {
+  std::vector<Piece> pieces;
+  for (size_t k = 0; k < bundles.size(); ++k) pieces.push_back(Piece{(int32_t)k, 0, 0, bundles[k].pairs});
+  std::vector<int32_t> order(bundles.size());
+  std::iota(order.begin(), order.end(), 0);
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return bundles[x].cost > bundles[y].cost; });
+  using End = std::pair<int64_t, int32_t>;             // when a share ends, the share
+  std::priority_queue<End, std::vector<End>, std::greater<End>> ends;
+  for (int32_t s = 0; s < shares; ++s) ends.push({0, s});
+  end = 0;
+  for (int32_t k : order) {
+    const int32_t s = ends.top().second;
+    const int64_t e = ends.top().first + bundles[k].cost * (s < shares / 2 ? 100 - kOld : kOld);
+    ends.pop();
+    ends.push({e, s});
+    pieces[k].share = s;
+    end = std::max(end, e);
+  }
+  end = end * 100 / (2 * kOld * (100 - kOld));
+  return pieces;
 }
 
 }  // namespace
@@ -61,16 +139,6 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   // the registers); up to four of a request make a bundle that runs together.
   p.rb = p.dtype == WISP_BF16 && (int64_t)most * G > 16 ? 2 : 1;
   const int R = 16 * p.rb;
-  // The cost of a page pair in quarters of a wave's turn: one row group's pairs are spread over four
-  // waves; two groups have two waves each but share what is read, three or four one.  Starting
-  // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
-  // 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
-  // A prompt of 4096 rows: 216 us, 215, 226 and 253.
-  constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
-  struct Bundle {
-    int32_t req, first, groups, tokens;   // tokens: up to its last row's causal limit
-    int64_t pairs, cost;
-  };
   std::vector<Bundle> bundles;
   int64_t total = 0, bytes = 0;
   int64_t n_bundles = 0;
@@ -95,58 +163,47 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
       total += bundles.back().cost;
     }
   }
-  // Every kv head's work, the same for all, is cut into shares of equal cost, one for each
-  // workgroup (two per CU); a bundle that a share's border cuts becomes several items.  Short shares
-  // are whole turns of all four waves.  Where both workgroups of a CU are there, the older one's
-  // waves go first: it takes 55 % of their work (128 requests of 0.25-32k: 330 us;
-  // 50 %: 334, 60 %: 349).
+  // Every kv head's work, the same for all, in shares, one for each workgroup (two per CU).
   const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
-  constexpr int64_t kTurn = 32, kOld = 55;             // cost of a turn; percent of the older half
   int64_t size = (total + most_shares - 1) / most_shares;
   if (size < 8 * kTurn) size = std::max<int64_t>(1, (size + kTurn - 1) / kTurn) * kTurn;
-  const int64_t shares = std::max<int64_t>(1, (total + size - 1) / size), half = shares / 2;
-  auto border = [&](int64_t s) {                       // cost before share s
-    if (size < 8 * kTurn) return s * size;
-    return s <= half ? total * kOld / 100 * s / std::max<int64_t>(1, half)
-                     : total * kOld / 100 + total * (100 - kOld) / 100 * (s - half) / (shares - half);
-  };
-  if ((n_bundles + shares) * p.nkv > kKv8MaxItems) return too_many((n_bundles + shares) * p.nkv);
-  std::vector<Kv8Item> items;
+  const int64_t shares = std::max<int64_t>(1, (total + size - 1) / size);
+  if (n_bundles + shares > kKv8MaxItems / p.nkv) return too_many((n_bundles + shares) * p.nkv);
+  std::vector<Piece> pieces = by_borders(bundles, shares, size, total);
+  // Cut bundles start twice, write what they have per row group and wait for its join: shares of whole
+  // ones may end that much later.  Requests of one row group, 128 of 0.3-1.2k tokens (12 % more in the
+  // longest share): 50.4 us cut, 42.0 whole; 66 of 2k (76 % more) 56.0 and 61.0; prompts of
+  // 1500-2000 rows (8 %) 105 and 87.  Short shares are cut: whole bundles would leave CUs idle.
+  if (size >= 8 * kTurn) {
+    int64_t end = 0, n_groups = 0;
+    for (const Bundle &u : bundles) n_groups += u.groups;
+    std::vector<Piece> whole = by_length(bundles, shares, end);
+    if (end <= size + 180 + 40 * n_groups / (int64_t)bundles.size()) pieces.swap(whole);
+  }
+  std::vector<Kv8Item> items(pieces.size());
   std::vector<Kv8Group> groups;
-  std::vector<int32_t> first{0};
-  items.reserve(bundles.size() + shares);
+  std::vector<int32_t> first(shares + 1, 0);
+  for (const Piece &x : pieces) ++first[x.share + 1];
+  std::partial_sum(first.begin(), first.end(), first.begin());
+  std::vector<int32_t> next(first);                    // a share's next item
   p.n_parts = 0;
-  int64_t at = 0;                                      // cost before this bundle
-  for (const Bundle &u : bundles) {
-    const int64_t snap = size / 16;                    // a cut this close to the bundle's edge is left out
-    const int64_t grain = u.groups == 1 ? 8 : u.groups == 2 ? 4 : 2, unit = kPair[u.groups] * grain;   // pairs of a turn
-    const size_t item0 = items.size();
-    auto item = [&](int64_t a, int64_t e) {
-      items.push_back(Kv8Item{u.req, (int32_t)(32 * a), (int32_t)std::min<int64_t>(u.tokens, 32 * e), d->ctx_len[u.req],
-                              row0[u.req], nrow[u.req], kv8_pack(u.first, u.groups), -1});
-    };
-    int64_t done = 0;
-    while ((int64_t)first.size() < shares) {
-      const int64_t b = border((int64_t)first.size());
-      if (b >= at + u.cost - snap) break;
-      const int64_t cut = (std::max<int64_t>(b - at - kStart, 0) + unit / 2) / unit * grain;   // pairs before it
-      if (cut > done && cut < u.pairs && b > at + snap) {
-        item(done, cut);
-        done = cut;
-      }
-      first.push_back((int32_t)items.size());
+  for (size_t k = 0; k < pieces.size();) {
+    const Bundle &u = bundles[pieces[k].bundle];
+    int32_t n = 0;                                     // its pieces
+    while (k + n < pieces.size() && pieces[k + n].bundle == pieces[k].bundle) ++n;
+    for (int32_t x = 0; x < n; ++x) {
+      const Piece &w = pieces[k + x];
+      items[next[w.share]++] = Kv8Item{u.req, (int32_t)(32 * w.from), (int32_t)std::min<int64_t>(u.tokens, 32 * w.to),
+                                       d->ctx_len[u.req], row0[u.req], nrow[u.req], kv8_pack(u.first, u.groups),
+                                       n > 1 ? p.n_parts + x * u.groups : -1};
     }
-    item(done, u.pairs);
-    at += u.cost;
-    const int32_t n = (int32_t)(items.size() - item0);
     if (n > 1) {
-      for (int32_t k = 0; k < n; ++k) items[item0 + k].part = p.n_parts + k * u.groups;
       for (int32_t g = 0; g < u.groups; ++g)
         groups.push_back(Kv8Group{row0[u.req], nrow[u.req], u.first + g, p.n_parts + g, n, u.groups, {0, 0}});
       p.n_parts += n * u.groups;
     }
+    k += n;
   }
-  while ((int64_t)first.size() <= shares) first.push_back((int32_t)items.size());
   p.n_items = (int32_t)items.size();
   p.n_groups = (int32_t)groups.size();
   p.n_shares = (int32_t)shares;
