@@ -42,13 +42,13 @@ template <> __device__ __forceinline__ float logit<uint16_t>(const uint16_t *x, 
 // of the row of a workgroup; false: the row has no token, and is left as it was
 __device__ __forceinline__ bool row_counts(const int32_t *tokens, int64_t row) { return !tokens || tokens[row] != -1; }
 
-__device__ __forceinline__ Part join(const Part &a, const Part &b, double sc) {
+__device__ __forceinline__ Part join(const Part &a, const Part &b, float sc) {
   // about the larger maximum; a side without entries (s = 0) adds nothing, a NaN stays
   Part r;
   r.m = fmaxf(a.m, b.m);
   r.pad = 0.f;
   auto side = [&](const Part &p, double &s, double &c) {
-    const double d = p.m == r.m ? 0.0 : (double)p.m - (double)r.m, w = exp2(d * sc);
+    const double d = p.m == r.m ? 0.0 : (double)p.m - (double)r.m, w = __builtin_amdgcn_exp2f((float)d * sc);
     s = p.s == 0.0 ? 0.0 : p.s * w;
     c = p.s == 0.0 ? 0.0 : w * (p.c + d * p.s);
   };
@@ -103,8 +103,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__res
   float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kGroup; ++k) m = fmaxf(m, v[k]);
-  if (gmax) gmax[(row * nch + ch) * kThreads + t] = m;
-  // sums about the wave's maximum; in a wave of nothing but -inf about 0, where they are 0
+    // sums about the wave's maximum; in a wave of nothing but -inf about 0, where they are 0
   const float mw = wave_max(m), mc = mw == -INFINITY ? 0.f : mw;
   float s = 0.f, c = 0.f;
 #pragma unroll
@@ -113,6 +112,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__res
     s += e;
     c = fmaf(fmaxf(d, -3.4e38f), e, c);   // -inf x 0 stays out; a NaN enters through e
   }
+  if (gmax) gmax[(row * nch + ch) * kThreads + t] = m;
   s = wave_sum(s);
   c = wave_sum(c);
   __shared__ Part sh[kThreads / 64];
@@ -127,32 +127,39 @@ __device__ __forceinline__ uint32_t key_of(float f) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kCand = 1024;   // candidates, and groups read again, that the quick way takes
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
 
-struct Best {
-  float v[kCand];
-  int32_t i[kCand];
-};
+constexpr int kCand = 1024, kList = 256;   // candidates, and groups of a wave, that the quick way takes
 
-// The n candidates' ranks (by value, then index): those below k are written out.
-__device__ void write_ranked(const Best &b, int n, int k, const double m, double T, double lse, int32_t *ids, float *lps) {
-  for (int a = threadIdx.x; a < n; a += kThreads) {
-    const float v = b.v[a];
-    const int id = b.i[a];
+// A candidate as a number that is larger for a larger value, and of equal ones (-0 is 0) for the first
+__device__ __forceinline__ uint64_t candidate(float v, int i) { return (uint64_t)key_of(v + 0.f) << 32 | (uint32_t)~i; }
+
+// The n candidates' ranks: those below k are written out.
+__device__ void write_ranked(const uint64_t *best, int n, int k, const double m, double T, double lse, int32_t *ids, float *lps) {
+  for (int a = threadIdx.x; a < n; a += blockDim.x) {
+    const uint64_t mine = best[a];
     int rank = 0;
-    for (int o = 0; o < n; ++o) rank += b.v[o] > v || (b.v[o] == v && b.i[o] < id);
+    for (int o = 0; o < n; o += 8)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rank += o + i < n && best[o + i] > mine;
     if (rank < k) {
-      ids[rank] = id;
-      lps[rank] = (float)(((double)v - m) / T - lse);
+      const uint32_t key = (uint32_t)(mine >> 32);
+      ids[rank] = (int32_t)~(uint32_t)mine;
+      lps[rank] = (float)(((double)value_of(key) - m) / T - lse);
     }
   }
 }
 
-// One workgroup per row, N chunks at most (0: any number), so that a thread holds the group maxima
-// that it needs: those of its own groups, one a chunk.  Bound by latency (a handful of rows) or by
-// starting a workgroup for each: everything that depends on no other load is asked for first.
+// One workgroup per row: four waves look for the most probable tokens, a fifth joins the chunks
+// meanwhile (n_top = 0: alone).  N chunks at most (0: any number), so that a thread holds the group
+// maxima that it needs: those of its own groups, one a chunk.  Bound by latency (a handful of rows) or by
+// starting a workgroup for each: everything that depends on no other load is asked for first, and a
+// wave reads its own groups again, so that two barriers are enough (five of them, and the join in
+// every wave: 6 rows of 128256 with 5 tokens each 7.5 us, so 6.4; 742 rows with 20 15.1 and 13.7).
 template <typename T, int W, int N>
-__global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
+__global__ __launch_bounds__(kThreads + 64) void logprobs_row_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
                                                                float temperature, const int32_t *__restrict__ tokens,
                                                                const Part *__restrict__ parts, const float *__restrict__ gmax,
                                                                int top, float *__restrict__ logprob,
@@ -164,134 +171,154 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
   if (tokens && tok == -1) return;
   const T *x = logits + row * ld;
   const float *gm = gmax + row * nch * kThreads;
-  float gv[N ? N : 1];
-  if (N && top > 0) {
-#pragma unroll
-    for (int c = 0; c < N; ++c) gv[c] = c < nch ? gm[c * kThreads + t] : -INFINITY;
-  }
-  const bool tok_ok = tok >= 0 && tok < V;
-  const float xt = tok_ok ? logit(x, tok) : 0.f;
-  // the chunks joined, by every wave: a lane's chunks in order, then the lanes
-  const float sc = kLog2e / temperature;
-  float m = -INFINITY;
-  double s = 0.0, cs = 0.0;
-  for (int c = lane; c < nch; c += 64) {
-    const Part p = parts[row * nch + c];
-    const float hi = fmaxf(m, p.m);
-    const double d0 = m == hi ? 0.0 : (double)m - hi, d1 = p.m == hi ? 0.0 : (double)p.m - hi;
-    const float w0 = __builtin_amdgcn_exp2f((float)d0 * sc), w1 = __builtin_amdgcn_exp2f((float)d1 * sc);
-    // a side without entries adds nothing, a NaN stays
-    cs = (s == 0.0 ? 0.0 : w0 * (cs + d0 * s)) + (p.s == 0.0 ? 0.0 : w1 * (p.c + d1 * p.s));
-    s = (s == 0.0 ? 0.0 : w0 * s) + (p.s == 0.0 ? 0.0 : w1 * p.s);
-    m = hi;
-  }
-  const float mw = wave_max(m);
-  {
-    const double d = m == mw ? 0.0 : (double)m - mw;
-    const float w = __builtin_amdgcn_exp2f((float)d * sc);
-    cs = s == 0.0 ? 0.0 : w * (cs + d * s);
-    s = s == 0.0 ? 0.0 : w * s;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    s += __shfl_xor(s, o);
-    cs += __shfl_xor(cs, o);
-  }
-  const double Td = temperature, lse = log(s), md = mw;
-  const bool none = s == 0.0;                  // every logit is -inf
-  if (t == 0) {
-    if (logprob) {
-      if (!tok_ok) flag_error(err, kErrToken);
-      logprob[row] = !tok_ok || s != s ? NAN : none || xt == -INFINITY ? -INFINITY : (float)(((double)xt - md) / Td - lse);
-    }
-    if (entropy) entropy[row] = none ? 0.f : (float)(lse - cs / s / Td);
-  }
-  if (top == 0) return;
-
   int32_t *ids = top_ids + row * top;
   float *lps = top_lps + row * top;
   __shared__ float sh_max[kThreads];
-  __shared__ Best best;
-  __shared__ int32_t sh_group[kCand];
-  __shared__ int sh_n, sh_groups;
-  __shared__ float sh_tau;
-  if (t == 0) {
-    sh_n = 0;
-    sh_groups = 0;
-  }
-  if (t < top) {                               // places that no entry fills
-    ids[t] = -1;
-    lps[t] = s != s ? NAN : -INFINITY;
-  }
-  float mine = -INFINITY;
-  if constexpr (N > 0) {
+  __shared__ uint64_t best[kCand];
+  __shared__ int32_t sh_group[kThreads / 64][kList];
+  __shared__ int sh_n;
+  __shared__ bool sh_many;
+  __shared__ float sh_m;
+  __shared__ double sh_lse;
+  const bool search = t + 64 < (int)blockDim.x;
+  if (!search) {
+    // the chunks joined: a lane's in order, then the lanes
+    const bool tok_ok = tok >= 0 && tok < V;
+    const float xt = tok_ok ? logit(x, tok) : 0.f;
+    const float sc = kLog2e / temperature;
+    float m = -INFINITY;
+    double s = 0.0, cs = 0.0;
+    for (int c = lane; c < nch; c += 64) {
+      const Part p = parts[row * nch + c];
+      const float hi = fmaxf(m, p.m);
+      const double d0 = m == hi ? 0.0 : (double)m - hi, d1 = p.m == hi ? 0.0 : (double)p.m - hi;
+      const float w0 = __builtin_amdgcn_exp2f((float)d0 * sc), w1 = __builtin_amdgcn_exp2f((float)d1 * sc);
+      // a side without entries adds nothing, a NaN stays
+      cs = (s == 0.0 ? 0.0 : w0 * (cs + d0 * s)) + (p.s == 0.0 ? 0.0 : w1 * (p.c + d1 * p.s));
+      s = (s == 0.0 ? 0.0 : w0 * s) + (p.s == 0.0 ? 0.0 : w1 * p.s);
+      m = hi;
+    }
+    const float mw = wave_max(m);
+    {
+      const double d = m == mw ? 0.0 : (double)m - mw;
+      const float w = __builtin_amdgcn_exp2f((float)d * sc);
+      cs = s == 0.0 ? 0.0 : w * (cs + d * s);
+      s = s == 0.0 ? 0.0 : w * s;
+    }
 #pragma unroll
-    for (int c = 0; c < N; ++c) mine = fmaxf(mine, gv[c]);
-  } else {
-    for (int c = 0; c < nch; ++c) mine = fmaxf(mine, gm[c * kThreads + t]);
+    for (int o = 32; o > 0; o >>= 1) {
+      s += __shfl_xor(s, o);
+      cs += __shfl_xor(cs, o);
+    }
+    const double lse = log(s);
+    const bool none = s == 0.0;                // every logit is -inf
+    if (lane == 0) {
+      if (logprob) {
+        if (!tok_ok) flag_error(err, kErrToken);
+        logprob[row] = !tok_ok || s != s                ? NAN
+                       : none || xt == -INFINITY ? -INFINITY
+                                                 : (float)(((double)xt - mw) / temperature - lse);
+      }
+      if (entropy) entropy[row] = none ? 0.f : (float)(lse - cs / s / temperature);
+      sh_m = mw;
+      sh_lse = lse;
+    }
+    if (lane < top) {                          // places that no entry fills
+      ids[lane] = -1;
+      lps[lane] = s != s ? NAN : -INFINITY;
+    }
+    if (top == 0) return;                      // there is no other wave
   }
-  sh_max[t] = mine;
+  float gv[N ? N : 1];
+  if (search) {
+    float mine = -INFINITY;
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int c = 0; c < N; ++c) gv[c] = c < nch ? gm[c * kThreads + t] : -INFINITY;
+#pragma unroll
+      for (int c = 0; c < N; ++c) mine = fmaxf(mine, gv[c]);
+    } else {
+      for (int c = 0; c < nch; ++c) mine = fmaxf(mine, gm[c * kThreads + t]);
+    }
+    sh_max[t] = mine;
+    if (t == 0) {
+      sh_n = 0;
+      sh_many = false;
+    }
+  }
   __syncthreads();
-  // the top-th largest of 64 maxima, each of four threads' groups: at least `top` entries reach it
-  static_assert(WISP_TOP_MAX <= 64, "a bound from 64 maxima");
-  if (t < 64) {
-    mine = fmaxf(fmaxf(sh_max[t], sh_max[t + 64]), fmaxf(sh_max[t + 128], sh_max[t + 192]));
+  if (search) {
+    // A bound that at least `top` entries reach: the top-th largest of 64 maxima, each of four threads'
+    // groups.  Their keys' last six bits give way to the lane, so that all differ.
+    static_assert(WISP_TOP_MAX <= 64, "a bound from 64 maxima; a wave fills the places");
+    const float most = fmaxf(fmaxf(sh_max[lane], sh_max[lane + 64]), fmaxf(sh_max[lane + 128], sh_max[lane + 192]));
+    const uint32_t key = key_of(most + 0.f) & ~63u;
+    const uint32_t mine = key | lane;
     int rank = 0;
-#pragma unroll 16
-    for (int o = 0; o < 64; ++o) {
-      const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), o));
-      rank += v > mine || (v == mine && o < t);
-    }
-    if (rank == top - 1) sh_tau = mine;
-  }
-  __syncthreads();
-  const float tau = sh_tau;
-  auto list = [&](float v, int c) {
-    if (v >= tau && v > -INFINITY) {
-      const int at = atomicAdd(&sh_groups, 1);   // the order does not matter: candidates are ranked
-      if (at < kCand) sh_group[at] = c * kThreads + t;
-    }
-  };
-  if constexpr (N > 0) {
 #pragma unroll
-    for (int c = 0; c < N; ++c) list(gv[c], c);
-  } else {
-    for (int c = 0; c < nch; ++c) list(gm[c * kThreads + t], c);
-  }
-  __syncthreads();
-  const int ng = sh_groups;
-  if (ng <= kCand) {
-    constexpr int P = kGroup / W;                // loads of a group
-    for (int u = t; u < ng * P; u += kThreads) {
-      const int g = sh_group[u / P], e0 = g / kThreads * kChunk + entry_at<W>(g % kThreads, u % P * W);
-      float v[W];
-      if (W > 1 && e0 + W <= V) {
-        const uint4 r = ld16(x + e0);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    for (int o = 0; o < 64; ++o) rank += (uint32_t)__builtin_amdgcn_readlane(mine, o) > mine;
+    const uint32_t tau = __builtin_amdgcn_readlane(key, __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == top - 1)));
+    auto reaches = [&](float v) { return v > -INFINITY && key_of(v + 0.f) >= tau; };
+    // the wave's groups that do
+    int32_t *list = sh_group[t >> 6];
+    int ng = 0;
+    auto note = [&](float v, int c) {
+      const bool in = reaches(v);
+      const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
+      const int at = ng + __popcll(mask & ((1ull << lane) - 1));
+      if (in && at < kList) list[at] = c * kThreads + t;
+      ng += __popcll(mask);
+    };
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int c = 0; c < N; ++c) note(gv[c], c);
+    } else {
+      for (int c = 0; c < nch; ++c) note(gm[c * kThreads + t], c);
+    }
+    if (ng > kList) {
+      if (lane == 0) sh_many = true;
+    } else {
+      constexpr int P = kGroup / W;            // loads of a group
+      for (int u0 = 0; u0 < ng * P; u0 += 64) {
+        const int u = min(u0 + lane, ng * P - 1), g = list[u / P];
+        const int e0 = g / kThreads * kChunk + entry_at<W>(g % kThreads, u % P * W);
+        float v[W];
+        if (W > 1 && e0 + W <= V) {
+          const uint4 r = ld16(x + e0);
+          const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i % 4]);
+            else v[i] = __uint_as_float(i & 1 ? w[i / 2 % 4] & 0xFFFF0000u : w[i / 2 % 4] << 16);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i) v[i] = e0 + i < V ? logit(x, e0 + i) : -INFINITY;
+        }
+        uint64_t mask[W];
+        int n = 0;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i % 4]);
-          else v[i] = __uint_as_float(i & 1 ? w[i / 2 % 4] & 0xFFFF0000u : w[i / 2 % 4] << 16);
+          mask[i] = __builtin_amdgcn_ballot_w64(u0 + lane < ng * P && reaches(v[i]));
+          n += __popcll(mask[i]);
         }
-      } else {
+        if (n == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh_n, n);   // the order does not matter: candidates are ranked
+        at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = e0 + i < V ? logit(x, e0 + i) : -INFINITY;
+        for (int i = 0; i < W; ++i) {
+          const int to = at + __popcll(mask[i] & ((1ull << lane) - 1));
+          if ((mask[i] >> lane & 1) && to < kCand) best[to] = candidate(v[i], e0 + i);
+          at += __popcll(mask[i]);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < W; ++i)
-        if (v[i] >= tau && v[i] > -INFINITY) {
-          const int at = atomicAdd(&sh_n, 1);
-          if (at < kCand) {
-            best.v[at] = v[i];
-            best.i[at] = e0 + i;
-          }
-        }
     }
-    __syncthreads();
-    if (sh_n <= kCand) {
-      write_ranked(best, sh_n, top, md, Td, lse, ids, lps);
-      return;
-    }
+  }
+  __syncthreads();
+  if (!sh_many && sh_n <= kCand) {
+    write_ranked(best, sh_n, top, sh_m, temperature, sh_lse, ids, lps);
+    return;
   }
 
   // Too many reach the bound (a mask's lowest value in most places, say): the top-th largest
@@ -302,11 +329,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
   uint32_t prefix = 0, left = top;               // keys wanted among those with this prefix
   for (int shift = 24; shift >= 0; shift -= 8) {
     __syncthreads();
-    hist[t] = 0;
+    if (search) hist[t] = 0;
     __syncthreads();
-    for (int e = t; e < (V + 63) / 64 * 64; e += kThreads) {   // whole waves
+    for (int e = search ? t : INT32_MAX; e < (V + 63) / 64 * 64; e += kThreads) {   // whole waves
       const float v = e < V ? logit(x, e) : -INFINITY;
-      const uint32_t key = key_of(v);
+      const uint32_t key = key_of(v + 0.f);
       const bool in = e < V && v > -INFINITY && (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8));
       const int bin = key >> shift & 255;
       uint64_t todo = __builtin_amdgcn_ballot_w64(in);
@@ -335,25 +362,23 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(const T *__restr
   __syncthreads();
   for (int e0 = 0; e0 < V; e0 += kThreads) {
     const int e = e0 + t;
-    const float v = e < V ? logit(x, e) : -INFINITY;
-    const uint32_t key = key_of(v);
-    const bool here = e < V && v > -INFINITY;
+    const bool in = search && e < V;
+    const float v = in ? logit(x, e) : -INFINITY;
+    const uint32_t key = key_of(v + 0.f);
+    const bool here = in && v > -INFINITY;
     const uint64_t eq = __builtin_amdgcn_ballot_w64(here && key == prefix);
-    if ((t & 63) == 0) sh_count[t >> 6] = __popcll(eq);
+    if (search && (t & 63) == 0) sh_count[t >> 6] = __popcll(eq);
     __syncthreads();
     uint32_t at = equal_before + __popcll(eq & ((1ull << (t & 63)) - 1));
-    for (int w = 0; w < (t >> 6); ++w) at += sh_count[w];
+    for (int w = 0; w < kThreads / 64; ++w) at += w < (t >> 6) ? sh_count[w] : 0;
     if (here && (key > prefix || (key == prefix && at < left))) {
       const int k = atomicAdd(&sh_n, 1);
-      if (k < kCand) {
-        best.v[k] = v;
-        best.i[k] = e;
-      }
+      if (k < kCand) best[k] = candidate(v, e);
     }
     for (int w = 0; w < kThreads / 64; ++w) equal_before += sh_count[w];
     __syncthreads();
   }
-  write_ranked(best, min(sh_n, kCand), top, md, Td, lse, ids, lps);
+  write_ranked(best, min(sh_n, kCand), top, sh_m, temperature, sh_lse, ids, lps);
 }
 
 int chunks_of(int32_t vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
@@ -394,7 +419,7 @@ extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, in
     const float sc = kLog2e / temperature;
     auto go = [&](auto *x, auto chunk, auto row) {
       launch(chunk, (uint32_t)(rows * nch), kThreads, 0, s, x, (int)vocab, ld, nch, sc, tokens, parts, gmax);
-      launch(row, (uint32_t)rows, kThreads, 0, s, x, (int)vocab, ld, nch, temperature, tokens, (const Part *)parts,
+      launch(row, (uint32_t)rows, n_top ? kThreads + 64 : 64, 0, s, x, (int)vocab, ld, nch, temperature, tokens, (const Part *)parts,
              (const float *)gmax, (int)n_top, logprob, entropy, top_tokens, top_logprobs, err);
     };
     // the row kernel that holds the chunks' group maxima (V <= 131072: 16, twice that: 32)

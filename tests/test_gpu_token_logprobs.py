@@ -146,6 +146,21 @@ def test_values_that_are_not_finite():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [40, 5000, 90000])
+def test_zeros_of_either_sign_are_equal(V):
+    x, tok = _logits(3, V, torch.float32, V)
+    x[0] = -x[0].abs()
+    x[0, ::7], x[0, 3::7] = -0.0, 0.0          # the largest: by index, whichever sign
+    x[1] = 0.0
+    x[1, ::2] = -0.0
+    x[2] = -x[2].abs()
+    x[2, V - 3:], x[2, 2] = 0.0, -0.0          # a few
+    for top in (1, 6, 32):
+        got, _ = _run(x, V, tok, 1.0, top)
+        _check(x, V, tok, 1.0, top, got)
+
+
+@pytest.mark.gpu
 def test_rows_without_a_token_are_left():
     x, tok = _logits(6, 30000, torch.float32, 5)
     tok[[0, 3, 5]] = -1
