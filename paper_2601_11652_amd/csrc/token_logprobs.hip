@@ -60,7 +60,10 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b, float sc) {
   return r;
 }
 
-// grid rows x chunks, chunks fastest
+// Grid rows x chunks, chunks fastest.  Bound by the memory where there are many fp32 rows (742 of
+// 128256: 66 us for 381 MB, 5.8 TB/s), by instructions in bf16, whose entries come twice as fast (300
+// of 50021: 11.3 us for 30 MB).  A chunk is 32 entries a thread: with the sums about the wave's own
+// maximum, known before the first exponential, an entry takes one exponential and no rescaling.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
                                                                  float sc, const int32_t *__restrict__ tokens,
@@ -74,23 +77,32 @@ __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__res
   float v[kGroup];
   if constexpr (VEC) {
     uint4 raw[kGroup / W];
+    const bool whole = n == kChunk;        // every chunk but the row's last
 #pragma unroll
     for (int k = 0; k < kGroup / W; ++k) {   // all loads of the thread in flight at once
       const int e = (k * kThreads + t) * W;
-      raw[k] = make_uint4(0, 0, 0, 0);
-      if (e + W <= n) raw[k] = ld16_stream(x + e);
+      if (whole || e + W <= n) raw[k] = ld16_stream(x + e);
     }
 #pragma unroll
     for (int k = 0; k < kGroup / W; ++k) {
-      const int e = (k * kThreads + t) * W;
       const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        float f;
-        if constexpr (sizeof(T) == 4) f = __uint_as_float(w[i]);
-        else f = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
-        if (e + W > n) f = e + i < n ? logit(x, e + i) : -INFINITY;
-        v[k * W + i] = f;
+        if constexpr (sizeof(T) == 4) v[k * W + i] = __uint_as_float(w[i]);
+        else v[k * W + i] = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+      }
+    }
+    if (!whole) {
+#pragma unroll
+      for (int k = 0; k < kGroup / W; ++k) {
+        const int e = (k * kThreads + t) * W;
+        if (e + W > n) {                   // at or past the row's end
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const float f = logit(x, min(e + i, n - 1));
+            v[k * W + i] = e + i < n ? f : -INFINITY;
+          }
+        }
       }
     }
   } else {
