@@ -12,6 +12,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "api.h"
@@ -24,6 +25,7 @@ using namespace wisp;
 namespace {
 
 constexpr int kChunk = 8192, kThreads = 256, kGroup = kChunk / kThreads;
+constexpr int kMaxChunks = 1 << 23;   // of a launch
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Part {   // of one chunk: the maximum, and the sums about it (0 where nothing is above -inf)
@@ -429,10 +431,19 @@ extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, in
     int *err = reinterpret_cast<int *>(ws);
     const hipStream_t s = (hipStream_t)stream;
     const float sc = kLog2e / temperature;
+    // a launch has less than 2^32 threads: this many rows each (at least 64)
+    const int32_t step = kMaxChunks / nch;
     auto go = [&](auto *x, auto chunk, auto row) {
-      launch(chunk, (uint32_t)(rows * nch), kThreads, 0, s, x, (int)vocab, ld, nch, sc, tokens, parts, gmax);
-      launch(row, (uint32_t)rows, n_top ? kThreads + 64 : 64, 0, s, x, (int)vocab, ld, nch, temperature, tokens, (const Part *)parts,
-             (const float *)gmax, (int)n_top, logprob, entropy, top_tokens, top_logprobs, err);
+      for (int64_t r = 0; r < rows; r += step) {
+        const uint32_t n = (uint32_t)std::min<int64_t>(step, rows - r);
+        const int32_t *tok = tokens ? tokens + r : nullptr;
+        Part *p = parts + r * nch;
+        float *g = gmax ? gmax + r * nch * kThreads : nullptr;
+        launch(chunk, n * nch, kThreads, 0, s, x + r * ld, (int)vocab, ld, nch, sc, tok, p, g);
+        launch(row, n, n_top ? kThreads + 64 : 64, 0, s, x + r * ld, (int)vocab, ld, nch, temperature, tok, (const Part *)p,
+               (const float *)g, (int)n_top, logprob ? logprob + r : nullptr, entropy ? entropy + r : nullptr,
+               n_top ? top_tokens + r * n_top : nullptr, n_top ? top_logprobs + r * n_top : nullptr, err);
+      }
     };
     // the row kernel that holds the chunks' group maxima (V <= 131072: 16, twice that: 32)
     auto rows_of = [&](auto *x, auto w) {

@@ -188,6 +188,23 @@ def test_tokens_out_of_range_are_reported():
 
 
 @pytest.mark.gpu
+def test_more_rows_than_a_launch_has_threads_for():
+    rows, V = (1 << 24) + 4097, 3
+    x, tok = _logits(rows, V, torch.float32, 9)
+    tok[5::2] = -1
+    (lp, H, _, _), ws = _run(x, V, tok, 1.0, 0)
+    W.wisp_check(ws)
+    log(f"logprobs of {rows} rows")
+    keep = tok != -1
+    ls = torch.log_softmax(x.double(), -1)
+    want = ls.gather(1, tok.clamp_min(0).long()[:, None])[:, 0]
+    # three entries: each sum takes a handful of fp32 roundings of terms below 16
+    assert ((lp.double() - want).abs()[keep] <= 64 * 2.0 ** -24 * (1 + want.abs()[keep])).all()
+    assert ((H.double() + (ls.exp() * ls).sum(-1)).abs()[keep] <= 64 * 2.0 ** -24 * 16).all()
+    assert (lp[~keep] == 7).all() and (H[~keep] == 7).all()
+
+
+@pytest.mark.gpu
 def test_captured_replayed_and_on_two_streams():
     x, tok = _logits(20, 40000, torch.float32, 8)
     rows, V, top = 20, 40000, 6
