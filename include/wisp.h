@@ -276,7 +276,13 @@ typedef struct {
  * for wisp_attention), and desc's ctx_len, gamma, prefill_len: rows are ordered as in
  * wisp_verify.  While `stream` is being captured the lists travel as kernel arguments.
  * The calls below only launch kernels: they may be captured, on any stream ordered after the
- * plan's.  They use the workspace's scratch, so calls on one plan must not overlap.
+ * plan's.  They use the workspace's scratch, so calls on one plan must not overlap.  Outputs must not
+ * overlap inputs.  Block ids outside [0, n_blocks) are recorded in the workspace for wisp_check: such
+ * a page is not written, and what a row reads of it is undefined.
+ * WISP_E_UNSUPPORTED (and a workspace size of 0): more than WISP_ROWS_MAX rows, more than 2^22 items of
+ * attention work (for each kv head and request one per 128 rows x query heads of a kv head, for fp32
+ * and batches of at most 16 of them per request 64, and 512 in all), or more than 2^32 threads of an
+ * append ((pages that get rows) x n_kv x 2 head_dim + rows x n_q x head_dim / 32).
  */
 typedef struct { uint64_t opaque[32]; } wisp_kv8_batch;
 
@@ -314,7 +320,8 @@ wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, 
  * operators above (a step's plan is its own).  Inputs, outputs, errors and the rollback by length as
  * wisp_verify's; the workspace holds wisp_verify_kv8_workspace_size bytes, plus
  * wisp_logits_workspace_size when target_logits is NULL.  An fp32 model's contexts have no limit
- * of their own.
+ * of their own.  Batches are limited as wisp_kv8_plan's.  Like wisp_verify it is not for a stream that is
+ * being captured.
  */
 size_t wisp_verify_kv8_workspace_size(const wisp_model *model, const wisp_batch_desc *desc);
 wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const wisp_batch_desc *desc,
@@ -541,7 +548,8 @@ wisp_status wisp_reject_predict(const wisp_reject_mlp *mlp, const float *feature
  * A NaN or +infinity among a row's logits makes its ln p and entropy NaN.  A token outside -1 ..
  * vocab - 1 gets NaN and is reported by wisp_check(workspace): workspace is DEVICE scratch of
  * wisp_token_logprobs_workspace_size bytes, 16-byte aligned, its first 256 bytes zero before the
- * first use.
+ * first use.  The call only launches kernels: it may be captured.  WISP_E_UNSUPPORTED: vocab above 2^30, or
+ * rows x ceil(vocab / 8192) of 2^31 or more.
  */
 #define WISP_TOP_MAX 32
 size_t wisp_token_logprobs_workspace_size(int32_t rows, int32_t vocab, int32_t n_top);

@@ -548,7 +548,7 @@ def wisp_kv8_plan(model: wisp_model, desc: BatchDesc, workspace, stream=None) ->
     all layers of a step."""
     _check_desc(desc)
     wp, wn = _ws(workspace)
-    if desc.B > 0 and desc.page_table.device != workspace.device:
+    if desc.page_table is not None and desc.B > 0 and desc.page_table.device != workspace.device:
         raise ValueError(f"desc.page_table: on {desc.page_table.device}, the workspace on {workspace.device}")
     c = wisp_kv8_batch()
     with _On(workspace.device):
@@ -615,11 +615,14 @@ def wisp_verify_kv8(model: wisp_model, kv: KV8Pool, desc: BatchDesc, tokens, dra
     V = model.vocab
     probs = _dev(draft_probs, "draft_probs", desc.S * V, dtype=_f32()) if desc.S > 0 else _ptr(draft_probs)
     logits = None if target_logits is None else _dev(target_logits, "target_logits", desc.M * V, dtype=_f32())
-    _ok(lib.wisp_verify_kv8(C.byref(model), C.byref(kv.c), C.byref(desc.c),
-                            _dev(tokens, "tokens", desc.rows, dtype=_i32()), probs, rng_seed & ((1 << 64) - 1),
-                            _dev(accept_len, "accept_len", desc.B, dtype=_i32()),
-                            _dev(out_tokens, "out_tokens", desc.M, dtype=_i32()), logits, *_ws(workspace),
-                            _stream(stream)))
+    args = (_dev(tokens, "tokens", desc.rows, dtype=_i32()), probs, rng_seed & ((1 << 64) - 1),
+            _dev(accept_len, "accept_len", desc.B, dtype=_i32()), _dev(out_tokens, "out_tokens", desc.M, dtype=_i32()),
+            logits, *_ws(workspace))
+    for t in (tokens, accept_len, out_tokens, workspace):
+        if t.device != kv.device:
+            raise ValueError(f"a tensor on {t.device}, kv on {kv.device}")
+    with _On(kv.device):
+        _ok(lib.wisp_verify_kv8(C.byref(model), C.byref(kv.c), C.byref(desc.c), *args, _stream(stream)))
 
 
 def wisp_uniform(rng_seed: int, req_id: int, tag: int, row: int, n: int, out, stream=None):

@@ -146,12 +146,15 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
     bytes += 2 * ((int64_t)d->ctx_len[i] + nrow[i]) * p.nkv * p.hd;
     n_bundles += (((int64_t)nrow[i] * G + R - 1) / R + 3) / 4;
   }
-  // Items carry a row group's index in 24 bits, and the kernels count a request's rows x G and the
-  // threads of an append in 32: both hold for every batch of at most kKv8MaxItems bundles x kv heads.
+  // Items carry a row group's index in 24 bits, and the kernels count a request's rows x G in 32: both
+  // hold for every batch of at most kKv8MaxItems bundles x kv heads.
   auto too_many = [&](int64_t n) {
     return fail(WISP_E_UNSUPPORTED, "the batch needs %lld attention work items (at most %d)", (long long)n, kKv8MaxItems);
   };
   if (n_bundles > kKv8MaxItems / p.nkv) return too_many(n_bundles * p.nkv);
+  // the append's threads, in one launch and counted in 32 bits
+  if (2 * p.hd * ((int64_t)p.n_units * p.nkv + 1) + (int64_t)p.rows * (p.hd / 16) * ((p.nq + 1) / 2) > UINT32_MAX)
+    return fail(WISP_E_UNSUPPORTED, "rows x heads beyond one append's 2^32 threads");
   p.stream = bytes > (256 << 20);                      // more than the last-level cache holds
   for (int i = 0; i < p.B; ++i) {
     const int64_t groups = ((int64_t)nrow[i] * G + R - 1) / R, nb = (groups + 3) / 4;

@@ -78,6 +78,11 @@ def test_plan_refusals():
     big = _desc([5] * n, [0] * n)
     assert W.wisp_kv8_workspace_size(W.GpuModel.shape_only(shape(32, 32, 64, True)), big) == 0
     assert "work items" in W.wisp_last_error()
+    # one that would pass an append's 2^32 threads: prompts of 229 thousand rows on 2048 heads
+    m = W.GpuModel.shape_only(shape(2048, 2048, 128, True))
+    wide = W.BatchDesc(np.zeros(7, np.int32), np.zeros(7, np.int32), None, 1.0, None, np.full(7, 32768, np.int32))
+    assert W.wisp_kv8_workspace_size(m, wide) == 0
+    assert "threads" in W.wisp_last_error()
     # long contexts do not: 64 requests of 2^29 tokens
     ctx = 1 << 29
     far = _desc([ctx] * 64, [0] * 64, stride=(ctx >> 4) + 1)
