@@ -13,6 +13,7 @@ wisp_check, wisp_last_error, wisp_schedule, wisp_draft_stats, wisp_reject_predic
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -222,7 +223,7 @@ def _dev(t, what: str, numel: int = 0, dtype=None, elem: int | None = None, cont
     on the GPU, of the element type the entry point reads, contiguous, and holding at least
     `numel` elements.  A host tensor's pointer must never reach a kernel."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what}: expected a device tensor, got {type(t).__name__}"
                          + (f" on {t.device}" if isinstance(t, torch.Tensor) else ""))
     if dtype is not None and t.dtype != dtype:
@@ -563,20 +564,13 @@ def _kv8_check(batch: KV8Batch, kv: KV8Pool, a, b):
         raise ValueError(f"tensors on {a.device} and {b.device}, kv on {kv.device}, the batch was planned on {batch.device}")
 
 
-class _On:
+_SAME = contextlib.nullcontext()
+
+
+def _On(device):
     """Makes a device current for a call on its tensors, if it is not."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+    import torch
+    return _SAME if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def wisp_kv8_append(batch: KV8Batch, kv: KV8Pool, qkv, q, stream=None):
@@ -693,10 +687,11 @@ def wisp_token_logprobs(logits, vocab: int, tokens, temperature: float, logprob,
     pv = None if top_logprobs is None else _dev(top_logprobs, "top_logprobs", dtype=f32)
     if ws is None:
         ws = workspace(wisp_token_logprobs_workspace_size(rows, vocab, n_top), logits.device)
+    on = logits.get_device()
     for t in (tokens, logprob, entropy, top_tokens, top_logprobs, ws):
-        if t is not None and t.device != logits.device:
+        if t is not None and t.get_device() != on:
             raise ValueError(f"a tensor on {t.device}, logits on {logits.device}")
-    ld = logits.stride(0) if rows > 1 else max(logits.shape[1], vocab)
+    ld = logits.stride(0) if rows > 1 else logits.shape[1]
     code = WISP_F32 if logits.dtype == f32 else WISP_BF16
     with _On(logits.device):
         _ok(lib.wisp_token_logprobs(px, code, rows, vocab, ld, temperature, pt, n_top, pl, pe, pi, pv, *_ws(ws),
