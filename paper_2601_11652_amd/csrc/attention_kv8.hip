@@ -188,7 +188,10 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
   float m_run[RB], l_run[RB];
   floatx4 o[RB][MB];
   int jrow[RB];
+  int open = 0;                          // tokens before it are seen by every row of the wave's group
   auto begin_item = [&]() __attribute__((always_inline)) {
+    const int first = (kv8_first(it.groups) + sh.rg) * ROWS;
+    open = min(sh.end, it.ctx + __builtin_amdgcn_readfirstlane(first / G) + 1);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       jrow[rb] = min((kv8_first(it.groups) + sh.rg) * ROWS + rb * 16 + lc, it.nrow * G - 1) / G;
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
     load_k(i + 1);
     __builtin_amdgcn_sched_barrier(0);
     // s[rb][h][x][e]: token tp + 32 h + 8 lg + 4 x + e, query row rb * 16 + lc of the group, without K's scale
-    if (tp + 64 > min(sh.end, it.ctx + 1)) {
+    if (tp + 64 > open) {
       const int t = opaque(tp + 8 * lg);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
