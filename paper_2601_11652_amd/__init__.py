@@ -7,8 +7,9 @@ the library has not been built -- there is no fallback implementation.
 
 Entry points keep the C names: wisp_verify, wisp_accept, wisp_attention,
 wisp_pack_linear, wisp_workspace_size, wisp_accept_workspace_size, wisp_uniform,
-wisp_check, wisp_last_error, wisp_schedule, wisp_draft_stats, wisp_reject_predict;
-``KVManager`` wraps the wisp_kvm_* calls and ``RejectMLP`` the predictor's weights.
+wisp_check, wisp_last_error, wisp_schedule, wisp_draft_stats, wisp_reject_predict,
+wisp_kv8_plan, wisp_kv8_append, wisp_attention_kv8, wisp_verify_kv8, wisp_token_logprobs;
+``KV8Pool`` holds the 8-bit cache and ``KV8Batch`` a batch planned for it, ``KVManager`` wraps the wisp_kvm_* calls and ``RejectMLP`` the predictor's weights.
 ``GpuModel`` and ``BatchDesc`` assemble the C structs.
 """
 from __future__ import annotations

@@ -13,6 +13,11 @@
 // first product in the order that the second consumes.  The waves of a row group are joined
 // through LDS, the parts of a context that several items share by a second kernel.
 //
+// Bound by the memory for long contexts (128 requests of 0.25-32k tokens, 32 + 8 heads of 128: 1.73 GB in
+// 327 us, 5.3 TB/s), by vector instructions for prompts (4096 rows: 197 us, 0.71 PFLOP/s: two conversions
+// and five instructions of softmax for each product), by latency for few requests (one of 1300
+// tokens: 8 us and 3 for the join).
+//
 // An fp32 model's queries and probabilities enter the products as three bf16 parts each (8 bits
 // of the significand per part: 24 in all), so its results are fp32's.
 #include "kernels.h"
@@ -507,7 +512,8 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
 }
 
 // Joins a row group's partials in order, in rounds of kRound whose loads are all issued before the
-// first is used: one thread per (row, 8 dims).  Bound by latency: a launch and two dependent loads.
+// first is used: one thread per (row, 8 dims).  Bound by latency: a launch and two
+// dependent loads (32 requests: 4.6 us).
 constexpr int kRound = 8;
 template <bool F32>
 __global__ __launch_bounds__(256) void kv8_join_kernel(const Kv8Group *__restrict__ groups, int rows_per_group, int hd,

@@ -42,7 +42,7 @@ struct Piece {                          // page pairs from .. to - 1 of a bundle
 // waves; two groups have two waves each but share what is read, three or four one.  Starting
 // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
 // 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
-// A prompt of 4096 rows: 216 us, 215, 226 and 253.
+// A prompt of 4096 rows, cut: 216 us, 215, 226 and 253.
 constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
 constexpr int64_t kTurn = 32;           // cost of a turn
 // Where both workgroups of a CU are there, the older one's waves go first: percent of the work that
