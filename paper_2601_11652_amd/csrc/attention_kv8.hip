@@ -14,12 +14,15 @@
 // through LDS, the parts of a context that several items share by a second kernel.
 //
 // Bound by the memory for long contexts (128 requests of 0.25-32k tokens, 32 + 8 heads of 128: 1.73 GB in
-// 327 us, 5.3 TB/s), by vector instructions for prompts (4096 rows: 197 us, 0.71 PFLOP/s: two conversions
-// and five instructions of softmax for each product), by latency for few requests (one of 1300
+// 327 us, 5.3 TB/s), by vector instructions for prompts (4096 rows: 185 us, 0.75 PFLOP/s: half
+// a conversion and five instructions of softmax for each product), by latency for few requests (one of 1300
 // tokens: 8 us and 3 for the join).
 //
 // An fp32 model's queries and probabilities enter the products as three bf16 parts each (8 bits
 // of the significand per part: 24 in all), so its results are fp32's.
+#include <algorithm>
+#include <type_traits>
+
 #include "kernels.h"
 #include "kv8.h"
 
@@ -57,8 +60,15 @@ __device__ __forceinline__ int opaque(int x) {
 // their row's result is NaN.
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, 3.402823466e38f); }
 
+// block ids, read through the scalar cache: nothing writes them while a kernel runs
+typedef const int32_t __attribute__((address_space(4))) ids_t;
+
+__device__ __forceinline__ uint4 as_uint4(bf16x8_t v) { return __builtin_bit_cast(uint4, v); }
+
 struct Kv8Args {
   const Kv8Item *items;
+  const int32_t *wide_first;   // as first, of the workgroups before wide_blocks, which run wide items
+  int wide_blocks;
   const int32_t *first;   // share s runs items first[s] .. first[s + 1] - 1
   const int32_t *page_table;
   const uint8_t *k, *v;
@@ -72,7 +82,286 @@ struct Kv8Args {
   bool packed;
 };
 
-template <int HD, int RB, bool F32, bool STREAM = false>
+// The online softmax of a quad: its scores s (without K's scale; [row block][pair][half of its pages'
+// slots]) to probabilities x V's scale, in the order that the second product consumes.  Scales of the
+// lane's pages: ks K's in base 2, lv log2 of V's, vi its inverse.
+template <int RB, int MB, int NP>
+__device__ __forceinline__ void softmax(const floatx4 (&s)[RB][2][2], const float (&ks)[2], const float (&lv)[2],
+                                        const float (&vi)[2], float (&m_run)[RB], float (&l_run)[RB], floatx4 (&o)[RB][MB],
+                                        uint4 (&pb)[NP][RB][2]) {
+  constexpr bool F32 = NP > 1;
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    float mx[2];                       // scores in base 2
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      mx[h] = ks[h] * max2(max2(max2(s[rb][h][0][0], s[rb][h][0][1]), max2(s[rb][h][0][2], s[rb][h][0][3])),
+                           max2(max2(s[rb][h][1][0], s[rb][h][1][1]), max2(s[rb][h][1][2], s[rb][h][1][3])));
+    const float top = xor32_max(xor16_max(fmaxf(mx[0], mx[1])));
+    // the running maximum rises only by more than 8: p stays below 2^8, and the accumulators
+    // are rescaled on few quads; numerator and denominator share the reference
+    const bool grow = top > m_run[rb] + 8.0f;
+    if (__builtin_amdgcn_ballot_w64(grow)) {
+      const float alpha = grow ? __builtin_amdgcn_exp2f(m_run[rb] - top) : 1.0f;
+      m_run[rb] = grow ? top : m_run[rb];
+      l_run[rb] *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) o[rb][mb] *= alpha;
+    }
+    const float m = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // p x V's scale = 2^(s ks - m + log2 vs)
+      const float off = lv[h] - m;
+      float rs = 0.f;
+      uint32_t pw[NP][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          float f = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e], ks[h], off));
+          float g = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e + 1], ks[h], off));
+          if constexpr (F32) rs += f + g;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const uint32_t w = pack2bf_rne(f, g);
+            pw[p][x * 2 + e / 2] = w;
+            f -= low(w);
+            g -= high(w);
+          }
+          // bf16: the sum adds the rounded values, as the second product does
+          if constexpr (!F32) {
+            const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+            rs = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[0][x * 2 + e / 2]), one, rs, false);
+          }
+        }
+      l_run[rb] = __builtin_fmaf(rs, vi[h], l_run[rb]);   // this lane's tokens; the lanes are added up at the end
+#pragma unroll
+      for (int p = 0; p < NP; ++p) pb[p][rb][h] = make_uint4(pw[p][0], pw[p][1], pw[p][2], pw[p][3]);
+    }
+  }
+}
+
+// The same for bundles of three or four row groups (a prompt's, whose rows are many and whose codes are
+// few), of which each wave takes one: by themselves they would all convert the same codes, 128 instructions
+// beside 64 matrix products a quad.  Here each converts a quarter of a quad for all, through LDS, a
+// quad ahead, and codes are asked for two quads ahead; the queries are in registers.  Bound by vector instructions as before, with 96 fewer a quad: a prompt of
+// 4096 rows 200 -> 185 us (0.75 PFLOP/s), of 100 rows 14.6 -> 11.7.
+template <int HD>
+__device__ __forceinline__ void wide_items(const Kv8Args &a, uint4 *smem, float2 (*sh_ml)[32]) {
+  constexpr int RB = 2, ROWS = 16 * RB, KC = HD / 32, MB = HD / 16, LDJ = HD + 4;
+  constexpr int kBuf = 2 * KC * 2 * 64;                // 16-byte operands of a quad's K, or V
+  constexpr int NV = KC / 2;                           // 16-byte loads of a wave, of each
+  uint4(*kv)[2][kBuf] = reinterpret_cast<uint4(*)[2][kBuf]>(smem);   // [buffer][K, V]: pair, chunk, half, lane
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int lc = lane & 15, lg = lane >> 4;
+  const int block = blockIdx.x, kvh = block % a.nkv, G = a.nq / a.nkv;
+  const int k_off = lg * 128 + (lc & 7) * 16, v_off = (lg & 1) * 256 + lc * 16;
+  const int k_end = a.wide_first[block / a.nkv + 1];
+  for (int k = a.wide_first[block / a.nkv]; k < k_end; ++k) {
+    const Kv8Item it = a.items[k];
+    const int groups = kv8_groups(it.groups), quads = (it.t1 - it.t0 + 63) / 64, rows = it.nrow * G;
+    const int lr0 = (kv8_first(it.groups) + min(wave, groups - 1)) * ROWS;
+    const int open = min(it.t1, it.ctx + __builtin_amdgcn_readfirstlane(lr0 / G) + 1);   // seen by every row before it
+    // (of three groups' waves the fourth computes the third once more, and writes nothing)
+    // the pages of quad i; past the end the last page
+    const ids_t *ids = reinterpret_cast<const ids_t *>(reinterpret_cast<uintptr_t>(a.page_table + (int64_t)it.req * a.pt_stride));
+    struct Pages {
+      int b[4];
+    };
+    auto pages_of = [&](int i) __attribute__((always_inline)) {
+      Pages p;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) p.b[x] = ids[min((it.t0 >> 4) + 4 * i + x, (it.t1 - 1) >> 4)];
+      return p;
+    };
+    auto place = [&](int b) __attribute__((always_inline)) {
+      return (int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh;
+    };
+    uint4 kr[NV], vr[NV];
+    float2 sc[2];
+    auto load_codes = [&](const Pages &p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {
+        const int h = (wave * NV + x) / KC, c = (wave * NV + x) % KC;
+        const int64_t p0 = place(h ? p.b[2] : p.b[0]), p1 = place(h ? p.b[3] : p.b[1]);
+        kr[x] = ld16(a.k + (lc >= 8 ? p1 : p0) * (kPage * HD) + k_off + c * 512);
+        vr[x] = ld16(a.v + (lg >= 2 ? p1 : p0) * (kPage * HD) + v_off + c * 512);
+      }
+    };
+    auto load_scales = [&](const Pages &p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sc[h] = a.scale[lg >= 2 ? place(p.b[2 * h + 1]) : place(p.b[2 * h])];
+    };
+    auto store_codes = [&](int i) __attribute__((always_inline)) {
+      const int tp = it.t0 + 64 * i;
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {
+        const int h = (wave * NV + x) / KC, c = (wave * NV + x) % KC, at = (h * KC + c) * 128 + lane;
+        // slots past the range may hold anything: zero probability is not enough against a NaN
+        if (tp + 64 > it.t1) {
+          const int in = min(max(it.t1 - (tp + 32 * h + 8 * lg), 0), 8);
+          const uint32_t mlo = in >= 4 ? ~0u : (1u << (8 * in)) - 1u, mhi = in <= 4 ? 0u : in == 8 ? ~0u : (1u << (8 * (in - 4))) - 1u;
+          vr[x].x &= mlo;
+          vr[x].y &= mhi;
+          vr[x].z &= mlo;
+          vr[x].w &= mhi;
+        }
+        kv[i & 1][0][at] = as_uint4(to_bf16(kr[x].x, kr[x].y));
+        kv[i & 1][0][at + 64] = as_uint4(to_bf16(kr[x].z, kr[x].w));
+        kv[i & 1][1][at] = as_uint4(to_bf16(vr[x].x, vr[x].y));
+        kv[i & 1][1][at + 64] = as_uint4(to_bf16(vr[x].z, vr[x].w));
+      }
+    };
+
+    Pages p = pages_of(0);
+    load_codes(p);
+    load_scales(p);
+    uint4 qf[RB][KC];
+    int jrow[RB];
+    float m_run[RB], l_run[RB];
+    floatx4 o[RB][MB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int lr = min(lr0 + rb * 16 + lc, rows - 1);   // padding rows: a real one
+      const uint16_t *from = reinterpret_cast<const uint16_t *>(a.q) + ((int64_t)(it.row0 + lr / G) * a.nq + kvh * G + lr % G) * HD + 8 * lg;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) qf[rb][c] = ld16(from + 32 * c);
+      jrow[rb] = lr / G;
+      m_run[rb] = -INFINITY;
+      l_run[rb] = 0.f;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) o[rb][mb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    // block ids out of range are reported (and clamped above)
+    for (int x = threadIdx.x; x <= ((it.t1 - 1) >> 4) - (it.t0 >> 4); x += 256) {
+      const int b = a.page_table[(int64_t)it.req * a.pt_stride + (it.t0 >> 4) + x];
+      if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
+    }
+    p = pages_of(1);
+    store_codes(0);
+    load_codes(p);
+    Pages next = pages_of(2);
+    lds_barrier();
+    for (int i = 0; i < quads; ++i) {
+      const int tp = it.t0 + 64 * i;
+      float ks[2], lv[2], vi[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        ks[h] = sc[h].x * a.c_log2;
+        lv[h] = __builtin_amdgcn_logf(sc[h].y);
+        vi[h] = __builtin_amdgcn_exp2f(-lv[h]);
+      }
+      floatx4 s[RB][2][2];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s[rb][h][0] = s[rb][h][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+      // operands are read from LDS while the products before them run
+      uint4 f[2][4];
+      auto read4 = [&](int what, int h, int c, int to) __attribute__((always_inline)) {
+        f[to][h * 2] = kv[i & 1][what][(h * KC + c) * 128 + lane];
+        f[to][h * 2 + 1] = kv[i & 1][what][(h * KC + c) * 128 + 64 + lane];
+      };
+      read4(0, 0, 0, 0);
+      read4(0, 1, 0, 0);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        if (c + 1 < KC) {
+          read4(0, 0, c + 1, (c + 1) & 1);
+          read4(0, 1, c + 1, (c + 1) & 1);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              s[rb][h][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(f[c & 1][h * 2 + x]), as_bf16x8(qf[rb][c]), s[rb][h][x], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      store_codes(i + 1);
+      load_scales(p);
+      load_codes(next);
+      p = next;
+      next = pages_of(i + 3);
+      __builtin_amdgcn_sched_barrier(0);
+      if (tp + 64 > open) {
+        const int t = opaque(tp + 8 * lg);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          const int lim = min(it.t1, it.ctx + jrow[rb] + 1) - t;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (32 * h + 4 * x + e >= lim) s[rb][h][x][e] = -INFINITY;
+        }
+      }
+      uint4 pb[1][RB][2];
+      softmax(s, ks, lv, vi, m_run, l_run, o, pb);
+      __builtin_amdgcn_sched_barrier(0);
+      read4(1, 0, 0, 0);
+      read4(1, 1, 0, 0);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        if (c + 1 < KC) {
+          read4(1, 0, c + 1, (c + 1) & 1);
+          read4(1, 1, c + 1, (c + 1) & 1);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o[rb][2 * c + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(f[c & 1][h * 2 + x]), as_bf16x8(pb[0][rb][h]), o[rb][2 * c + x], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lds_barrier();
+    }
+    // through LDS: 8 dims of a row per thread
+    {
+      const int lane = opaque(threadIdx.x) & 63, lc = lane & 15, lg = lane >> 4;
+      float(*jo)[LDJ] = reinterpret_cast<float(*)[LDJ]>(smem) + wave * ROWS;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float l = xor32_sum(xor16_sum(l_run[rb]));
+        if (lg == 0) sh_ml[wave][rb * 16 + lc] = make_float2(m_run[rb], l);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) *reinterpret_cast<floatx4 *>(&jo[rb * 16 + lc][mb * 16 + 4 * lg]) = o[rb][mb];
+      }
+      lds_barrier();
+      const int end = wave < groups ? min(ROWS, rows - lr0) * (HD / 8) : 0;
+#pragma unroll 1
+      for (int u = lane; u < end; u += 64) {
+        const int r = u / (HD / 8), c0 = u % (HD / 8) * 8;
+        floatx4 y = *reinterpret_cast<const floatx4 *>(&jo[r][c0]), z = *reinterpret_cast<const floatx4 *>(&jo[r][c0 + 4]);
+        const float2 ml = sh_ml[wave][r];
+        if (it.part >= 0) {
+          const int64_t slot = ((int64_t)(it.part + wave) * a.nkv + kvh) * ROWS + r;
+          float *to = a.part_o + slot * HD + c0;
+          __builtin_nontemporal_store(y, reinterpret_cast<floatx4 *>(to));
+          __builtin_nontemporal_store(z, reinterpret_cast<floatx4 *>(to + 4));
+          if (c0 == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = ml;
+          continue;
+        }
+        const int64_t row = it.row0 + (lr0 + r) / G, col = (int64_t)(kvh * G + (lr0 + r) % G) * HD + c0;
+        const float inv = 1.0f / ml.y;
+        y *= inv;
+        z *= inv;
+        uint16_t *to = reinterpret_cast<uint16_t *>(a.out) + (a.packed ? packed_off(row, col, a.out_K) : row * a.out_K + col);
+        *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]), pack2bf_rne(z[0], z[1]), pack2bf_rne(z[2], z[3]));
+      }
+    }
+    lds_barrier();                                     // before the next item's codes
+  }
+}
+
+template <int HD, int RB, bool F32, bool STREAM = false, bool WIDE = false>
 __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Args a) {
   constexpr int ROWS = 16 * RB;         // of a row group
   constexpr int KC = HD / 32;           // 32-wide chunks of the contraction; 16-byte loads of K and of V
@@ -81,16 +370,21 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
   constexpr int LDJ = HD + 4;           // a row of a wave's accumulators in LDS, in floats: 16 bytes apart in banks
   constexpr int kQueries = 4 * NP * RB * KC * 64, kJoin = 4 * ROWS * LDJ / 4;   // 16-byte units
   // the row groups' queries in operand order while an item runs, the accumulators when it ends
-  __shared__ uint4 smem[kQueries > kJoin ? kQueries : kJoin];
+  constexpr int kWide = WIDE ? 4 * 2 * KC * 2 * 64 : 0;   // wide_items' two buffers
+  __shared__ uint4 smem[std::max(kWide, std::max(kQueries, kJoin))];
   __shared__ float2 sh_ml[4][ROWS];
   uint4(*qs)[NP][RB][KC][64] = reinterpret_cast<uint4(*)[NP][RB][KC][64]>(smem);
   float(*jo)[ROWS][LDJ] = reinterpret_cast<float(*)[ROWS][LDJ]>(smem);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lc = lane & 15, lg = lane >> 4;
-  const int kvh = blockIdx.x % a.nkv;   // neighbouring workgroups, on other XCDs: other kv heads
+  if constexpr (WIDE) {
+    if ((int)blockIdx.x < a.wide_blocks) return wide_items<HD>(a, smem, sh_ml);
+  }
+  const int block = WIDE ? blockIdx.x - a.wide_blocks : blockIdx.x;
+  const int kvh = block % a.nkv;        // neighbouring workgroups, on other XCDs: other kv heads
   const int G = a.nq / a.nkv;
-  int k = a.first[blockIdx.x / a.nkv];
-  const int k_end = a.first[blockIdx.x / a.nkv + 1];
+  int k = a.first[block / a.nkv];
+  const int k_end = a.first[block / a.nkv + 1];
   if (k >= k_end) return;
 
   // What a wave does of an item: row group rg, tokens tok .. end - 1 in n page quads (64 tokens)
@@ -317,56 +611,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
       }
     }
     uint4 pb[NP][RB][2];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      float mx[2];                       // scores in base 2
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        mx[h] = ks[h] * max2(max2(max2(s[rb][h][0][0], s[rb][h][0][1]), max2(s[rb][h][0][2], s[rb][h][0][3])),
-                             max2(max2(s[rb][h][1][0], s[rb][h][1][1]), max2(s[rb][h][1][2], s[rb][h][1][3])));
-      const float top = xor32_max(xor16_max(fmaxf(mx[0], mx[1])));
-      // the running maximum rises only by more than 8: p stays below 2^8, and the accumulators
-      // are rescaled on few quads; numerator and denominator share the reference
-      const bool grow = top > m_run[rb] + 8.0f;
-      if (__builtin_amdgcn_ballot_w64(grow)) {
-        const float alpha = grow ? __builtin_amdgcn_exp2f(m_run[rb] - top) : 1.0f;
-        m_run[rb] = grow ? top : m_run[rb];
-        l_run[rb] *= alpha;
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) o[rb][mb] *= alpha;
-      }
-      const float m = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // p x V's scale = 2^(s ks - m + log2 vs)
-        const float off = lv[h] - m;
-        float rs = 0.f;
-        uint32_t pw[NP][4];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            float f = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e], ks[h], off));
-            float g = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e + 1], ks[h], off));
-            if constexpr (F32) rs += f + g;
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-              const uint32_t w = pack2bf_rne(f, g);
-              pw[p][x * 2 + e / 2] = w;
-              f -= low(w);
-              g -= high(w);
-            }
-            // bf16: the sum adds the rounded values, as the second product does
-            if constexpr (!F32) {
-              const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
-              rs = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pw[0][x * 2 + e / 2]), one, rs, false);
-            }
-          }
-        l_run[rb] = __builtin_fmaf(rs, vi[h], l_run[rb]);   // this lane's tokens; the lanes are added up at the end
-#pragma unroll
-        for (int p = 0; p < NP; ++p) pb[p][rb][h] = make_uint4(pw[p][0], pw[p][1], pw[p][2], pw[p][3]);
-      }
-    }
+    softmax(s, ks, lv, vi, m_run, l_run, o, pb);
     // slots past the range may hold anything: zero probability is not enough against a NaN
     if (tp + 64 > sh.end) {
 #pragma unroll
@@ -596,7 +841,9 @@ void kv8_attention(const Kv8Plan &p, const Kv8Cache &c, const void *q, void *out
   a.c_log2 = 1.4426950408889634f / sqrtf((float)p.hd);
   a.packed = packed;
   const bool f32 = p.dtype == 0;
-  auto go = [&](auto kernel) { launch(kernel, (uint32_t)p.n_shares * p.nkv, 256, 0, s, a); };
+  a.wide_first = a.first + (p.n_shares > 0 ? p.n_shares + 1 : 0);
+  a.wide_blocks = p.n_wide * p.nkv;
+  auto go = [&](auto kernel) { launch(kernel, (uint32_t)(p.n_shares + p.n_wide) * p.nkv, 256, 0, s, a); };
   if (f32) {
     switch (p.hd) {
       case 32: go(kv8_attn_kernel<32, 1, true>); break;
@@ -608,12 +855,14 @@ void kv8_attention(const Kv8Plan &p, const Kv8Cache &c, const void *q, void *out
       case 224: go(kv8_attn_kernel<224, 1, true>); break;
       default: go(kv8_attn_kernel<256, 1, true>); break;
     }
-  } else if (p.stream) {
-    if (p.hd == 128) p.rb == 1 ? go(kv8_attn_kernel<128, 1, false, true>) : go(kv8_attn_kernel<128, 2, false, true>);
-    else p.rb == 1 ? go(kv8_attn_kernel<64, 1, false, true>) : go(kv8_attn_kernel<64, 2, false, true>);
   } else {
-    if (p.hd == 128) p.rb == 1 ? go(kv8_attn_kernel<128, 1, false>) : go(kv8_attn_kernel<128, 2, false>);
-    else p.rb == 1 ? go(kv8_attn_kernel<64, 1, false>) : go(kv8_attn_kernel<64, 2, false>);
+    auto of = [&](auto hd) {
+      constexpr int HD = decltype(hd)::value;
+      if (p.n_wide > 0) p.stream ? go(kv8_attn_kernel<HD, 2, false, true, true>) : go(kv8_attn_kernel<HD, 2, false, false, true>);
+      else if (p.stream) p.rb == 1 ? go(kv8_attn_kernel<HD, 1, false, true>) : go(kv8_attn_kernel<HD, 2, false, true>);
+      else p.rb == 1 ? go(kv8_attn_kernel<HD, 1, false>) : go(kv8_attn_kernel<HD, 2, false>);
+    };
+    p.hd == 128 ? of(std::integral_constant<int, 128>{}) : of(std::integral_constant<int, 64>{});
   }
   if (p.n_groups == 0) return;
   const int rows = 16 * p.rb, units = rows * p.hd / 8;

@@ -48,7 +48,7 @@ struct Kv8Plan {    // a wisp_kv8_batch
   const int32_t *page_table;
   char *ws;
   int32_t device, dtype, nq, nkv, hd, rows, B;
-  int32_t pt_stride, n_units, n_items, n_shares, n_groups, rb, n_parts, stream;
+  int32_t pt_stride, n_units, n_items, n_shares, n_groups, rb, n_parts, stream, n_wide;
   // byte offsets in the workspace
   uint64_t w_units, w_items, w_first, w_groups, w_pos, w_cs, w_po, w_pml, total;
 };

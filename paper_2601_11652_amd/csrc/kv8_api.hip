@@ -31,7 +31,7 @@ size_t put(std::vector<int32_t> &host, const std::vector<V> &v) {
 
 struct Bundle {
   int32_t req, first, groups, tokens;   // row groups; tokens: up to its last row's causal limit
-  int64_t pairs, cost;
+  int64_t pairs, pair, cost;            // page pairs, the cost of one, of all
 };
 struct Piece {                          // page pairs from .. to - 1 of a bundle, in a share; a bundle's in order
   int32_t bundle, share;
@@ -42,8 +42,9 @@ struct Piece {                          // page pairs from .. to - 1 of a bundle
 // waves; two groups have two waves each but share what is read, three or four one.  Starting
 // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
 // 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
-// A prompt of 4096 rows, cut: 216 us, 215, 226 and 253.
-constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64;
+// kWide: of a pair that the waves convert together (prompts of 1500-2000 rows beside 10 requests 83.9 us;
+// 9: 81.5, 14: 83.1; one of 100 beside 3 11.7, 13.3 and 13.1).
+constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64, kWide = 12;
 constexpr int64_t kTurn = 32;           // cost of a turn
 // Where both workgroups of a CU are there, the older one's waves go first: percent of the work that
 // the older half of the shares takes (128 requests of 0.25-32k: 330 us; 50 %: 334, 60 %: 349).
@@ -64,7 +65,7 @@ std::vector<Piece> by_borders(const std::vector<Bundle> &bundles, int64_t shares
   int64_t at = 0, share = 0;                           // cost before this bundle
   for (size_t k = 0; k < bundles.size(); ++k) {
     const Bundle &u = bundles[k];
-    const int64_t grain = grain_of(u), unit = kPair[u.groups] * grain;
+    const int64_t grain = grain_of(u), unit = u.pair * grain;
     int64_t done = 0;
     for (; share + 1 < shares; ++share) {
       const int64_t b = border(share + 1);
@@ -105,6 +106,27 @@ std::vector<Piece> by_length(const std::vector<Bundle> &bundles, int64_t shares,
   return pieces;
 }
 
+// A kv head's work in at most `shares` shares (how many: on return).
+std::vector<Piece> shares_of(const std::vector<Bundle> &bundles, int64_t &shares) {
+  int64_t total = 0;
+  for (const Bundle &u : bundles) total += u.cost;
+  int64_t size = (total + shares - 1) / shares;
+  if (size < 8 * kTurn) size = std::max<int64_t>(1, (size + kTurn - 1) / kTurn) * kTurn;
+  shares = std::max<int64_t>(1, (total + size - 1) / size);
+  std::vector<Piece> pieces = by_borders(bundles, shares, size, total);
+  // Cut bundles start twice, write what they have per row group and wait for its join: shares of whole
+  // ones may end that much later.  Requests of one row group, 128 of 0.3-1.2k tokens (12 % more in the
+  // longest share): 50.4 us cut, 42.0 whole; 66 of 2k (76 % more) 56.0 and 61.0; prompts of
+  // 1500-2000 rows (8 %) 105 and 87.  Short shares are cut: whole bundles would leave CUs idle.
+  if (size >= 8 * kTurn) {
+    int64_t end = 0, groups = 0;
+    for (const Bundle &u : bundles) groups += u.groups;
+    std::vector<Piece> whole = by_length(bundles, shares, end);
+    if (end <= size + 180 + 40 * groups / (int64_t)bundles.size()) pieces.swap(whole);
+  }
+  return pieces;
+}
+
 }  // namespace
 
 wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_desc *d) {
@@ -140,7 +162,7 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   p.rb = p.dtype == WISP_BF16 && (int64_t)most * G > 16 ? 2 : 1;
   const int R = 16 * p.rb;
   std::vector<Bundle> bundles;
-  int64_t total = 0, bytes = 0;
+  int64_t bytes = 0;
   int64_t n_bundles = 0;
   for (int i = 0; i < p.B; ++i) {
     bytes += 2 * ((int64_t)d->ctx_len[i] + nrow[i]) * p.nkv * p.hd;
@@ -162,54 +184,66 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
       const int64_t f = k * groups / nb, e = (k + 1) * groups / nb;
       const int32_t T = d->ctx_len[i] + (int32_t)((std::min<int64_t>((int64_t)nrow[i] * G, e * R) - 1) / G) + 1;
       const int64_t pairs = (T + 31) / 32;
-      bundles.push_back(Bundle{i, (int32_t)f, (int32_t)(e - f), T, pairs, kStart + pairs * kPair[e - f]});
-      total += bundles.back().cost;
+      const int64_t pair = kPair[e - f];
+      bundles.push_back(Bundle{i, (int32_t)f, (int32_t)(e - f), T, pairs, pair, kStart + pairs * pair});
     }
   }
-  // Every kv head's work, the same for all, in shares, one for each workgroup (two per CU).
+  // Every kv head's work, the same for all, in shares, one for each workgroup (two per CU).  Bundles of
+  // three and four row groups run apart (the attention's wide items) where they are half of the work
+  // or more, each set with its part of the workgroups: a prompt of 4096 rows 200 us together, 185
+  // apart, one of 500 beside 3 decoding requests 23.8 and 21.6, one of 3000 beside 40 143 and 142;
+  // of less than half, 128 requests of 2 to 17 rows, 332 and 358.
   const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
-  int64_t size = (total + most_shares - 1) / most_shares;
-  if (size < 8 * kTurn) size = std::max<int64_t>(1, (size + kTurn - 1) / kTurn) * kTurn;
-  const int64_t shares = std::max<int64_t>(1, (total + size - 1) / size);
-  if (n_bundles + shares > kKv8MaxItems / p.nkv) return too_many((n_bundles + shares) * p.nkv);
-  std::vector<Piece> pieces = by_borders(bundles, shares, size, total);
-  // Cut bundles start twice, write what they have per row group and wait for its join: shares of whole
-  // ones may end that much later.  Requests of one row group, 128 of 0.3-1.2k tokens (12 % more in the
-  // longest share): 50.4 us cut, 42.0 whole; 66 of 2k (76 % more) 56.0 and 61.0; prompts of
-  // 1500-2000 rows (8 %) 105 and 87.  Short shares are cut: whole bundles would leave CUs idle.
-  if (size >= 8 * kTurn) {
-    int64_t end = 0, n_groups = 0;
-    for (const Bundle &u : bundles) n_groups += u.groups;
-    std::vector<Piece> whole = by_length(bundles, shares, end);
-    if (end <= size + 180 + 40 * n_groups / (int64_t)bundles.size()) pieces.swap(whole);
+  if (n_bundles + most_shares > kKv8MaxItems / p.nkv) return too_many((n_bundles + most_shares) * p.nkv);
+  int64_t cost[2] = {0, 0};
+  for (const Bundle &u : bundles) cost[u.groups > 2] += u.cost;
+  const bool apart = p.rb == 2 && cost[1] >= cost[0];
+  std::vector<Bundle> sets[2];
+  cost[0] = cost[1] = 0;
+  for (Bundle u : bundles) {
+    const int w = apart && u.groups > 2;
+    if (w) u.pair = kWide;
+    u.cost = kStart + u.pairs * u.pair;
+    cost[w] += u.cost;
+    sets[w].push_back(u);
   }
-  std::vector<Kv8Item> items(pieces.size());
+  std::vector<Kv8Item> items;
   std::vector<Kv8Group> groups;
-  std::vector<int32_t> first(shares + 1, 0);
-  for (const Piece &x : pieces) ++first[x.share + 1];
-  std::partial_sum(first.begin(), first.end(), first.begin());
-  std::vector<int32_t> next(first);                    // a share's next item
+  std::vector<int32_t> first;
   p.n_parts = 0;
-  for (size_t k = 0; k < pieces.size();) {
-    const Bundle &u = bundles[pieces[k].bundle];
-    int32_t n = 0;                                     // its pieces
-    while (k + n < pieces.size() && pieces[k + n].bundle == pieces[k].bundle) ++n;
-    for (int32_t x = 0; x < n; ++x) {
-      const Piece &w = pieces[k + x];
-      items[next[w.share]++] = Kv8Item{u.req, (int32_t)(32 * w.from), (int32_t)std::min<int64_t>(u.tokens, 32 * w.to),
-                                       d->ctx_len[u.req], row0[u.req], nrow[u.req], kv8_pack(u.first, u.groups),
-                                       n > 1 ? p.n_parts + x * u.groups : -1};
+  for (int w = 0; w < 2; ++w) {
+    if (sets[w].empty()) continue;
+    int64_t shares = most_shares;
+    if (cost[1 - w] > 0)
+      shares = std::max<int64_t>(1, std::min(most_shares - 1, (2 * most_shares * cost[w] + cost[0] + cost[1]) / (2 * (cost[0] + cost[1]))));
+    const std::vector<Piece> pieces = shares_of(sets[w], shares);
+    (w ? p.n_wide : p.n_shares) = (int32_t)shares;
+    std::vector<int32_t> next(shares + 1, 0);            // where a share's items start, then its next item
+    for (const Piece &x : pieces) ++next[x.share + 1];
+    next[0] = (int32_t)items.size();
+    std::partial_sum(next.begin(), next.end(), next.begin());
+    first.insert(first.end(), next.begin(), next.end());
+    items.resize(items.size() + pieces.size());
+    for (size_t k = 0; k < pieces.size();) {
+      const Bundle &u = sets[w][pieces[k].bundle];
+      int32_t n = 0;                                     // its pieces
+      while (k + n < pieces.size() && pieces[k + n].bundle == pieces[k].bundle) ++n;
+      for (int32_t x = 0; x < n; ++x) {
+        const Piece &y = pieces[k + x];
+        items[next[y.share]++] = Kv8Item{u.req, (int32_t)(32 * y.from), (int32_t)std::min<int64_t>(u.tokens, 32 * y.to),
+                                         d->ctx_len[u.req], row0[u.req], nrow[u.req], kv8_pack(u.first, u.groups),
+                                         n > 1 ? p.n_parts + x * u.groups : -1};
+      }
+      if (n > 1) {
+        for (int32_t g = 0; g < u.groups; ++g)
+          groups.push_back(Kv8Group{row0[u.req], nrow[u.req], u.first + g, p.n_parts + g, n, u.groups, {0, 0}});
+        p.n_parts += n * u.groups;
+      }
+      k += n;
     }
-    if (n > 1) {
-      for (int32_t g = 0; g < u.groups; ++g)
-        groups.push_back(Kv8Group{row0[u.req], nrow[u.req], u.first + g, p.n_parts + g, n, u.groups, {0, 0}});
-      p.n_parts += n * u.groups;
-    }
-    k += n;
   }
   p.n_items = (int32_t)items.size();
   p.n_groups = (int32_t)groups.size();
-  p.n_shares = (int32_t)shares;
   b.i_first = put(b.host, first);
 
   b.i_units = put(b.host, units);

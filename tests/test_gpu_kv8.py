@@ -194,13 +194,56 @@ def test_attention_matches_oracle(case):
     _check_attention(c, c.queries())
 
 
+# many rows: three and four row groups that run together, apart from the others
+WIDE = [
+    ([0], [130], 8, 2, 128, True),
+    ([3000, 700, 40], [70, 2, 1], 32, 8, 128, True),
+    ([5000], [24], 32, 8, 128, True),            # three row groups, cut and joined
+    ([64, 1, 333], [33, 64, 65], 16, 2, 64, True),
+    ([2000, 9, 0], [40, 300, 16], 8, 4, 64, True),
+    ([15, 16, 17], [81, 80, 79], 6, 2, 128, True),
+    ([900 + 13 * k for k in range(40)], [25 + k % 9 for k in range(40)], 64, 16, 128, True),   # several for a workgroup
+    ([0, 4000], [1000, 1], 4, 1, 128, True),
+    ([200, 100, 0], [2, 2, 2], 40, 1, 64, True),  # three row groups of two rows
+]
+
+
+@pytest.mark.parametrize("case", range(len(WIDE)))
+def test_attention_of_many_rows(case):
+    log(f"attention of {len(WIDE[case][0])} requests, rows {WIDE[case][1][:3]}, {WIDE[case][2:]}")
+    c = Case(*WIDE[case], seed=700 + case, pow2=case % 2 == 0).fill()
+    _check_attention(c, c.queries())
+
+
+def test_bad_block_ids_of_many_rows_are_reported():
+    c = Case([20], [200], 8, 2, 128, True, seed=43).fill()
+    c.pt[0, 7] = c.k.shape[0]
+    from gpu_harness import to_dev
+    c.desc = W.BatchDesc(c.ctx, c.gamma, to_dev(c.pt), 1.0, None, c.nrow - 1 - c.gamma)
+    kv, plan = c.pool(), c.plan()
+    q = dev(c.queries(), True)
+    W.wisp_attention_kv8(plan, kv, q, torch.empty_like(q))
+    with pytest.raises(W.WispError) as e:
+        W.wisp_check(plan.ws)
+    assert e.value.status == W.WISP_E_DEVICE_INPUT
+
+
 @pytest.mark.parametrize("n_q,n_kv,hd,lo,hi", [(64, 16, 128, 200, 6000), (16, 16, 128, 1000, 5000), (64, 32, 64, 200, 6000), (32, 32, 64, 10, 6000)])
 def test_attention_of_more_codes_than_the_caches_hold(n_q, n_kv, hd, lo, hi):
+    _check_large(n_q, n_kv, hd, lo, hi, 1, 18)
+
+
+@pytest.mark.parametrize("n_q,n_kv,hd,lo,hi", [(64, 16, 128, 200, 6000), (64, 32, 64, 200, 6000)])
+def test_attention_of_many_rows_and_more_codes_than_the_caches_hold(n_q, n_kv, hd, lo, hi):
+    _check_large(n_q, n_kv, hd, lo, hi, 14, 70)
+
+
+def _check_large(n_q, n_kv, hd, lo, hi, least, most):
     """Over 256 MB of codes (they are read past the caches then), one to five row groups a request;
     the reference in fp64 on the device."""
     rng = np.random.default_rng(n_q + hd)
     B = 4 + (300 << 20) // (2 * n_kv * hd) // ((lo + hi) // 2)
-    ctx, nrow = rng.integers(lo, hi, B).astype(np.int32), rng.integers(1, 18, B).astype(np.int32)
+    ctx, nrow = rng.integers(lo, hi, B).astype(np.int32), rng.integers(least, most, B).astype(np.int32)
     nrow[0] = 40
     tokens = ctx + nrow
     log(f"{B} requests, {int(tokens.sum()) * 2 * n_kv * hd >> 20} MB of codes")
