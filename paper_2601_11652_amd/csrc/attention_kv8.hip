@@ -4,7 +4,8 @@
 // A workgroup of four waves runs a share of one kv head's work, items one after another: an item is
 // up to four row groups (16 RB of a request's rows x query heads each) over a range of the request's
 // tokens.  One row group's tokens are split over the four waves, two row groups have two waves
-// each, three or four one each: waves that share tokens read the same lines at the same time.  Per
+// each, three or four one each: waves that share tokens read the same lines at the same time, and
+// bundles of three and four that run apart (wide_items) also convert their codes together.  Per
 // page pair (32 tokens) a wave computes S^T = K Q^T and O^T += V^T P^T with 16x16x32 matrix products in
 // bf16, which holds every e4m3 value exactly: the codes are converted between load and product,
 // the K scale multiplies the scores and the V scale the probabilities (a lane's eight tokens of
