@@ -400,6 +400,33 @@ def test_two_plans_on_two_streams():
         assert torch.equal(a, b)
 
 
+def test_pages_beyond_4_gib_of_pool():
+    """The same batch in a small pool and at the end of one of 4.6 GB: the same results, bit for bit."""
+    from gpu_harness import to_dev
+    c = Case([900, 0, 33], [6, 150, 3], 32, 8, 128, True, seed=91)
+    nb, n_big = c.k.shape[0], 280000
+    assert n_big * 8 * 2048 > 1 << 32
+    small, big = c.pool(), W.KV8Pool.zeros(1, n_big, 8, 128)
+    for b, a in ((big.k, small.k), (big.v, small.v)):
+        b.view(torch.uint8)[0, n_big - nb:] = a.view(torch.uint8)[0]
+    big.scale[0, n_big - nb:] = small.scale[0]
+    x = dev(c.qkv(), True)
+    out = []
+    for kv, shift in ((small, 0), (big, n_big - nb)):
+        pt = np.where(c.pt >= 0, c.pt + shift, -1).astype(np.int32)
+        d = W.BatchDesc(c.ctx, c.gamma, to_dev(pt), 1.0, None, c.nrow - 1 - c.gamma)
+        plan = W.wisp_kv8_plan(c.model, d, W.workspace(W.wisp_kv8_workspace_size(c.model, d)))
+        q = torch.empty(c.M, 32, 128, dtype=torch.bfloat16, device="cuda")
+        o = torch.empty_like(q)
+        W.wisp_kv8_append(plan, kv, x, q)
+        W.wisp_attention_kv8(plan, kv, q, o)
+        W.wisp_check(plan.ws)
+        out.append((q, o, kv.k.view(torch.uint8)[0, shift:shift + nb], kv.v.view(torch.uint8)[0, shift:shift + nb]))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert int(big.k.view(torch.uint8)[0, :nb].max()) == 0
+
+
 def test_wrapper_refuses_tensors_that_do_not_fit():
     c = Case([40, 20], [3, 3], 8, 2, 64, True, seed=71).fill()
     kv, plan = c.pool(), c.plan()

@@ -205,6 +205,23 @@ def test_more_rows_than_a_launch_has_threads_for():
 
 
 @pytest.mark.gpu
+def test_logits_beyond_2_31_entries():
+    """The last rows of 8.6 GB of logits: as by themselves, bit for bit."""
+    rows, V, k = 16900, 128256, 3
+    assert (rows - k) * V > 1 << 31
+    x = torch.zeros(rows, V, device="cuda")
+    tail, tok = _logits(k, V, torch.float32, 12)
+    x[-k:] = tail
+    all_tok = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    all_tok[-k:] = tok
+    got, ws = _run(x, V, all_tok, 1.0, 5)
+    W.wisp_check(ws)
+    alone, _ = _run(tail, V, tok, 1.0, 5)
+    for a, b in zip(got, alone):
+        assert torch.equal(a[-k:], b) and (a[:-k] == 7).all()
+
+
+@pytest.mark.gpu
 def test_captured_replayed_and_on_two_streams():
     x, tok = _logits(20, 40000, torch.float32, 8)
     rows, V, top = 20, 40000, 6
