@@ -282,6 +282,19 @@ def _raw_stream(torch):
     return _raw
 
 
+def _scratch(nbytes: int, device, stream):
+    """workspace() for a call on `stream` that nobody keeps afterwards: made and cleared on that
+    stream, so that torch's allocator hands the memory on only behind the call's kernels."""
+    import torch
+    if stream is None:
+        return workspace(nbytes, device)
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = _stream(stream)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return workspace(nbytes, device)
+
+
 # ------------------------------------------------------------------------------------------
 # struct builders
 # ------------------------------------------------------------------------------------------
@@ -664,7 +677,8 @@ def wisp_token_logprobs(logits, vocab: int, tokens, temperature: float, logprob,
     tokens (top_tokens int32, top_logprobs fp32, both [rows][n_top]) of logits rows [rows][ld],
     fp32 or bf16, of which the first `vocab` entries of a row count.  tokens, logprob, entropy and
     the top outputs may be None.  `ws` (a device byte tensor of wisp_token_logprobs_workspace_size bytes,
-    as workspace() makes it) is allocated when not given."""
+    as workspace() makes it) is allocated when not given; only a given one can tell wisp_check of tokens
+    out of range (their logprob is NaN either way)."""
     import torch
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or logits.shape[1] < vocab:
         raise ValueError(f"logits: expected [rows][>= {vocab}] with unit column stride")
@@ -687,7 +701,7 @@ def wisp_token_logprobs(logits, vocab: int, tokens, temperature: float, logprob,
     pi = None if top_tokens is None else _dev(top_tokens, "top_tokens", dtype=i32)
     pv = None if top_logprobs is None else _dev(top_logprobs, "top_logprobs", dtype=f32)
     if ws is None:
-        ws = workspace(wisp_token_logprobs_workspace_size(rows, vocab, n_top), logits.device)
+        ws = _scratch(wisp_token_logprobs_workspace_size(rows, vocab, n_top), logits.device, stream)
     on = logits.get_device()
     for t in (tokens, logprob, entropy, top_tokens, top_logprobs, ws):
         if t is not None and t.get_device() != on:

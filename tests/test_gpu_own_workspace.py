@@ -1,0 +1,39 @@
+"""Calls that make their own workspace on a stream beside torch's current one, which goes on allocating
+and writing memory meanwhile."""
+import pytest
+import torch
+
+import paper_2601_11652_amd as W
+from gpu_harness import log
+
+pytestmark = pytest.mark.gpu
+
+
+def _churn(nbytes):
+    """What the current stream does next: memory of about the workspace's size, written over."""
+    for k in range(8):
+        torch.full((nbytes // 4 + 64 * k,), float("nan"), device="cuda")
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+def test_token_logprobs_on_another_stream(raw):
+    rows, V, top = 64, 50000, 8
+    n = W.wisp_token_logprobs_workspace_size(rows, V, top)
+    side = torch.cuda.Stream()
+    for step in range(6):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(step)
+        x = torch.randn(rows, V, device="cuda", generator=g)
+        tok = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32, generator=g)
+        outs = lambda: (torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"),
+                        torch.zeros(rows, top, dtype=torch.int32, device="cuda"), torch.zeros(rows, top, device="cuda"))
+        a, b = outs(), outs()
+        W.wisp_token_logprobs(x, V, tok, 1.0, *a, W.workspace(n))
+        torch.cuda.synchronize()
+        _churn(n)                                   # in flight when the call is made
+        W.wisp_token_logprobs(x, V, tok, 1.0, *b, None, side.cuda_stream if raw else side)
+        _churn(n)
+        torch.cuda.synchronize()
+        log(f"token log probabilities, step {step}")
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
