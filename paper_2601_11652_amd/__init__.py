@@ -662,7 +662,7 @@ def wisp_draft_stats(logits, vocab: int, temperature: float, stats, ws=None, str
     if logits.dim() != 2 or logits.stride(1) != 1 or logits.shape[1] < vocab:
         raise ValueError(f"logits: expected [rows][>= {vocab}] with unit column stride")
     if ws is None:
-        ws = workspace(lib.wisp_draft_stats_workspace_size(rows, vocab))
+        ws = _scratch(lib.wisp_draft_stats_workspace_size(rows, vocab), logits.device, stream)
     _ok(lib.wisp_draft_stats(_dev(logits, "logits", dtype=_f32(), contiguous=False), rows, vocab, logits.stride(0),
                              temperature, _dev(stats, "stats", rows * 4, dtype=_f32()), *_ws(ws), _stream(stream)))
 

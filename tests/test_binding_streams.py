@@ -16,3 +16,12 @@ def test_token_logprobs_makes_its_workspace_on_its_stream(monkeypatch, stream, h
     name, args = c.calls[-1]
     assert name == "wisp_token_logprobs" and args[-1] == handle
     assert c.made == [(4096, handle)] and c.current == 1
+
+
+@pytest.mark.parametrize("stream,handle", STREAMS)
+def test_draft_stats_makes_its_workspace_on_its_stream(monkeypatch, stream, handle):
+    c = Calls(monkeypatch)
+    W.wisp_draft_stats(fake(3, 100), 100, 1.0, fake(3, 4), stream=stream)
+    name, args = c.calls[-1]
+    assert name == "wisp_draft_stats" and args[-1] == handle
+    assert c.made == [(4096, handle)] and c.current == 1

@@ -37,3 +37,23 @@ def test_token_logprobs_on_another_stream(raw):
         log(f"token log probabilities, step {step}")
         for p, q in zip(a, b):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+def test_draft_stats_on_another_stream(raw):
+    rows, V = 64, 50000
+    n = int(W.lib.wisp_draft_stats_workspace_size(rows, V))
+    side = torch.cuda.Stream()
+    for step in range(6):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(step)
+        x = torch.randn(rows, V, device="cuda", generator=g)
+        a, b = torch.zeros(rows, 4, device="cuda"), torch.zeros(rows, 4, device="cuda")
+        W.wisp_draft_stats(x, V, 1.0, a, W.workspace(n))
+        torch.cuda.synchronize()
+        _churn(n)
+        W.wisp_draft_stats(x, V, 1.0, b, None, side.cuda_stream if raw else side)
+        _churn(n)
+        torch.cuda.synchronize()
+        log(f"draft statistics, step {step}")
+        assert torch.equal(a, b)
