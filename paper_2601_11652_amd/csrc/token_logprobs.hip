@@ -227,8 +227,8 @@ __global__ __launch_bounds__(kThreads + 64) void logprobs_row_kernel(const T *__
     const double lse = log(s);
     const bool none = s == 0.0;                // every logit is -inf
     if (lane == 0) {
+      if (tokens && !tok_ok) flag_error(err, kErrToken);
       if (logprob) {
-        if (!tok_ok) flag_error(err, kErrToken);
         logprob[row] = !tok_ok || s != s                ? NAN
                        : none || xt == -INFINITY ? -INFINITY
                                                  : (float)(((double)xt - mw) / temperature - lse);
