@@ -28,6 +28,10 @@ constexpr int kChunk = 8192, kThreads = 256, kGroup = kChunk / kThreads;
 constexpr int kMaxChunks = 1 << 23;   // of a launch
 constexpr float kLog2e = 1.4426950408889634f;
 
+// log2(e) / T, finite: of a T below 4.3e-39 the quotient is infinite, and its product with the
+// maximum's difference, 0, would be NaN
+__host__ __device__ inline float scale_of(float T) { return fminf(kLog2e / T, 3.402823466e38f); }
+
 struct Part {   // of one chunk: the maximum, and the sums about it (0 where nothing is above -inf)
   double s, c;
   float m, pad;
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(kThreads + 64) void logprobs_row_kernel(const T *__
     // the chunks joined: a lane's in order, then the lanes
     const bool tok_ok = tok >= 0 && tok < V;
     const float xt = tok_ok ? logit(x, tok) : 0.f;
-    const float sc = kLog2e / temperature;
+    const float sc = scale_of(temperature);
     float m = -INFINITY;
     double s = 0.0, cs = 0.0;
     for (int c = lane; c < nch; c += 64) {
@@ -430,7 +434,7 @@ extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, in
     float *gmax = n_top ? reinterpret_cast<float *>(ws + 256 + align256((size_t)rows * nch * sizeof(Part))) : nullptr;
     int *err = reinterpret_cast<int *>(ws);
     const hipStream_t s = (hipStream_t)stream;
-    const float sc = kLog2e / temperature;
+    const float sc = scale_of(temperature);
     // a launch has less than 2^32 threads: this many rows each (at least 64)
     const int32_t step = kMaxChunks / nch;
     auto go = [&](auto *x, auto chunk, auto row) {
