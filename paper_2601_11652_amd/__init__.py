@@ -626,8 +626,9 @@ def wisp_verify_kv8(model: wisp_model, kv: KV8Pool, desc: BatchDesc, tokens, dra
     args = (_dev(tokens, "tokens", desc.rows, dtype=_i32()), probs, rng_seed & ((1 << 64) - 1),
             _dev(accept_len, "accept_len", desc.B, dtype=_i32()), _dev(out_tokens, "out_tokens", desc.M, dtype=_i32()),
             logits, *_ws(workspace))
-    for t in (tokens, accept_len, out_tokens, workspace):
-        if t.device != kv.device:
+    for t in (tokens, draft_probs if desc.S > 0 else None, accept_len, out_tokens, target_logits, workspace,
+              desc.page_table if desc.B > 0 else None):
+        if t is not None and t.device != kv.device:
             raise ValueError(f"a tensor on {t.device}, kv on {kv.device}")
     with _On(kv.device):
         _ok(lib.wisp_verify_kv8(C.byref(model), C.byref(kv.c), C.byref(desc.c), *args, _stream(stream)))
