@@ -18,6 +18,7 @@
 #include "host_guard.h"
 #include "kernels.h"
 #include "kv8_plan.h"
+#include "staging.h"
 
 using namespace wisp;
 
@@ -622,41 +623,13 @@ bool wisp::launch_timing_events(hipEvent_t *start, hipEvent_t *stop) {
 }
 
 namespace {
-
-// pinned staging for the descriptor upload, reused once the previous copy has finished
-struct Staging {
-  void *buf = nullptr;
-  size_t cap = 0;
-  hipEvent_t ev = nullptr;
-  bool pending = false;
-};
-thread_local Staging g_stage;
+thread_local Staging g_stage;   // of the descriptor uploads
 }  // namespace
 
 wisp_status wisp::upload_ints(const std::vector<int32_t> &host, void *dst, hipStream_t s) {
-  const size_t bytes = host.size() * sizeof(int32_t);
-  if (bytes == 0) return WISP_OK;
-  if (g_stage.pending) {
-    if (hipEventSynchronize(g_stage.ev) != hipSuccess) return fail(WISP_E_HIP, "staging event sync failed");
-    g_stage.pending = false;
-  }
-  if (g_stage.cap < bytes) {
-    if (g_stage.buf) (void)hipHostFree(g_stage.buf);
-    g_stage.buf = nullptr;
-    g_stage.cap = 0;
-    size_t cap = std::max<size_t>(bytes, 1 << 16);
-    if (hipHostMalloc(&g_stage.buf, cap, hipHostMallocDefault) != hipSuccess)
-      return fail(WISP_E_HIP, "pinned staging allocation failed");
-    g_stage.cap = cap;
-  }
-  if (!g_stage.ev && hipEventCreateWithFlags(&g_stage.ev, hipEventDisableTiming) != hipSuccess)
-    return fail(WISP_E_HIP, "event creation failed");
-  std::memcpy(g_stage.buf, host.data(), bytes);
-  if (hipMemcpyAsync(dst, g_stage.buf, bytes, hipMemcpyHostToDevice, s) != hipSuccess)
-    return fail(WISP_E_HIP, "descriptor upload failed");
-  if (hipEventRecord(g_stage.ev, s) != hipSuccess) return fail(WISP_E_HIP, "event record failed");
-  g_stage.pending = true;
-  return WISP_OK;
+  if (host.empty()) return WISP_OK;
+  const char *what = g_stage.upload(host.data(), host.size() * sizeof(int32_t), dst, s);
+  return what ? fail(WISP_E_HIP, "%s", what) : WISP_OK;
 }
 
 wisp_status wisp::hip_check(const char *what) {
