@@ -57,14 +57,14 @@ struct Plan {
   std::vector<int32_t> host;         // descriptor block uploaded to the device
   // int32 offsets inside the descriptor block
   size_t i_off = 0, i_doff = 0, i_gamma = 0, i_ctx = 0, i_req = 0, i_row_req = 0, i_row_pos = 0,
-         i_items = 0, i_groups = 0, i_first = 0, i_voff = 0, i_nrow = 0, i_vrow = 0;
+         i_items = 0, i_groups = 0, i_first = 0, i_voff = 0, i_nrow = 0, i_vrow = 0, i_kv8 = 0;
   // byte offsets inside the workspace
   size_t w_err = 0, w_desc = 0, w_rope = 0, w_h = 0, w_xn = 0, w_ao = 0, w_af = 0, w_q = 0,
          w_part = 0, w_attn_o = 0, w_attn_ml = 0, w_sm = 0, w_si = 0, w_ss = 0, w_rk = 0, w_ri = 0,
          w_rR = 0, w_vtok = 0, total = 0;
   int max_group_chunks = 0;          // most chunks any attention group combines
   int race_chunk = 0;                // vocabulary entries per workgroup of the acceptance's race
-  bool kv8 = false;                  // the step runs on the 8-bit cache, which has a plan of its own
+  const Kv8Build *kv8 = nullptr;     // the 8-bit cache's own plan, of a step that runs on one
 };
 
 
@@ -480,6 +480,7 @@ void lay_out(Plan &p, const wisp_batch_desc *d, bool forward, const std::vector<
   take(p.i_voff, p.B + 1);
   take(p.i_nrow, p.B);
   take(p.i_vrow, p.Mv);
+  take(p.i_kv8, p.kv8 ? p.kv8->host.size() : 0);
   p.host.assign(n, 0);
   for (int i = 0; i <= p.B; ++i) {
     p.host[p.i_off + i] = off[i];
@@ -500,6 +501,7 @@ void lay_out(Plan &p, const wisp_batch_desc *d, bool forward, const std::vector<
   if (!p.items.empty()) std::memcpy(&p.host[p.i_items], p.items.data(), p.items.size() * sizeof(AttnItem));
   std::copy(p.first.begin(), p.first.end(), p.host.begin() + p.i_first);
   if (!p.groups.empty()) std::memcpy(&p.host[p.i_groups], p.groups.data(), p.groups.size() * sizeof(AttnGroup));
+  if (p.kv8) std::copy(p.kv8->host.begin(), p.kv8->host.end(), p.host.begin() + p.i_kv8);
 
   // workspace
   size_t w = 0;
@@ -848,16 +850,9 @@ wisp_status plan_verify(Plan &p, const wisp_model *model, const wisp_batch_desc 
 // lists travel in the step's descriptor block and whose partial results follow its workspace.
 wisp_status plan_kv8_step(Plan &p, Kv8Build &b, const wisp_model *model, const wisp_batch_desc *desc) {
   wisp_status st;
-  p.kv8 = true;
-  if ((st = make_plan(p, model, desc, true)) != WISP_OK || (st = kv8_build(b, model, desc)) != WISP_OK) return st;
-  const size_t at = p.host.size();
-  p.host.insert(p.host.end(), b.host.begin(), b.host.end());
-  // the descriptor block has grown: everything behind it moves
-  const size_t grown = align256(p.host.size() * 4) - align256(at * 4);
-  for (size_t *w : {&p.w_rope, &p.w_h, &p.w_xn, &p.w_ao, &p.w_af, &p.w_q, &p.w_part, &p.w_sm, &p.w_si, &p.w_ss, &p.w_rk,
-                    &p.w_ri, &p.w_rR, &p.w_vtok, &p.total})
-    *w += grown;
-  kv8_place(b, nullptr, p.w_desc + at * 4, p.total);
+  p.kv8 = &b;
+  if ((st = kv8_build(b, model, desc)) != WISP_OK || (st = make_plan(p, model, desc, true)) != WISP_OK) return st;
+  kv8_place(b, nullptr, p.w_desc + p.i_kv8 * 4, p.total);
   b.p.w_cs = p.w_rope;   // the step's own table of rotations
   return WISP_OK;
 }
