@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2601_11652_amd as W
+import test_gpu_token_logprobs as base
 from gpu_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +56,41 @@ def test_temperatures_at_the_ends_of_fp32(T, V):
         fin = ~torch.isinf(w32)
         # a chunk's exponentials and sums: 2^-22 of 16 binary orders each, and the result's rounding
         assert ((g.double() - w).abs()[fin] <= 2.0 ** -23 * w.abs()[fin] + 2.0 ** -17).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(7, 0), (0, 1)], ids=["wide loads", "single loads"])
+def test_vocabularies_of_more_chunks_than_a_thread_holds(pad, shift, dtype):
+    V = 270001
+    low = torch.finfo(dtype).min
+    x, tok = base._logits(6, V, dtype, 21, pad, shift)
+    x[1, :V] = low                              # a mask's lowest value: too many to rank at once
+    x[1, [V // 3, V - 1, 5]] = torch.tensor([1.0, 1.0, -2.0], device="cuda", dtype=dtype)
+    x[2, :V] = -float("inf")
+    x[3, :V] = 0.0
+    x[4, V - 1] = 30.0                          # the last entry of the last chunk
+    tok[1], tok[4] = 5, V - 1
+    for top in (0, 1, 32):
+        got, ws = base._run(x, V, tok, 1.0, top)
+        W.wisp_check(ws)
+        log(f"  top {top}: worst {base._check(x, V, tok, 1.0, top, got):.3f} of its bound")
+
+
+def test_most_probable_tokens_of_more_rows_than_a_launch_takes():
+    rows, V, top = (1 << 23) + 261, 2, 1
+    x = torch.randn(rows, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    tok = torch.arange(rows, device="cuda", dtype=torch.int32) % 3 - 1       # every third row has none
+    lp, H = torch.full((rows,), 7.0, device="cuda"), torch.full((rows,), 7.0, device="cuda")
+    ids, tlp = torch.full((rows, top), 7, dtype=torch.int32, device="cuda"), torch.full((rows, top), 7.0, device="cuda")
+    ws = W.workspace(W.wisp_token_logprobs_workspace_size(rows, V, top))
+    log(f"{rows} rows, {ws.numel() >> 20} MB of workspace")
+    W.wisp_token_logprobs(x, V, tok, 1.0, lp, H, ids, tlp, ws)
+    W.wisp_check(ws)
+    on, ls = tok >= 0, torch.log_softmax(x.double(), -1)
+    first = x[:, 1] > x[:, 0]
+    assert torch.equal(ids[on, 0], first[on].int())
+    # two entries: a handful of fp32 roundings of terms below 16
+    for g, w in ((lp, ls.gather(1, tok.clamp_min(0).long()[:, None])[:, 0]), (tlp[:, 0], ls.amax(-1)), (H, -(ls.exp() * ls).sum(-1))):
+        assert ((g.double() - w).abs()[on] <= 64 * 2.0 ** -24 * (1 + w.abs()[on])).all()
+        assert (g[~on] == 7).all()
+    assert (ids[~on] == 7).all()
