@@ -256,8 +256,9 @@ wisp_status wisp_attention(const wisp_model *model, const wisp_kv *kv, const wis
  *   K:  (((e / 32) * 4 + (e % 32) / 8) * 8 + (s / 8) * 4 + s % 4) * 16 + ((s / 4) % 2) * 8 + e % 8
  *   V:  ((e / 32) * 2 + s / 8) * 256 + (e % 16) * 16 + ((e / 16) % 2) * 8 + s % 8
  * (a lane's K or V operands of two matrix products are one 16-byte load).  The pools are 16-byte
- * aligned, the scales 8-byte.  Scales of pages in use are positive and finite, their V codes no NaN; both
- * hold for whatever wisp_kv8_append writes.  One layer's operators take that layer's pools.
+ * aligned, the scales 8-byte.  Scales of pages in use are 2^-100 to 2^100, their V codes no NaN; both
+ * hold for whatever wisp_kv8_append writes.  Attention sums V in fp32: contexts of any length at scales of
+ * up to 2^92, and of 2^(123 - k) tokens at 2^k above.  One layer's operators take that layer's pools.
  */
 typedef struct {
   void *k_pool, *v_pool;

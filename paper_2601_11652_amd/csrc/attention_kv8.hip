@@ -31,17 +31,25 @@ namespace wisp {
 
 namespace {
 
+// Eight codes x 2^EXP in bf16 (exact)
+template <int EXP = 0>
 __device__ __forceinline__ bf16x8_t to_bf16(uint32_t lo, uint32_t hi) {
+  constexpr float scale = EXP >= 0 ? 1 << EXP : 1.f / (1 << -EXP);
   union {
     bf16x2_t h[4];
     bf16x8_t v;
   } u;
-  u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return u.v;
 }
+// V's codes enter the second product x 2^-12, and the results leave it x 2^12: a probability of up to 2^8
+// (the reference lags behind the maximum) x a scale of 2^100 x 448 overflowed fp32 after 2^11
+// tokens; so 2^23 may follow, and at scales of 2^-100 a sum still has 24 bits above fp32's least.
+constexpr int kVDown = -12;
+constexpr float kVUp = 4096.f;
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
@@ -210,8 +218,8 @@ __device__ __forceinline__ void wide_items(const Kv8Args &a, uint4 *smem, float2
         }
         kv[i & 1][0][at] = as_uint4(to_bf16(kr[x].x, kr[x].y));
         kv[i & 1][0][at + 64] = as_uint4(to_bf16(kr[x].z, kr[x].w));
-        kv[i & 1][1][at] = as_uint4(to_bf16(vr[x].x, vr[x].y));
-        kv[i & 1][1][at + 64] = as_uint4(to_bf16(vr[x].z, vr[x].w));
+        kv[i & 1][1][at] = as_uint4(to_bf16<kVDown>(vr[x].x, vr[x].y));
+        kv[i & 1][1][at + 64] = as_uint4(to_bf16<kVDown>(vr[x].z, vr[x].w));
       }
     };
 
@@ -351,7 +359,7 @@ __device__ __forceinline__ void wide_items(const Kv8Args &a, uint4 *smem, float2
           continue;
         }
         const int64_t row = it.row0 + (lr0 + r) / G, col = (int64_t)(kvh * G + (lr0 + r) % G) * HD + c0;
-        const float inv = 1.0f / ml.y;
+        const float inv = kVUp / ml.y;
         y *= inv;
         z *= inv;
         uint16_t *to = reinterpret_cast<uint16_t *>(a.out) + (a.packed ? packed_off(row, col, a.out_K) : row * a.out_K + col);
@@ -632,7 +640,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const bf16x8_t v0 = to_bf16(vr[h][c].x, vr[h][c].y), v1 = to_bf16(vr[h][c].z, vr[h][c].w);
+        const bf16x8_t v0 = to_bf16<kVDown>(vr[h][c].x, vr[h][c].y), v1 = to_bf16<kVDown>(vr[h][c].z, vr[h][c].w);
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
@@ -694,7 +702,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void kv8_attn_kernel(Kv8Arg
         continue;
       }
       const int64_t row = it.row0 + (lr0 + r) / G, col = (int64_t)(kvh * G + (lr0 + r) % G) * HD + c0;
-      const float inv = 1.0f / l;
+      const float inv = kVUp / l;
       x *= inv;
       y *= inv;
       if constexpr (F32) {
@@ -801,7 +809,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(const Kv8Group *__restric
         acc[4] += y[c].x * w; acc[5] += y[c].y * w; acc[6] += y[c].z * w; acc[7] += y[c].w * w;
       }
     }
-    const float inv = 1.0f / den;
+    const float inv = kVUp / den;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= inv;
     const int64_t row = g.row0 + (lr0 + rr) / G;
