@@ -312,7 +312,8 @@ wisp_status wisp_kv8_append(const wisp_kv8_batch *batch, const wisp_kv8 *kv, con
 /*
  * wisp_attention over one layer of the 8-bit cache: q and out DEVICE [rows][n_q_heads][head_dim]
  * of the model's dtype, 16-byte aligned; row j of request i sees keys 0 .. ctx_len[i] + j.
- * Contexts may be of any length (no limit for fp32 models).
+ * Contexts may be of any length (no limit for fp32 models).  Scores may be as large as fp32 holds; a row
+ * with a larger one is NaN.
  */
 wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *q, void *out, void *stream);
 

@@ -91,11 +91,14 @@ struct Kv8Args {
   bool packed;
 };
 
+// Magnitude of a score in base 2 up to which its maximum's rounding moves a probability by less than bf16's
+constexpr float kFarScore = 65536.f;
+
 // The online softmax of a quad: its scores s (without K's scale; [row block][pair][half of its pages'
 // slots]) to probabilities x V's scale, in the order that the second product consumes.  Scales of the
 // lane's pages: ks K's in base 2, lv log2 of V's, vi its inverse.
 template <int RB, int MB, int NP>
-__device__ __forceinline__ void softmax(const floatx4 (&s)[RB][2][2], const float (&ks)[2], const float (&lv)[2],
+__device__ __forceinline__ void softmax(floatx4 (&s)[RB][2][2], const float (&ks)[2], const float (&lv)[2],
                                         const float (&vi)[2], float (&m_run)[RB], float (&l_run)[RB], floatx4 (&o)[RB][MB],
                                         uint4 (&pb)[NP][RB][2]) {
   constexpr bool F32 = NP > 1;
@@ -117,7 +120,21 @@ __device__ __forceinline__ void softmax(const floatx4 (&s)[RB][2][2], const floa
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) o[rb][mb] *= alpha;
     }
-    const float m = m_run[rb] == -INFINITY ? 0.f : m_run[rb];
+    float m = m_run[rb] == -INFINITY ? 0.f : m_run[rb], k[2] = {ks[0], ks[1]};
+    // m is a rounded product, s ks below an exact one: of large scores their difference would be mostly
+    // m's rounding (from 2^31 on, infinite probabilities)
+    if (__builtin_amdgcn_ballot_w64(fabsf(m) > kFarScore)) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[rb][h][x][e] = s[rb][h][x][e] * ks[h] - m;
+        k[h] = 1.f;
+      }
+      m = 0.f;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       // p x V's scale = 2^(s ks - m + log2 vs)
@@ -128,8 +145,8 @@ __device__ __forceinline__ void softmax(const floatx4 (&s)[RB][2][2], const floa
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
-          float f = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e], ks[h], off));
-          float g = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e + 1], ks[h], off));
+          float f = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e], k[h], off));
+          float g = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][h][x][e + 1], k[h], off));
           if constexpr (F32) rs += f + g;
 #pragma unroll
           for (int p = 0; p < NP; ++p) {

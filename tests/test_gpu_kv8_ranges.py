@@ -67,3 +67,58 @@ def test_long_contexts_of_equal_tokens(T, v_exp, code, bf16):
     err = np.abs(got / (v * 2.0 ** v_exp) - 1).max()
     log(f"{T} tokens of {code} x 2^{v_exp}: off by {err:.2e}")
     assert err <= tol
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("k_exp", [-100, 0, 6, 8, 20, 30, 60, 100])
+def test_large_equal_scores(k_exp, sign, bf16):
+    """Scores of 448 x 2^k_exp x 64 x 1.37 / 8, all alike, of either sign: the result is every token's V."""
+    hd, v = 64, np.linspace(-448.0, 448.0, 64)
+    v = kv8.VALUES[kv8.e4m3_encode(v)]
+    for T in (17, 5000):
+        got = _same_page(T, k_exp, 0, (np.full(hd, sign * 448.0), v), 2, hd, bf16, 1.37)
+        tol = 2.0 ** -8 if bf16 else (2 * 30 + 8) * 2.0 ** -24
+        err = np.abs(got - v).max() / 448.0
+        log(f"{T} tokens, K's scale 2^{k_exp}: off by {err:.2e}")
+        assert (np.abs(got - v) <= tol * np.abs(v)).all()
+
+
+@pytest.mark.parametrize("exps", [(10, 10), (16, 17), (24, 25), (40, 41), (99, 100), (-100, 100), (-100, 0, 30)])
+@pytest.mark.parametrize("k", range(len(SHAPES)))
+def test_scales_of_k_at_the_ends(k, exps):
+    """A row whose largest score stands out by more than fp32's error of it takes that token's V; where
+    it does not, the result still lies within V."""
+    c = Case(*SHAPES[k], seed=80 + k).fill()
+    c.scale[..., 0] = 2.0 ** np.random.default_rng(k).choice(exps, c.scale.shape[:2])
+    q = c.queries()
+    kv, plan = c.pool(), c.plan()
+    out = torch.full((c.M, c.n_q, c.hd), 7.0, dtype=torch.bfloat16 if c.bf16 else torch.float32, device="cuda")
+    W.wisp_attention_kv8(plan, kv, dev(q, c.bf16), out)
+    W.wisp_check(plan.ws)
+    got, G, off = out.double().cpu().numpy(), c.n_q // c.n_kv, np.concatenate([[0], np.cumsum(c.nrow)])
+    hk, hv, hs = host_pool(kv)
+    sure = n = 0
+    for b in range(len(c.ctx)):
+        end = int(c.ctx[b] + c.nrow[b])
+        blocks = c.pt[b, :(end + 15) // 16]
+        for h in range(c.n_kv):
+            K, V = (kv8.tokens(p, hs, w, blocks, h, end, c.hd) for p, w in ((hk, "k"), (hv, "v")))
+            for j in range(int(c.nrow[b])):
+                T = int(c.ctx[b]) + j + 1
+                for g in range(G):
+                    x = q[off[b] + j, h * G + g]
+                    s = K[:T] @ x / np.sqrt(c.hd)
+                    # the products' sum and the scaling, as in attention_bound, of either score
+                    fuzz = (c.hd + 8) * 2.0 ** -24 * (np.abs(K[:T]) @ np.abs(x)) / np.sqrt(c.hd)
+                    at = int(s.argmax())
+                    rest = np.delete(s + fuzz, at)
+                    o, top = got[off[b] + j, h * G + g], np.abs(V[:T]).max(0)
+                    n += 1
+                    assert np.isfinite(o).all() and np.all(np.abs(o) <= top * (1 + 2.0 ** -7))
+                    # 40 below: a share of e^-40 of each other token, less than fp32's half step of all
+                    if rest.size == 0 or s[at] - fuzz[at] > rest.max() + 40.0:
+                        sure += 1
+                        assert np.all(np.abs(o - V[at]) <= (2.0 ** -8 if c.bf16 else 2.0 ** -22) * np.abs(V[at]) + 2.0 ** -40 * top)
+    log(f"{SHAPES[k]}, K's scales {exps}: {sure} of {n} rows have one token")
+    assert min(exps) < 10 or sure > n // 2
