@@ -320,7 +320,7 @@ wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, 
 /*
  * wisp_verify on the 8-bit cache: the same step, its K and V appended and read by the two
  * operators above (a step's plan is its own).  Inputs, outputs, errors and the rollback by length as
- * wisp_verify's; the workspace holds wisp_verify_kv8_workspace_size bytes, plus
+ * wisp_verify's; the workspace (16-byte aligned) holds wisp_verify_kv8_workspace_size bytes, plus
  * wisp_logits_workspace_size when target_logits is NULL.  An fp32 model's contexts have no limit
  * of their own.  Batches are limited as wisp_kv8_plan's.  Like wisp_verify it is not for a stream that is
  * being captured.

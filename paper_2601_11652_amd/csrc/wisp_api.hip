@@ -1070,6 +1070,7 @@ wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const w
     if ((st = check_verify(model, nullptr, desc, tokens, accept_len, out_tokens, kv)) != WISP_OK) return st;
     if (desc->B == 0) return WISP_OK;
     if (!workspace) return fail(WISP_E_INVALID, "NULL workspace");
+    if ((uintptr_t)workspace & 15) return fail(WISP_E_INVALID, "workspace must be 16-byte aligned");
     Plan p;
     Kv8Build b;
     if ((st = plan_kv8_step(p, b, model, desc)) != WISP_OK) return st;
