@@ -145,7 +145,7 @@ constexpr int kQHeads = 2;   // q heads of a thread
 // one row (1 head: 50 us, 4: 53 us where 2 took 48).  Q is stored through the caches: past them this
 // kernel took 47 us, but the attention that reads Q next 11 us more.
 template <typename T, int S>
-__global__ __launch_bounds__(512) void kv8_append_kernel(const Kv8Unit *__restrict__ units, int n_units,
+__global__ __launch_bounds__(512) void kv8_append_kernel(const Kv8Unit *__restrict__ units,
                                                          const int32_t *__restrict__ page_table, int pt_stride,
                                                          const float2 *__restrict__ cs, QkvRows src, T *__restrict__ q,
                                                          uint8_t *__restrict__ k_pool, uint8_t *__restrict__ v_pool,
@@ -317,7 +317,7 @@ void append(const Kv8Plan &p, const Kv8Cache &c, const QkvRows &src, T *q, int *
   // rounded up: with blocks < 2^31 (wisp_kv8_plan) the error stays below one step, and the last step is whole
   const uint32_t q_share = (uint32_t)((((uint64_t)q_blocks << 32) + blocks - 1) / blocks);
   auto go = [&](auto kernel) {
-    launch(kernel, (uint32_t)blocks, threads, 0, s, units, p.n_units, p.page_table, p.pt_stride, cs, src, q, c.k, c.v,
+    launch(kernel, (uint32_t)blocks, threads, 0, s, units, p.page_table, p.pt_stride, cs, src, q, c.k, c.v,
            reinterpret_cast<float2 *>(c.scale), c.n_blocks, p.rows, p.nq, p.nkv, p.hd, q_share, err);
   };
   if (src.splits == 0) go(kv8_append_kernel<T, 0>);

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__res
   float m = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kGroup; ++k) m = fmaxf(m, v[k]);
-    // sums about the wave's maximum; in a wave of nothing but -inf about 0, where they are 0
+  // sums about the wave's maximum; in a wave of nothing but -inf about 0, where they are 0
   const float mw = wave_max(m), mc = mw == -INFINITY ? 0.f : mw;
   float s = 0.f, c = 0.f;
 #pragma unroll

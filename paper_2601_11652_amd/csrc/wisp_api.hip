@@ -37,7 +37,6 @@ wisp_status wisp::fail(wisp_status st, const char *fmt, ...) {
 
 namespace {
 
-
 // ------------------------------------------------------------------------------------------
 // launch plan
 // ------------------------------------------------------------------------------------------
@@ -756,8 +755,7 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
       ProfScope ps(WISP_PROF_ROWS, 0, 0, s);
       qkv_rope_append<T>(sd, part, sq, cs, qb, kl, vl, p.M, p.nq, p.nkv, p.hd, s);
     }
-    if (k8) {
-    } else if (p.bf16) {
+    if (!k8 && p.bf16) {
       float *po = reinterpret_cast<float *>(ws + p.w_attn_o);
       float *pml = reinterpret_cast<float *>(ws + p.w_attn_ml);
       {
@@ -769,7 +767,7 @@ wisp_status run_forward(const Plan &p, const wisp_model *m, const wisp_kv *kv, c
       ProfScope ps(WISP_PROF_ATTN_COMBINE, 0, 0, s);
       attention_bf16_combine(sd, groups, (int)p.groups.size(), p.item_rows, p.max_group_chunks, po, pml,
                              (uint16_t *)ao, true, p.qdim, p.nq, p.nkv, p.hd, s);
-    } else {
+    } else if (!k8) {
       ProfScope ps(WISP_PROF_ATTN, attn_bytes, attn_flops, s);
       attention_f32(sd, p.M, (const float *)qb, (const float *)kl, (const float *)vl, (float *)ao, p.nq,
                     p.nkv, p.hd, p.max_tokens, s);
