@@ -313,7 +313,8 @@ wisp_status wisp_kv8_append(const wisp_kv8_batch *batch, const wisp_kv8 *kv, con
  * wisp_attention over one layer of the 8-bit cache: q and out DEVICE [rows][n_q_heads][head_dim]
  * of the model's dtype, 16-byte aligned; row j of request i sees keys 0 .. ctx_len[i] + j.
  * Contexts may be of any length (no limit for fp32 models).  Scores may be as large as fp32 holds; a row
- * with a larger one is NaN.
+ * with a larger one is NaN.  For WISP_BF16 each probability is rounded to bf16 (2^-8 of it at most) before it
+ * multiplies V and in the sum of probabilities, as wisp_attention does; for WISP_F32 it keeps 24 bits.
  */
 wisp_status wisp_attention_kv8(const wisp_kv8_batch *batch, const wisp_kv8 *kv, const void *q, void *out, void *stream);
 

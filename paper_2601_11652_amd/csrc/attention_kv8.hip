@@ -15,9 +15,14 @@
 // through LDS, the parts of a context that several items share by a second kernel.
 //
 // Bound by the memory for long contexts (128 requests of 0.25-32k tokens, 32 + 8 heads of 128: 1.73 GB in
-// 327 us, 5.3 TB/s), by vector instructions for prompts (4096 rows: 185 us, 0.75 PFLOP/s: half
-// a conversion and five instructions of softmax for each product), by latency for few requests (one of 1300
-// tokens: 8 us and 3 for the join).
+// 328 us, 5.3 TB/s), by vector instructions for prompts (4096 rows: 172 us in a row of calls, 0.81 PFLOP/s,
+// 192 by itself: two instructions of softmax, half a conversion and two of addresses, scales and
+// rescaling for each product), by latency for few requests (one of 1300 tokens: 8 us and 3 for the join).
+//
+// A bf16 model's probabilities are rounded to bf16 (2^-8 of each at most) for the second product, as those
+// over a bf16 cache are: in one part that product takes half a prompt's matrix instructions, in two
+// two thirds.  The sum that divides adds the same rounded values.  Against 64 bits the results are off by
+// 1.7e-3 to 1.9e-3 of their size, of which the output's own rounding makes 1.7e-3.
 //
 // An fp32 model's queries and probabilities enter the products as three bf16 parts each (8 bits
 // of the significand per part: 24 in all), so its results are fp32's.
@@ -171,8 +176,9 @@ __device__ __forceinline__ void softmax(floatx4 (&s)[RB][2][2], const float (&ks
 // The same for bundles of three or four row groups (a prompt's, whose rows are many and whose codes are
 // few), of which each wave takes one: by themselves they would all convert the same codes, 128 instructions
 // beside 64 matrix products a quad.  Here each converts a quarter of a quad for all, through LDS, a
-// quad ahead, and codes are asked for two quads ahead; the queries are in registers.  Bound by vector instructions as before, with 96 fewer a quad: a prompt of
-// 4096 rows 200 -> 185 us (0.75 PFLOP/s), of 100 rows 14.6 -> 11.7.
+// quad ahead, and codes are asked for two quads ahead; the queries are in registers.  Bound by vector
+// instructions as before, with 96 fewer a quad: a prompt of 4096 rows takes 185 us without and 172
+// with it, one of 100 rows beside three requests 14.8 and 11.9.
 template <int HD>
 __device__ __forceinline__ void wide_items(const Kv8Args &a, uint4 *smem, float2 (*sh_ml)[32]) {
   constexpr int RB = 2, ROWS = 16 * RB, KC = HD / 32, MB = HD / 16, LDJ = HD + 4;

@@ -41,13 +41,17 @@ struct Piece {                          // page pairs from .. to - 1 of a bundle
 // The cost of a page pair in quarters of a wave's turn: one row group's pairs are spread over four
 // waves; two groups have two waves each but share what is read, three or four one.  Starting
 // an item takes as long as two turns of four waves (15 thousand cycles, a turn 7).  128 requests of
-// 0.25-32k: 330 us; with pairs of 4, 4 and 7 398, of 4, 8 and 16 341, without the cost of an item 338.
-// kWide: of a pair that the waves convert together (prompts of 1500-2000 rows beside 10 requests 83.9 us;
-// 9: 81.5, 14: 83.1; one of 100 beside 3 11.7, 13.3 and 13.1).
+// 0.25-32k: 331 us; with pairs of 4, 4 and 7 405, of 4, 8 and 16 338, without the cost of an item 338; 32 of
+// 0.5-2k 25.3, 27.4, 24.8 and 28.1; 16 of 4-32k on 64 query heads 86, 104, 88 and 89; 128 of 0.3-1.2k 38.9,
+// 38.7, 39.0 and 52.4.
+// kWide: of a pair that the waves convert together (two prompts of 1500-2000 rows beside 10 requests 79.7 us;
+// 9: 77.8, 14: 79.7; one of 100 beside 3 11.9, 13.5 and 13.2; one of 4096 172 with all).
 constexpr int64_t kPair[5] = {0, 4, 7, 14, 14}, kStart = 64, kWide = 12;
 constexpr int64_t kTurn = 32;           // cost of a turn
 // Where both workgroups of a CU are there, the older one's waves go first: percent of the work that
-// the older half of the shares takes (128 requests of 0.25-32k: 330 us; 50 %: 334, 60 %: 349).
+// the older half of the shares takes (128 requests of 0.25-32k: 331 us; 50 %: 356, 60 %: 355; 66 of 2k 55.7,
+// 57.2 and 61.0; 64 of 1-6k on 64 query heads 112, 115 and 117; but a prompt of 4096 rows 172, 168 and 186,
+// one of 3000 beside 40 requests 115, 108 and 117).
 constexpr int64_t kOld = 55;
 int64_t grain_of(const Bundle &u) { return u.groups == 1 ? 8 : u.groups == 2 ? 4 : 2; }   // pairs of a turn
 
@@ -115,9 +119,10 @@ std::vector<Piece> shares_of(const std::vector<Bundle> &bundles, int64_t &shares
   shares = std::max<int64_t>(1, (total + size - 1) / size);
   std::vector<Piece> pieces = by_borders(bundles, shares, size, total);
   // Cut bundles start twice, write what they have per row group and wait for its join: shares of whole
-  // ones may end that much later.  Requests of one row group, 128 of 0.3-1.2k tokens (12 % more in the
-  // longest share): 50.4 us cut, 42.0 whole; 66 of 2k (76 % more) 56.0 and 61.0; prompts of
-  // 1500-2000 rows (8 %) 105 and 87.  Short shares are cut: whole bundles would leave CUs idle.
+  // ones may end that much later.  128 requests of 0.3-1.2k tokens: 47.2 us cut, 38.9 whole; 66 of 2k 56
+  // and 61; 256 of 1-4k 207 and 191; 64 of 1-6k on 64 query heads 112 and 245; two prompts of 1500-2000 rows
+  // beside 10 requests 113 and 80, six of them 215 and 202, one of 4096 181 and 172.  The rule takes the
+  // better side of each.  Short shares are cut: whole bundles would leave CUs idle.
   if (size >= 8 * kTurn) {
     int64_t end = 0, groups = 0;
     for (const Bundle &u : bundles) groups += u.groups;
@@ -190,9 +195,9 @@ wisp_status wisp::kv8_build(Kv8Build &b, const wisp_model *m, const wisp_batch_d
   }
   // Every kv head's work, the same for all, in shares, one for each workgroup (two per CU).  Bundles of
   // three and four row groups run apart (the attention's wide items) where they are half of the work
-  // or more, each set with its part of the workgroups: a prompt of 4096 rows 200 us together, 185
-  // apart, one of 500 beside 3 decoding requests 23.8 and 21.6, one of 3000 beside 40 143 and 142;
-  // of less than half, 128 requests of 2 to 17 rows, 332 and 358.
+  // or more, each set with its part of the workgroups: a prompt of 4096 rows 185 us together, 172
+  // apart, one of 500 beside 3 decoding requests 23.7 and 21.6, one of 3000 beside 40 116 and 115, six of
+  // 1500-2000 224 and 202; of less than half, 128 requests of 0.25-32k and up to 17 rows, 331 and 357.
   const int64_t wgs = (int64_t)device_cus() * 2, most_shares = std::max<int64_t>(1, wgs / p.nkv);
   if (n_bundles + most_shares > kKv8MaxItems / p.nkv) return too_many((n_bundles + most_shares) * p.nkv);
   int64_t cost[2] = {0, 0};

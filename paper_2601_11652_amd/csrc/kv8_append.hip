@@ -136,13 +136,14 @@ constexpr uint32_t kNan4 = 0x7F7F7F7Fu;   // four e4m3 NaN
 constexpr int kQHeads = 2;   // q heads of a thread
 
 // Two kinds of workgroups, interleaved over the grid in one even pattern.  A page's chain of loads
-// (unit, page table, old codes) would leave the memory idle by itself: all pages first, 12922 rows of
-// 32 + 2 x 8 heads of 128 took 58 us, interleaved 52 us (283 MB, 5.4 TB/s: near a copy's rate, so the
-// memory bounds it; 32 requests of 2 to 9 rows 4.7 us, the chain's latency).
+// (unit, page table, old codes) would leave the memory idle by itself: all pages first, 12538 rows of
+// 32 + 2 x 8 heads of 128 take 58.5 us, interleaved 55.9 (283 MB, 5.1 TB/s: a copy's rate, so the
+// memory bounds it; 32 requests of 2 to 9 rows 4.6 us, the chain's latency).
 // One page of one kv head, 2 * hd threads: the first hd hold K, thread (slot, i) the dims 8i .. 8i + 7
 // and their rotation partners; the others V, thread (half, p) the dims 2p, 2p + 1 of 8 slots: each
 // thread's values make whole 8-byte pieces of the page.  Or Q, a thread 8 + 8 dims of kQHeads heads of
-// one row (1 head: 50 us, 4: 53 us where 2 took 48).  Q is stored through the caches: past them this
+// one row (the same rows 54.6 us with 1 head, 59.6 with 4; 64 query heads 88.9 with 1, 92.7 with 2; but 3600
+// rows 16.7 and 16.0, 256 requests 14.4 and 13.5).  Q is stored through the caches: past them this
 // kernel took 47 us, but the attention that reads Q next 11 us more.
 template <typename T, int S>
 __global__ __launch_bounds__(512) void kv8_append_kernel(const Kv8Unit *__restrict__ units,

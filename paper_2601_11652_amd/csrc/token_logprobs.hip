@@ -67,9 +67,14 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b, float sc) {
 }
 
 // Grid rows x chunks, chunks fastest.  Bound by the memory where there are many fp32 rows (742 of
-// 128256: 66 us for 381 MB, 5.8 TB/s), by instructions in bf16, whose entries come twice as fast (300
-// of 50021: 11.3 us for 30 MB).  A chunk is 32 entries a thread: with the sums about the wave's own
-// maximum, known before the first exponential, an entry takes one exponential and no rescaling.
+// 128256: 66 us for 381 MB, 5.8 TB/s).  In bf16, whose entries come twice as fast, about half of the time
+// is vector instructions (12 for each place of a chunk, of 300 rows of 50021 5 to 6 of 11 us for 30 MB), the
+// rest waits for loads, which a thread of one round has nothing to do beside.  A chunk is 32 entries a
+// thread: with the sums about the wave's own maximum, known before the first exponential, an entry
+// takes one exponential and no rescaling.
+// VEC: 16-byte loads, where every row starts on 16 bytes; else one entry a load.  742 contiguous rows of
+// 50257 (which start anywhere) with 8 tokens each take 40 us in fp32 and 50 in
+// bf16, padded to rows of 16 bytes 36 and 31; 6 rows 10.2 and 12.9, padded 10.1 and 10.4.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void logprobs_chunk_kernel(const T *__restrict__ logits, int V, int64_t ld, int nch,
                                                                  float sc, const int32_t *__restrict__ tokens,
