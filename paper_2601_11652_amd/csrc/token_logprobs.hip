@@ -462,7 +462,7 @@ extern "C" wisp_status wisp_token_logprobs(const void *logits, int32_t dtype, in
     };
     using One = std::integral_constant<int, 1>;
     const int es = dtype == WISP_F32 ? 4 : 2;
-    const bool vec = ((uintptr_t)logits & 15) == 0 && ld * es % 16 == 0;
+    const bool vec = ((uintptr_t)logits & 15) == 0 && (rows == 1 || ld * es % 16 == 0);   // every row starts on 16 bytes
     if (dtype == WISP_F32) {
       const float *x = static_cast<const float *>(logits);
       vec ? go(x, logprobs_chunk_kernel<float, true>, rows_of(x, std::integral_constant<int, 4>{}))

@@ -94,3 +94,17 @@ def test_most_probable_tokens_of_more_rows_than_a_launch_takes():
         assert ((g.double() - w).abs()[on] <= 64 * 2.0 ** -24 * (1 + w.abs()[on])).all()
         assert (g[~on] == 7).all()
     assert (ids[~on] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 7, 8193, 50257, 270001])
+@pytest.mark.parametrize("shift", [0, 1, 8])
+def test_a_single_row_of_any_length(shift, V, dtype):
+    """Its length says nothing of its start: wide loads where that is on 16 bytes, up to the last entry."""
+    x, tok = base._logits(1, V, dtype, 31 + V, 0, shift)
+    x[0, V - 1] = 12.0
+    tok[0] = V - 1
+    for top in (0, 5):
+        got, ws = base._run(x, V, tok, 1.0, top)
+        W.wisp_check(ws)
+        log(f"one row of {V}, off by {shift}, top {top}: worst {base._check(x, V, tok, 1.0, top, got):.3f} of its bound")
