@@ -52,8 +52,8 @@ def test_step_with_partial_sums(case):
     W.wisp_check(ws)
     ref = _forward(s, kv, pt, ctx, nrow, tokens, True)      # checks the new rows' pages
     ref = ref[np.concatenate([np.arange(e - g - 1, e) for e, g in zip(np.cumsum(nrow), gamma)])]
-    # a layer rounds to bf16 eight times on a row's way (two norms, queries, probabilities, heads, the MLP's
-    # product, the last norm, and the two sides' weights are the same): 2^-8 each of the row's scale
+    # a row is rounded to bf16 seven times on its way (two norms, queries, probabilities, heads, the MLP's
+    # product, the last norm): 2^-8 each of its scale, and as much for all fp32 sums
     err = np.abs(logits.cpu().numpy() - ref) / np.abs(ref).max(-1, keepdims=True)
     log(f"  logits off by {err.max():.2e} of their row's largest")
     assert err.max() <= 8 * 2.0 ** -8
