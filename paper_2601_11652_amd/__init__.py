@@ -664,8 +664,13 @@ def wisp_draft_stats(logits, vocab: int, temperature: float, stats, ws=None, str
         raise ValueError(f"logits: expected [rows][>= {vocab}] with unit column stride")
     if ws is None:
         ws = _scratch(lib.wisp_draft_stats_workspace_size(rows, vocab), logits.device, stream)
-    _ok(lib.wisp_draft_stats(_dev(logits, "logits", dtype=_f32(), contiguous=False), rows, vocab, logits.stride(0),
-                             temperature, _dev(stats, "stats", rows * 4, dtype=_f32()), *_ws(ws), _stream(stream)))
+    args = (_dev(logits, "logits", dtype=_f32(), contiguous=False), rows, vocab, logits.stride(0), temperature,
+            _dev(stats, "stats", rows * 4, dtype=_f32()), *_ws(ws))
+    for t in (stats, ws):
+        if t.device != logits.device:
+            raise ValueError(f"a tensor on {t.device}, logits on {logits.device}")
+    with _On(logits.device):
+        _ok(lib.wisp_draft_stats(*args, _stream(stream)))
 
 
 def wisp_token_logprobs_workspace_size(rows: int, vocab: int, n_top: int) -> int:

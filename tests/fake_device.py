@@ -35,10 +35,11 @@ class FakeStream:
 
 class Calls:
     """Patches torch.cuda and the library.  `made`: (bytes, handle of the stream that was current) of
-    every workspace; `calls`: (name, arguments) of every library call."""
+    every workspace; `calls`, `devices`: (name, arguments) of every library call, and the device current in it."""
 
     def __init__(self, monkeypatch, workspace_bytes=4096):
-        self.made, self.calls, self.current = [], [], 1
+        self.made, self.calls, self.current, self.on = [], [], 1, 0
+        self.devices = []
         cuda = torch.cuda
 
         @contextlib.contextmanager
@@ -47,6 +48,12 @@ class Calls:
             yield
             self.current = was
 
+        @contextlib.contextmanager
+        def device(d):
+            was, self.on = self.on, torch.device(d).index
+            yield
+            self.on = was
+
         def workspace(n, device="cuda"):
             self.made.append((n, self.current))
             return fake(max(n, 256), dtype=torch.uint8, index=torch.device(device).index or 0)
@@ -54,6 +61,7 @@ class Calls:
         def call(name):
             def f(*args):
                 self.calls.append((name, args))
+                self.devices.append(self.on)
                 return workspace_bytes if name.endswith("_size") else W.WISP_OK
             return f
 
@@ -63,7 +71,7 @@ class Calls:
 
         for name, v in (("Stream", FakeStream), ("ExternalStream", lambda raw, device=None: FakeStream(raw)),
                         ("default_stream", lambda device=None: FakeStream(0)), ("stream", stream),
-                        ("current_device", lambda: 0), ("device", lambda d: contextlib.nullcontext())):
+                        ("current_device", lambda: self.on), ("device", device)):
             monkeypatch.setattr(cuda, name, v)
         monkeypatch.setattr(W, "_raw", lambda i: self.current)
         monkeypatch.setattr(W, "workspace", workspace)

@@ -35,3 +35,23 @@ def test_the_step_refuses_a_second_device(monkeypatch, name):
     with pytest.raises(ValueError):
         _step(**{name: 1})
     assert not c.calls
+
+
+def test_calls_run_on_their_tensors_device(monkeypatch):
+    c = Calls(monkeypatch)
+    W.wisp_draft_stats(fake(3, 100, index=1), 100, 1.0, fake(3, 4, index=1))
+    W.wisp_token_logprobs(fake(3, 100, index=1), 100, fake(3, dtype=torch.int32, index=1), 1.0, fake(3, index=1))
+    _step(**{n: 1 for n in ("tokens", "draft_probs", "accept_len", "out_tokens", "target_logits", "workspace", "page_table", "kv")})
+    ran = {name: on for (name, _), on in zip(c.calls, c.devices) if not name.endswith("_size")}
+    assert ran == {"wisp_draft_stats": 1, "wisp_token_logprobs": 1, "wisp_verify_kv8": 1}
+    assert c.on == 0
+
+
+@pytest.mark.parametrize("name", ["stats", "ws"])
+def test_draft_stats_refuses_a_second_device(monkeypatch, name):
+    c = Calls(monkeypatch)
+    at = {name: 1}
+    with pytest.raises(ValueError):
+        W.wisp_draft_stats(fake(3, 100), 100, 1.0, fake(3, 4, index=at.get("stats", 0)),
+                           fake(4096, dtype=torch.uint8, index=at.get("ws", 0)))
+    assert not c.calls
