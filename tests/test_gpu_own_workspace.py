@@ -57,3 +57,32 @@ def test_draft_stats_on_another_stream(raw):
         torch.cuda.synchronize()
         log(f"draft statistics, step {step}")
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("named", [False, True], ids=["current stream", "named stream"])
+def test_captured_with_its_own_workspace(named):
+    rows, V, top = 20, 40000, 6
+    x = torch.randn(rows, V, device="cuda")
+    tok = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32)
+    outs = lambda: (torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"),
+                    torch.zeros(rows, top, dtype=torch.int32, device="cuda"), torch.zeros(rows, top, device="cuda"))
+    a, b, stats, want = outs(), outs(), torch.zeros(rows, 4, device="cuda"), torch.zeros(rows, 4, device="cuda")
+    n, side = W.wisp_token_logprobs_workspace_size(rows, V, top), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        W.wisp_token_logprobs(x, V, tok, 1.0, *a, None, side if named else None)
+        W.wisp_draft_stats(x, V, 1.0, stats, None, side if named else None)
+    for step in range(4):
+        x.normal_()
+        _churn(n)
+        torch.cuda.synchronize()
+        graph.replay()
+        _churn(n)
+        W.wisp_token_logprobs(x, V, tok, 1.0, *b, W.workspace(n))
+        W.wisp_draft_stats(x, V, 1.0, want)
+        torch.cuda.synchronize()
+        log(f"captured with its own workspace, replay {step}")
+        assert torch.equal(stats, want)
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
