@@ -332,6 +332,91 @@ wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const w
                             int32_t *out_tokens, float *target_logits, void *workspace, size_t workspace_bytes,
                             void *stream);
 
+/*
+ * Batches whose requests share prefixes (Sec. 4.5's paged KV: the blocks of a common system prompt or
+ * document stand in several requests' tables).  A group is a run of consecutive requests whose first
+ * prefix_len tokens (whole pages, at most every member's ctx_len) are the same blocks; group_size and
+ * prefix_len are HOST arrays of n_groups, the sizes add up to desc->B, a group of one request or a
+ * prefix of 0 shares nothing, and n_groups = 0 means that no request does.  The common blocks are read through the first
+ * member's table.
+ *
+ * wisp_shared_plan plans a batch for the calls below, on all layers: it uploads their work lists into the workspace
+ * (DEVICE, 256-byte aligned, at least wisp_shared_workspace_size bytes; its first 256 bytes are the fault
+ * record of wisp_check, zero before the first use) and keeps desc->kv_page_table and pt_stride.  It
+ * reads model's shape and dtype, and desc's ctx_len, gamma, prefill_len: rows are ordered as in
+ * wisp_verify.  While `stream` is being captured the lists travel as kernel arguments.  A planned batch
+ * (its fields are the library's own) is copied freely and valid while its workspace and page table are.  The
+ * calls on it only launch kernels: they may be captured, on any stream ordered after the plan's.  They use the
+ * workspace's scratch, so calls on one plan must not overlap.  Pools, q and out are 16-byte aligned; outputs must not
+ * overlap inputs unless stated.  Block ids outside [0, n_blocks) are recorded in the workspace for wisp_check; what
+ * is read of such a page is undefined.
+ * WISP_E_UNSUPPORTED (and a workspace size of 0): more than WISP_ROWS_MAX rows, more than 64 query heads per kv head, or
+ * more than 2^22 work items (x kv heads: one per 128 rows x query heads of a kv head and part of the tokens;
+ * one per 128 tokens and part of the rows).
+ */
+typedef struct { uint64_t opaque[32]; } wisp_shared_batch;
+
+size_t wisp_shared_workspace_size(const wisp_model *model, const wisp_batch_desc *desc, int32_t n_groups,
+                                  const int32_t *group_size, const int32_t *prefix_len);
+wisp_status wisp_shared_plan(const wisp_model *model, const wisp_batch_desc *desc, int32_t n_groups,
+                             const int32_t *group_size, const int32_t *prefix_len, void *workspace,
+                             size_t workspace_bytes, wisp_shared_batch *batch, void *stream);
+
+/*
+ * wisp_attention over one layer's pools, a group's common tokens read and computed once for all its rows:
+ *   q, out  DEVICE [rows][n_q_heads][head_dim] of the model's dtype (q rotated)
+ *   lse     DEVICE fp32 [rows][n_q_heads] or NULL: ln of the sum of exp(q . k / sqrt(head_dim)) over the
+ *           keys that the row sees
+ * Row j of request i sees keys 0 .. ctx_len[i] + j; tokens that a row does not see do not touch it, whatever they
+ * hold, nor do slots past a request's last token.  Contexts of any length.  Scores may be as large as fp32 holds; a
+ * row with a NaN, or with a score of +infinity, is NaN.  For WISP_BF16 each probability is rounded to bf16 (2^-8 of it at
+ * most) before it multiplies V; the sum that divides, and lse, add them in fp32.
+ */
+wisp_status wisp_attention_shared(const wisp_shared_batch *batch, const wisp_kv *kv, const void *q, void *out,
+                                  float *lse, void *stream);
+
+/*
+ * The attention weight that each token of the cache gets from the batch's rows, for the eviction below:
+ * over the rows r that count and see token t, and the query heads of kv head h,
+ *   mass[t][h] = decay * prev[t][h] + sum exp(q_r . k_t / sqrt(head_dim) - lse_r)
+ * with decay * prev for tokens cached before (positions below ctx_len) only.
+ *   q       as above; lse DEVICE fp32 [rows][n_q_heads], as wisp_attention_shared gives it
+ *   count   DEVICE int32 [B] or NULL: the first count[i] rows of request i count (its prompt, root and accepted
+ *           drafts, say); NULL: all.  Tokens that only rows past them see get 0.
+ *   prev, mass  DEVICE fp32 [n_blocks][n_kv_heads][16], one value for each slot of a layer's pages; prev may be
+ *           NULL (nothing before) or mass itself.  Slots of the batch's tokens are written, others left.
+ * A page that is not common to a group belongs to one request; a group's common tokens get the sum over all its rows.
+ * Sums are fp32, in a fixed order.  A row whose lse is NaN makes the tokens that it sees NaN; one of +infinity adds 0.
+ */
+wisp_status wisp_attention_mass(const wisp_shared_batch *batch, const wisp_kv *kv, const void *q, const float *lse,
+                                const int32_t *count, float decay, const float *prev, float *mass, void *stream);
+
+/*
+ * Eviction: of each request's ctx_len cached tokens, in every layer and kv head by itself, keep[i] stay (all,
+ * where it is not less): the first sink[i], the last recent[i], and of the others those of greatest mass
+ * (equal ones: the first; NaN is less than any number).  They move together, in order, to positions
+ * 0 .. keep[i] - 1: K is rotated by its new position less its old one (rotate-half pairing, angle as in the
+ * step), rounded once, so that the cache is again one of ctx_len = keep[i] tokens at those positions, for every call of this
+ * library; V and mass move as they are.
+ *   kv      model->n_layers layers, as wisp_verify's (a model of one layer: that layer's pools)
+ *   desc    B, ctx_len, kv_page_table, pt_stride only
+ *   keep, sink, recent  HOST int32 [B]; sink and recent may be NULL (0); sink + recent <= keep where tokens leave
+ *   to_table  DEVICE int32 [B][to_stride]: the pages that take the kept tokens, each the request's own page at the
+ *           same index, or one that no request of the call has; NULL: desc's table (in place)
+ *   mass    DEVICE fp32 [n_layers][n_blocks][n_kv_heads][16]
+ *   kept    DEVICE int32 [n_layers][n_kv_heads][sum of min(keep, ctx_len)]: the old positions of the tokens kept
+ * A token that keeps its position and page is not written: pages of the first `sink` tokens may be shared.  Pages past the
+ * kept tokens, and the last one's slots past them, are left as they were.  The workspace (DEVICE, 256-byte
+ * aligned, wisp_kv_evict_workspace_size bytes; its first 256 bytes the fault record of wisp_check) may be used again by
+ * a call on a stream ordered after this one.  Reads of block ids out of range are undefined, writes are left
+ * out.  While `stream` is being captured the requests' figures travel as kernel arguments.
+ * WISP_E_CAPACITY: a table too short for ctx_len or keep.
+ */
+size_t wisp_kv_evict_workspace_size(const wisp_model *model, const wisp_batch_desc *desc);
+wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp_batch_desc *desc, const int32_t *keep,
+                          const int32_t *sink, const int32_t *recent, const int32_t *to_table, int32_t to_stride,
+                          float *mass, int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Uniform draws of the step's random stream: out[k] = draw (seed, req_id, tag, row, k),
  * k < n (DEVICE fp32).  tag 1 = acceptance, 2 = race. */
 wisp_status wisp_uniform(uint64_t rng_seed, uint32_t req_id, uint32_t tag, uint32_t row, uint32_t n,

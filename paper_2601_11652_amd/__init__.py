@@ -8,8 +8,9 @@ the library has not been built -- there is no fallback implementation.
 Entry points keep the C names: wisp_verify, wisp_accept, wisp_attention,
 wisp_pack_linear, wisp_workspace_size, wisp_accept_workspace_size, wisp_uniform,
 wisp_check, wisp_last_error, wisp_schedule, wisp_draft_stats, wisp_reject_predict,
-wisp_kv8_plan, wisp_kv8_append, wisp_attention_kv8, wisp_verify_kv8, wisp_token_logprobs;
-``KV8Pool`` holds the 8-bit cache and ``KV8Batch`` a batch planned for it, ``KVManager`` wraps the wisp_kvm_* calls and ``RejectMLP`` the predictor's weights.
+wisp_kv8_plan, wisp_kv8_append, wisp_attention_kv8, wisp_verify_kv8, wisp_token_logprobs, wisp_shared_plan,
+wisp_attention_shared, wisp_attention_mass, wisp_kv_evict;
+``SharedBatch`` holds a batch planned with shared prefixes, ``KV8Pool`` holds the 8-bit cache and ``KV8Batch`` a batch planned for it, ``KVManager`` wraps the wisp_kvm_* calls and ``RejectMLP`` the predictor's weights.
 ``GpuModel`` and ``BatchDesc`` assemble the C structs.
 """
 from __future__ import annotations
@@ -48,7 +49,8 @@ EXPORTS = ("wisp_workspace_size", "wisp_logits_workspace_size", "wisp_accept_wor
            "wisp_kvm_get_stats", "wisp_draft_stats_workspace_size", "wisp_draft_stats", "wisp_reject_predict",
            "wisp_gemm_plan", "wisp_attention_plan", "wisp_verify_noalloc", "wisp_kv8_workspace_size", "wisp_kv8_plan",
            "wisp_kv8_append", "wisp_attention_kv8", "wisp_verify_kv8_workspace_size", "wisp_verify_kv8",
-           "wisp_token_logprobs_workspace_size", "wisp_token_logprobs")
+           "wisp_token_logprobs_workspace_size", "wisp_token_logprobs", "wisp_shared_workspace_size", "wisp_shared_plan",
+           "wisp_attention_shared", "wisp_attention_mass", "wisp_kv_evict_workspace_size", "wisp_kv_evict")
 
 
 class WispError(RuntimeError):
@@ -79,6 +81,10 @@ class wisp_kv8(C.Structure):
 
 
 class wisp_kv8_batch(C.Structure):
+    _fields_ = [("opaque", C.c_uint64 * 32)]
+
+
+class wisp_shared_batch(C.Structure):
     _fields_ = [("opaque", C.c_uint64 * 32)]
 
 
@@ -186,7 +192,17 @@ def _load():
     L.wisp_verify_kv8_workspace_size.restype = C.c_size_t
     L.wisp_verify_kv8.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_kv8), C.POINTER(wisp_batch_desc),
                                   _VP, _VP, C.c_uint64, _VP, _VP, _VP, _VP, C.c_size_t, _VP]
-    for name in ("wisp_verify_kv8", "wisp_token_logprobs", "wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
+    L.wisp_shared_workspace_size.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc), C.c_int32, _I32P, _I32P]
+    L.wisp_shared_workspace_size.restype = C.c_size_t
+    L.wisp_shared_plan.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc), C.c_int32, _I32P, _I32P, _VP, C.c_size_t,
+                                   C.POINTER(wisp_shared_batch), _VP]
+    L.wisp_attention_shared.argtypes = [C.POINTER(wisp_shared_batch), C.POINTER(wisp_kv), _VP, _VP, _VP, _VP]
+    L.wisp_attention_mass.argtypes = [C.POINTER(wisp_shared_batch), C.POINTER(wisp_kv), _VP, _VP, _VP, C.c_float, _VP, _VP, _VP]
+    L.wisp_kv_evict_workspace_size.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_batch_desc)]
+    L.wisp_kv_evict_workspace_size.restype = C.c_size_t
+    L.wisp_kv_evict.argtypes = [C.POINTER(wisp_model), C.POINTER(wisp_kv), C.POINTER(wisp_batch_desc), _I32P, _I32P, _I32P, _VP,
+                                C.c_int32, _VP, _VP, _VP, C.c_size_t, _VP]
+    for name in ("wisp_shared_plan", "wisp_attention_shared", "wisp_attention_mass", "wisp_kv_evict", "wisp_verify_kv8", "wisp_token_logprobs", "wisp_kv8_plan", "wisp_kv8_append", "wisp_attention_kv8", "wisp_pack_linear", "wisp_pack_gate_up", "wisp_verify", "wisp_verify_noalloc", "wisp_accept", "wisp_attention", "wisp_uniform",
                  "wisp_check", "wisp_gemm_plan", "wisp_attention_plan", "wisp_profile_enable", "wisp_profile_read", "wisp_profile_reset",
                  "wisp_schedule", "wisp_kvm_create", "wisp_kvm_lookup", "wisp_kvm_reserve", "wisp_kvm_commit",
                  "wisp_kvm_release", "wisp_kvm_get_stats", "wisp_draft_stats", "wisp_reject_predict"):
@@ -632,6 +648,125 @@ def wisp_verify_kv8(model: wisp_model, kv: KV8Pool, desc: BatchDesc, tokens, dra
             raise ValueError(f"a tensor on {t.device}, kv on {kv.device}")
     with _On(kv.device):
         _ok(lib.wisp_verify_kv8(C.byref(model), C.byref(kv.c), C.byref(desc.c), *args, _stream(stream)))
+
+
+def _host_i32(x, what: str, n: int | None = None):
+    """(int32 array, pointer) of a host sequence; (None, None) of None."""
+    if x is None:
+        return None, None
+    a = np.ascontiguousarray(x, dtype=np.int32)
+    if a.ndim != 1 or (n is not None and a.shape[0] != n):
+        raise ValueError(f"{what}: expected [{'' if n is None else n}], got {a.shape}")
+    return a, a.ctypes.data_as(C.POINTER(C.c_int32))
+
+
+def _groups(group_size, prefix_len):
+    size, ps = _host_i32(group_size, "group_size")
+    n = 0 if size is None else size.shape[0]
+    prefix, pp = _host_i32(prefix_len, "prefix_len", n)
+    if (size is None) != (prefix is None):
+        raise ValueError("group_size and prefix_len come together")
+    return n, ps, pp, (size, prefix)
+
+
+def wisp_shared_workspace_size(model: wisp_model, desc: BatchDesc, group_size=None, prefix_len=None) -> int:
+    n, ps, pp, _ = _groups(group_size, prefix_len)
+    return int(lib.wisp_shared_workspace_size(C.byref(model), C.byref(desc.c), n, ps, pp))
+
+
+class SharedBatch:
+    """A batch planned with its shared prefixes (wisp_shared_plan): keeps the workspace and the page
+    table alive, and the sizes that the calls on it check their tensors against."""
+
+    def __init__(self, c, model: wisp_model, desc: BatchDesc, ws):
+        import torch
+        self.c, self.ws, self.page_table, self.model, self.B = c, ws, desc.page_table, model, desc.B
+        self.heads = desc.rows * model.n_q_heads
+        self.q_numel, self.page = self.heads * model.head_dim, (model.n_kv_heads, PAGE * model.head_dim)
+        self.dtype = torch.bfloat16 if model.dtype == WISP_BF16 else torch.float32
+        self.device = ws.device
+
+
+def wisp_shared_plan(model: wisp_model, desc: BatchDesc, group_size, prefix_len, workspace, stream=None) -> SharedBatch:
+    """Plans desc in `workspace` (wisp_shared_workspace_size bytes), once for all layers of a step.
+    group_size, prefix_len: host sequences, one entry for each run of requests that share their first
+    prefix_len tokens (both None: none do)."""
+    _check_desc(desc)
+    wp, wn = _ws(workspace)
+    if desc.page_table is not None and desc.B > 0 and desc.page_table.device != workspace.device:
+        raise ValueError(f"desc.page_table: on {desc.page_table.device}, the workspace on {workspace.device}")
+    n, ps, pp, _keep = _groups(group_size, prefix_len)
+    c = wisp_shared_batch()
+    with _On(workspace.device):
+        _ok(lib.wisp_shared_plan(C.byref(model), C.byref(desc.c), n, ps, pp, wp, wn, C.byref(c), _stream(stream)))
+    return SharedBatch(c, model, desc, workspace)
+
+
+def _shared_check(batch: SharedBatch, kv: KVPool, *tensors):
+    if tuple(kv.k.shape[2:]) != batch.page or kv.k.dtype != batch.dtype or kv.v.dtype != batch.dtype:
+        raise ValueError(f"kv: pages of {tuple(kv.k.shape[2:])} {kv.k.dtype}, expected {batch.page} {batch.dtype}")
+    for t in (kv.k, kv.v) + tensors:
+        if t is not None and t.device != batch.device:
+            raise ValueError(f"a tensor on {t.device}, the batch was planned on {batch.device}")
+
+
+def wisp_attention_shared(batch: SharedBatch, kv: KVPool, q, out, lse=None, stream=None):
+    """wisp_attention over layer 0 of kv (kv.layer(l) for another): q and out [rows][n_q][head_dim] of the
+    model's dtype, lse fp32 [rows][n_q] or None."""
+    pq, po = _dev(q, "q", batch.q_numel, dtype=batch.dtype), _dev(out, "out", batch.q_numel, dtype=batch.dtype)
+    pl = None if lse is None else _dev(lse, "lse", batch.heads, dtype=_f32())
+    _shared_check(batch, kv, q, out, lse)
+    with _On(batch.device):
+        _ok(lib.wisp_attention_shared(C.byref(batch.c), C.byref(kv.c), pq, po, pl, _stream(stream)))
+
+
+def wisp_attention_mass(batch: SharedBatch, kv: KVPool, q, lse, mass, prev=None, decay: float = 1.0, count=None, stream=None):
+    """mass = decay * prev + the attention weight that each token of layer 0 of kv gets from the batch's rows:
+    mass and prev fp32 [n_blocks][n_kv][16] (prev may be mass, or None), count int32 [B] or None."""
+    n = kv.c.n_blocks * batch.page[0] * PAGE
+    pq, pl = _dev(q, "q", batch.q_numel, dtype=batch.dtype), _dev(lse, "lse", batch.heads, dtype=_f32())
+    pm = _dev(mass, "mass", n, dtype=_f32())
+    pp = None if prev is None else _dev(prev, "prev", n, dtype=_f32())
+    pc = None if count is None else _dev(count, "count", batch.B, dtype=_i32())
+    _shared_check(batch, kv, q, lse, mass, prev, count)
+    with _On(batch.device):
+        _ok(lib.wisp_attention_mass(C.byref(batch.c), C.byref(kv.c), pq, pl, pc, decay, pp, pm, _stream(stream)))
+
+
+def wisp_kv_evict_workspace_size(model: wisp_model, desc: BatchDesc) -> int:
+    return int(lib.wisp_kv_evict_workspace_size(C.byref(model), C.byref(desc.c)))
+
+
+def wisp_kv_evict(model: wisp_model, kv: KVPool, desc: BatchDesc, keep, mass, kept, workspace, sink=None, recent=None, to_table=None,
+                  stream=None):
+    """Keeps keep[i] of request i's cached tokens in every layer and kv head: the first sink[i], the last
+    recent[i] and those of greatest mass (fp32 [n_layers][n_blocks][n_kv][16]), moved together into the pages of
+    to_table (int32 [B][stride]; None: in place).  kept: int32 [n_layers][n_kv][sum of min(keep, ctx_len)], their
+    old positions.  keep, sink, recent: host sequences; workspace: wisp_kv_evict_workspace_size bytes."""
+    _check_desc(desc)
+    _check_kv(model, kv, model.n_layers)
+    B = desc.B
+    (ka, pk), (sa, ps), (ra, pr) = (_host_i32(x, w, B) for x, w in ((keep, "keep"), (sink, "sink"), (recent, "recent")))
+    if ka is None:
+        raise ValueError("keep: expected a sequence")
+    if tuple(kv.k.shape[2:]) != (model.n_kv_heads, PAGE * model.head_dim):
+        raise ValueError(f"kv: pages of {tuple(kv.k.shape[2:])}, expected {(model.n_kv_heads, PAGE * model.head_dim)}")
+    total = int(np.minimum(ka.astype(np.int64), desc.ctx_len).clip(min=0).sum())
+    layers = model.n_layers * model.n_kv_heads
+    pm = _dev(mass, "mass", layers * kv.c.n_blocks * PAGE, dtype=_f32())
+    pe = _dev(kept, "kept", layers * total, dtype=_i32())
+    pt, stride = None, 0
+    if to_table is not None:
+        pt = _dev(to_table, "to_table", dtype=_i32())
+        if to_table.dim() != 2 or to_table.shape[0] < B:
+            raise ValueError(f"to_table: expected [>= {B}][stride], got {tuple(to_table.shape)}")
+        stride = to_table.shape[1]
+    wp, wn = _ws(workspace)
+    for t in (kv.k, kv.v, mass, kept, to_table, workspace, desc.page_table if B > 0 else None):
+        if t is not None and t.device != kv.k.device:
+            raise ValueError(f"a tensor on {t.device}, kv on {kv.k.device}")
+    with _On(kv.k.device):
+        _ok(lib.wisp_kv_evict(C.byref(model), C.byref(kv.c), C.byref(desc.c), pk, ps, pr, pt, stride, pm, pe, wp, wn, _stream(stream)))
 
 
 def wisp_uniform(rng_seed: int, req_id: int, tag: int, row: int, n: int, out, stream=None):

@@ -1,0 +1,207 @@
+// The attention weight that every cached token gets from a batch's rows: for token t and kv head h the sum
+// over rows r that see t, and query heads g of h, of exp(q . k_t / sqrt(head_dim) - lse).
+#include <algorithm>
+
+#include "../../include/wisp.h"
+#include "kernels.h"
+#include "shared.h"
+#include "shared_tile.h"
+#include "wave_reduce.h"
+
+namespace wisp {
+
+namespace {
+
+struct MassArgs {
+  const MassItem *items;
+  const int32_t *page_table, *row;      // row: (request, row in it) of every row
+  const void *k, *q;
+  const float *lse;
+  const int32_t *count;
+  const float *prev;
+  float *mass, *part;
+  int *err;
+  int pt_stride, n_blocks, nq, nkv;
+  float scale, decay;
+};
+
+// A token's new weight: what it had, less the decay, if it was cached before, and what it got
+__device__ __forceinline__ void put_mass(const int32_t *page_table, int pt_stride, int n_blocks, int nkv, int kvh, int table, int t,
+                                         bool old, float decay, const float *prev, float got, float *mass, int *err) {
+  const int b = page_table[(int64_t)table * pt_stride + (t >> 4)];
+  if (b < 0 || b >= n_blocks) {
+    flag_error(err, kErrBlock);
+    return;
+  }
+  const int64_t at = ((int64_t)b * nkv + kvh) * kPage + (t & 15);
+  mass[at] = old && prev ? __builtin_fmaf(decay, prev[at], got) : got;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mass_kernel(MassArgs a) {
+  constexpr int KB = HD / 16, PIECES = KB * (int)sizeof(T) / 2;   // 1 KiB pieces of a row tile in operand order
+  __shared__ uint4 rows_of[2][PIECES][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int lc = lane & 31, hf = lane >> 5;
+  const int kvh = blockIdx.x % a.nkv;
+  const MassItem it = a.items[blockIdx.x / a.nkv];
+  const int G = a.nq / a.nkv, rows = it.nrow * G;
+  const int tp = it.t0 + wave * kTile, tq = min(tp, (it.t1 - 1) & ~15);   // this wave's tokens; past the end the last page
+  // rows past those that count give nothing
+  int counted = it.nrow;
+  if (a.count && it.req >= 0) counted = min(max(a.count[it.req], 0), it.nrow);
+  const int r_end = min(it.r1, counted * G);
+  Op8<T> kf[KB];
+  {
+    const int32_t *ids = a.page_table + (int64_t)it.table * a.pt_stride;
+    const int b = ids[min((tq >> 4) + ((lane >> 4) & 1), (it.t1 - 1) >> 4)];
+    const T *kt = static_cast<const T *>(a.k) + ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * (kPage * HD);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_off(lane, kb));
+  }
+  const float c_log2 = a.scale * kLog2e;
+  floatx16 acc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+  // a row tile's operands straight into LDS; its rows' lse and how far they see, in registers
+  struct Rows {
+    float lse;
+    int lim;                             // tokens that the lane's row sees; 0: it does not count
+  };
+  auto bring = [&](int r, int b) __attribute__((always_inline)) {
+    const int f = min(r + lc, rows - 1);
+    const T *from = static_cast<const T *>(a.q) + ((int64_t)(it.row0 + f / G) * a.nq + kvh * G + f % G) * HD + 8 * hf;
+#pragma unroll
+    for (int x = 0; x < (PIECES + 3) / 4; ++x) {
+      const int u = wave + 4 * x;
+      if (PIECES % 4 == 0 || u < PIECES)
+        lds_dma16(reinterpret_cast<const char *>(from + 16 * (u / ((int)sizeof(T) / 2))) + 16 * (u % ((int)sizeof(T) / 2)), &rows_of[b][u][0]);
+    }
+  };
+  auto figures = [&](int r) __attribute__((always_inline)) {
+    const int f = min(r + lc, rows - 1), j = f / G;
+    Rows w;
+    w.lse = a.lse[(int64_t)(it.row0 + j) * a.nq + kvh * G + f % G];
+    bool on = r + lc < r_end;
+    if (a.count && it.req < 0) {
+      const int2 of = *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + j));
+      on = on && of.y < a.count[of.x];
+    }
+    w.lim = on ? it.ctx + j + 1 : 0;
+    return w;
+  };
+  if (it.r0 < r_end) {
+    bring(it.r0, 0);
+    Rows w = figures(it.r0);
+    int b = 0;
+    for (int r = it.r0; r < r_end; r += kTile, b ^= 1) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      const Rows now = w;
+      if (r + kTile < r_end) {
+        bring(r + kTile, b ^ 1);
+        w = figures(r + kTile);
+      }
+      floatx16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        Op8<T> x;
+#pragma unroll
+        for (int y = 0; y < (int)sizeof(T) / 2; ++y) x.v[y] = rows_of[b][kb * ((int)sizeof(T) / 2) + y][lane];
+        s = mma(s, kf[kb], x);
+      }
+      const float l2 = now.lse * kLog2e;
+      if (__builtin_amdgcn_ballot_w64(now.lim < tp + kTile || fabsf(l2) > kFarScore)) {
+        // rows that do not see a token, or do not count; and scores so large that the roundings on both sides
+        // of the difference may make it positive
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float e = __builtin_fmaf(s[i], c_log2, -l2);
+          if (fabsf(l2) > kFarScore) e = e > 0.f ? 0.f : e;
+          e = __builtin_amdgcn_exp2f(e);
+          acc[i] += tp + reg_token(lane, i) < now.lim ? e : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -l2));
+      }
+    }
+  }
+  // over the rows: the lanes of a half
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float v = acc[i];
+    v += dpp<kXor1>(v);
+    v += dpp<kXor2>(v);
+    v += dpp<kHalfMirror>(v);
+    v += dpp<kMirror>(v);
+    v = xor16_sum(v);
+    sum = lc == i ? v : sum;
+  }
+  const int t = tp + reg_token(lane, lc & 15);
+  if (lc >= 16 || t >= it.t1) return;
+  if (it.part >= 0) {
+    a.part[(int64_t)it.part + (int64_t)kvh * it.step + t - it.t0] = sum;
+    return;
+  }
+  put_mass(a.page_table, a.pt_stride, a.n_blocks, a.nkv, kvh, it.table, t, t < it.ctx, a.decay, a.prev, sum, a.mass, a.err);
+}
+
+__global__ __launch_bounds__(kMassBlock) void mass_join_kernel(const MassJoin *joins, const float *part, const int32_t *page_table,
+                                                               int pt_stride, int n_blocks, int nkv, float decay, const float *prev,
+                                                               float *mass, int *err) {
+  const int kvh = blockIdx.x % nkv;
+  const MassJoin j = joins[blockIdx.x / nkv];
+  const int t = j.t0 + threadIdx.x;
+  if (t >= j.t1) return;
+  float got = 0.f;
+  for (int p = 0; p < j.parts; ++p) got += part[(int64_t)j.part + (int64_t)kvh * j.step + (int64_t)p * kMassBlock + threadIdx.x];
+  put_mass(page_table, pt_stride, n_blocks, nkv, kvh, j.table, t, t < j.ctx, decay, prev, got, mass, err);
+}
+
+}  // namespace
+
+void shared_mass(const SharedPlan &p, const SharedCache &c, const void *q, const float *lse, const int32_t *count, float decay,
+                 const float *prev, float *mass, int *err, hipStream_t s) {
+  MassArgs a{};
+  a.items = reinterpret_cast<const MassItem *>(p.ws + p.w_mass);
+  a.page_table = p.page_table;
+  a.row = reinterpret_cast<const int32_t *>(p.ws + p.w_row);
+  a.k = c.k;
+  a.q = q;
+  a.lse = lse;
+  a.count = count;
+  a.prev = prev;
+  a.mass = mass;
+  a.part = reinterpret_cast<float *>(p.ws + p.w_pm);
+  a.err = err;
+  a.pt_stride = p.pt_stride;
+  a.n_blocks = c.n_blocks;
+  a.nq = p.nq;
+  a.nkv = p.nkv;
+  a.scale = 1.0f / sqrtf((float)p.hd);
+  a.decay = decay;
+  auto go = [&](auto kernel) { launch(kernel, p.n_mass * p.nkv, 256, 0, s, a); };
+  if (p.dtype == WISP_BF16) {
+    if (p.hd == 128) go(mass_kernel<uint16_t, 128>);
+    else go(mass_kernel<uint16_t, 64>);
+  } else {
+    switch (p.hd) {
+      case 32: go(mass_kernel<float, 32>); break;
+      case 64: go(mass_kernel<float, 64>); break;
+      case 96: go(mass_kernel<float, 96>); break;
+      case 128: go(mass_kernel<float, 128>); break;
+      case 160: go(mass_kernel<float, 160>); break;
+      case 192: go(mass_kernel<float, 192>); break;
+      case 224: go(mass_kernel<float, 224>); break;
+      default: go(mass_kernel<float, 256>);
+    }
+  }
+  if (p.n_mass_join > 0)
+    launch(mass_join_kernel, p.n_mass_join * p.nkv, kMassBlock, 0, s, reinterpret_cast<const MassJoin *>(p.ws + p.w_mass_join),
+           (const float *)a.part, p.page_table, p.pt_stride, c.n_blocks, p.nkv, decay, prev, mass, err);
+}
+
+}  // namespace wisp

@@ -1,0 +1,419 @@
+// Attention of a batch whose requests share prefixes: the rows of a group attend to their common tokens
+// together, each request's rows to its own, and the partial results of a row are joined.
+#include <algorithm>
+
+#include "../../include/wisp.h"
+#include "kernels.h"
+#include "shared.h"
+#include "shared_tile.h"
+
+namespace wisp {
+
+namespace {
+
+struct SharedArgs {
+  const SharedItem *items;
+  const int32_t *page_table;
+  const void *k, *v, *q;
+  void *out;
+  float *lse, *part_o, *part_ml;
+  int *err;
+  int pt_stride, n_blocks, nq, nkv;
+  float scale;
+};
+
+template <typename T, int HD>
+struct Geo {
+  static constexpr int KB = HD / 16, MB = HD / 32;            // steps of the contraction; blocks of output dims
+  static constexpr int PAGE = kPage * HD, PAGE_BYTES = PAGE * (int)sizeof(T);
+  static constexpr int STAGE = PAGE_BYTES <= 4096 ? 4 : 2;    // pages staged at a time
+  static constexpr int STAGE_BYTES = STAGE * 2 * PAGE_BYTES;
+  static constexpr int LDJ = HD + 4;                          // a row of accumulators in LDS, in floats
+  static constexpr int SMEM = std::max(2 * STAGE_BYTES, 4 * kTile * LDJ * 4);
+  static constexpr bool AHEAD = sizeof(T) == 2 || HD <= 64;   // registers hold the operands of a tile ahead
+  static constexpr int WGS = AHEAD ? 2 : 1;
+};
+
+// maximum that passes over a NaN (the row's sum holds it)
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(SharedArgs a) {
+  using G_ = Geo<T, HD>;
+  constexpr int KB = G_::KB, MB = G_::MB, PAGE = G_::PAGE, PAGE_BYTES = G_::PAGE_BYTES, STAGE = G_::STAGE, LDJ = G_::LDJ;
+  __shared__ __attribute__((aligned(1024))) char smem[G_::SMEM];
+  __shared__ float2 sh_ml[4][kTile];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int lc = lane & 31, hf = lane >> 5;
+  const int kvh = blockIdx.x % a.nkv;                 // neighbouring workgroups, on other XCDs: other kv heads
+  const SharedItem it = a.items[blockIdx.x / a.nkv];
+  const int G = a.nq / a.nkv, rows = it.nrow * G;
+  const bool wide = it.tiles > 2;                     // one tile of rows a wave; else the waves share the tokens
+  const int parts = wide ? 1 : 4 / it.tiles, tile = wide ? min(wave, it.tiles - 1) : wave % it.tiles;
+  const int part = wide ? 0 : wave / it.tiles;
+  const int fr0 = (it.tile0 + tile) * kTile, fr = min(fr0 + lc, rows - 1);   // padding rows: a real one
+  const int64_t q_at = ((int64_t)(it.row0 + fr / G) * a.nq + kvh * G + fr % G) * HD + 8 * hf;
+  Op8<T> qf[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) qf[kb] = load_op(static_cast<const T *>(a.q) + q_at + 16 * kb);
+  const int lim = min(it.t1, it.ctx + fr / G + 1);    // tokens that this lane's row sees
+  const int open = min(it.t1, it.ctx + __builtin_amdgcn_readfirstlane(fr0 / G) + 1);   // that every row of the tile sees
+  const float c_log2 = a.scale * kLog2e, tau = 8.0f / c_log2;
+  float m_run = -INFINITY, l_run = 0.f;
+  floatx16 o[MB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[mb][i] = 0.f;
+
+  // Online softmax of a tile's scores to probabilities.  The running maximum rises only by more
+  // than 2^8 in the probabilities, so the accumulators are rescaled on few tiles.
+  auto softmax = [&](floatx16 &s, int tp) __attribute__((always_inline)) {
+    if (tp + kTile > open) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (tp + reg_token(lane, i) >= lim) s[i] = -INFINITY;
+    }
+    float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) mx = max3(mx, s[i], s[i + 1]);
+    mx = xor32_max(fmaxf(mx, s[15]));
+    const bool grow = mx > m_run + tau;
+    if (__builtin_amdgcn_ballot_w64(grow)) {
+      const float alpha = grow ? __builtin_amdgcn_exp2f((m_run - mx) * c_log2) : 1.0f;
+      m_run = grow ? mx : m_run;
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
+    }
+    const float m = m_run == -INFINITY ? 0.f : m_run, mc = m * c_log2;
+    if (__builtin_amdgcn_ballot_w64(fabsf(mc) > kFarScore)) {
+      // of large scores the rounding of m x log2(e) would be most of their difference
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - m) * c_log2);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -mc));
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += s[i];
+    l_run += sum;                                     // this lane's tokens: the halves are added at the end
+  };
+  // O += P V of a tile, V's operands from v(page, block); page_at(page): where its V lies
+  auto weigh = [&](const floatx16 &p, int tp, auto &&v, auto &&page_at) __attribute__((always_inline)) {
+    if (tp + kTile > open) {
+      // slots past the last token may hold anything; and a token that some rows do not see may be
+      // infinite or NaN, which a product with a probability of 0 would hand on to them
+      bool special = false;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          Op8<T> x = v(g, mb);
+          keep_first(x, it.t1 - (tp + 16 * g + 8 * hf));
+          special |= any_special(x);
+        }
+      if (__builtin_amdgcn_ballot_w64(special)) {
+#pragma unroll 1
+        for (int t = 0; t < kTile; ++t) {
+          float w = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w = (t >> 4) * 8 + (t & 7) == i ? p[i] : w;
+          w = __shfl(w, lc + 32 * ((t >> 3) & 1));
+          if (tp + t >= it.t1) break;
+          const T *from = page_at(t >> 4);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = as_float(from[v_page_off(t & 15, 32 * mb + 8 * (i >> 2) + 4 * hf + (i & 3))]);
+              o[mb][i] = tp + t < lim ? __builtin_fmaf(w, x, o[mb][i]) : o[mb][i];
+            }
+        }
+        return;
+      }
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[8 * g + i];
+        Op8<T> pb;
+        to_op(pb, e);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          Op8<T> x = v(g, mb);
+          keep_first(x, it.t1 - (tp + 16 * g + 8 * hf));
+          o[mb] = mma(o[mb], x, pb);
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = p[8 * g + i];
+      Op8<T> pb;
+      to_op(pb, e);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], v(g, mb), pb);
+    }
+  };
+
+  const_ids_t *ids = const_ids(a.page_table + (int64_t)it.table * a.pt_stride);
+  const int page0 = it.t0 >> 4, page_end = (it.t1 - 1) >> 4;       // pages past the end: the last
+  auto place = [&](int b) __attribute__((always_inline)) {
+    return ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * PAGE;
+  };
+  // block ids out of range are reported (and clamped above)
+  for (int x = page0 + threadIdx.x; x <= page_end; x += 256) {
+    const int b = a.page_table[(int64_t)it.table * a.pt_stride + x];
+    if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
+  }
+  const T *kp = static_cast<const T *>(a.k), *vp = static_cast<const T *>(a.v);
+  const int n_tiles = (it.t1 - it.t0 + kTile - 1) / kTile;
+
+  if (wide) {
+    // pages go straight into LDS, one stage ahead; a page lies there as it does in memory
+    constexpr int UNITS = STAGE * 2 / 4, CHUNKS = PAGE_BYTES / 1024;      // pages (K or V) of a wave a stage
+    constexpr int TILES = STAGE / 2;
+    const int stages = (n_tiles + TILES - 1) / TILES;
+    auto id_of = [&](int s) __attribute__((always_inline)) { return ids[min(page0 + s * STAGE + (STAGE == 4 ? wave : wave >> 1), page_end)]; };
+    auto bring = [&](int s, int id) __attribute__((always_inline)) {
+      const int64_t at = place(id);
+      char *to = smem + (s & 1) * G_::STAGE_BYTES;
+#pragma unroll
+      for (int x = 0; x < UNITS; ++x) {
+        const int u = wave * UNITS + x;               // page u / 2, K or V
+        const char *from = reinterpret_cast<const char *>((u & 1 ? vp : kp) + at) + lane * 16;
+#pragma unroll
+        for (int y = 0; y < CHUNKS; ++y) lds_dma16(from + y * 1024, to + u * PAGE_BYTES + y * 1024);
+      }
+    };
+    bring(0, id_of(0));
+    int next = id_of(1);
+    for (int s = 0; s < stages; ++s) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (s + 1 < stages) bring(s + 1, next);
+      next = id_of(s + 2);
+      const T *buf = reinterpret_cast<const T *>(smem + (s & 1) * G_::STAGE_BYTES);
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        const int tp = it.t0 + (s * TILES + x) * kTile;
+        if (tp >= it.t1) break;
+        const T *kt = buf + (4 * x + 2 * ((lane >> 4) & 1)) * PAGE;      // this lane's K page: units are page, K or V
+        floatx16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) sc = mma(sc, load_op(kt + k_op_off(lane, kb)), qf[kb]);
+        softmax(sc, tp);
+        weigh(sc, tp, [&](int g, int mb) __attribute__((always_inline)) { return load_op(buf + (4 * x + 2 * g + 1) * PAGE + v_op_off(lane, mb)); },
+              [&](int g) { return buf + (4 * x + 2 * g + 1) * PAGE; });
+      }
+    }
+  } else {
+    // the waves of a row tile take its token tiles in turn, operands straight from memory, a tile ahead
+    Op8<T> kf[KB], vf[2][MB];
+    const T *vb[2];
+    int b0 = 0, b1 = 0;
+    auto ids_of = [&](int x) __attribute__((always_inline)) {
+      b0 = ids[min(page0 + 2 * x, page_end)];
+      b1 = ids[min(page0 + 2 * x + 1, page_end)];
+    };
+    auto load_k = [&]() __attribute__((always_inline)) {
+      const T *kt = kp + ((lane >> 4) & 1 ? place(b1) : place(b0));
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_off(lane, kb));
+    };
+    auto load_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) vf[g][mb] = load_op(vb[g] + v_op_off(lane, mb));
+    };
+    if (part < n_tiles) {
+      ids_of(part);
+      if constexpr (G_::AHEAD) load_k();
+      vb[0] = vp + place(b0);
+      vb[1] = vp + place(b1);
+      if constexpr (G_::AHEAD) load_v();
+    }
+    for (int x = part; x < n_tiles; x += parts) {
+      const int tp = it.t0 + x * kTile;
+      if constexpr (!G_::AHEAD) {
+        ids_of(x);
+        load_k();
+        vb[0] = vp + place(b0);
+        vb[1] = vp + place(b1);
+      } else {
+        ids_of(x + parts);
+      }
+      floatx16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) sc = mma(sc, kf[kb], qf[kb]);
+      if constexpr (G_::AHEAD) load_k();               // past the end: the last pages once more
+      softmax(sc, tp);
+      if constexpr (!G_::AHEAD) load_v();
+      weigh(sc, tp, [&](int g, int mb) __attribute__((always_inline)) { return vf[g][mb]; }, [&](int g) { return vb[g]; });
+      vb[0] = vp + place(b0);
+      vb[1] = vp + place(b1);
+      if constexpr (G_::AHEAD) load_v();
+    }
+  }
+
+  // through LDS: 8 dims of a row a thread, the waves of a row tile added in order
+  __syncthreads();
+  float(*jo)[kTile][LDJ] = reinterpret_cast<float(*)[kTile][LDJ]>(smem);
+  const float l = xor32_sum(l_run);
+  if (hf == 0) sh_ml[wave][lc] = make_float2(m_run, l);
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<floatx4 *>(&jo[wave][lc][32 * mb + 8 * x + 4 * hf]) =
+          floatx4{o[mb][4 * x], o[mb][4 * x + 1], o[mb][4 * x + 2], o[mb][4 * x + 3]};
+  __syncthreads();
+  constexpr int CH = HD / 8;
+  for (int u = threadIdx.x; u < it.tiles * kTile * CH; u += 256) {
+    const int c0 = u % CH * 8, r = u / CH % kTile, t = u / CH / kTile;
+    const int f = (it.tile0 + t) * kTile + r;
+    if (f >= rows) continue;
+    float m = -INFINITY, den = 0.f;
+    for (int x = 0; x < parts; ++x) m = fmaxf(m, sh_ml[t + x * it.tiles][r].x);
+    floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
+    for (int x = 0; x < parts; ++x) {
+      const float2 ml = sh_ml[t + x * it.tiles][r];
+      if (ml.x == -INFINITY) {
+        den += ml.y;                                  // 0, or NaN of a row's NaN scores
+        continue;
+      }
+      const float w = __builtin_amdgcn_exp2f((ml.x - m) * c_log2);
+      den += ml.y * w;
+      y += *reinterpret_cast<const floatx4 *>(&jo[t + x * it.tiles][r][c0]) * w;
+      z += *reinterpret_cast<const floatx4 *>(&jo[t + x * it.tiles][r][c0 + 4]) * w;
+    }
+    if (it.part >= 0) {
+      const int64_t slot = ((int64_t)it.part + (int64_t)kvh * it.step + t) * kTile + r;
+      float *to = a.part_o + slot * HD + c0;
+      *reinterpret_cast<floatx4 *>(to) = y;
+      *reinterpret_cast<floatx4 *>(to + 4) = z;
+      if (c0 == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(m, den);
+      continue;
+    }
+    const int64_t row = (int64_t)(it.row0 + f / G) * a.nq + kvh * G + f % G;
+    const float inv = 1.0f / den;
+    y *= inv;
+    z *= inv;
+    T *to = static_cast<T *>(a.out) + row * HD + c0;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]), pack2bf_rne(z[0], z[1]), pack2bf_rne(z[2], z[3]));
+    } else {
+      *reinterpret_cast<floatx4 *>(to) = y;
+      *reinterpret_cast<floatx4 *>(to + 4) = z;
+    }
+    if (a.lse && c0 == 0) a.lse[row] = m * a.scale + logf(den);
+  }
+}
+
+// The partial results of a row, joined in order: its own segment's, then its group's.  A workgroup for
+// each row, a thread for 8 dims of a head.
+template <typename T>
+__global__ __launch_bounds__(512) void shared_join_kernel(const int32_t *row_req, const SharedJoin *joins, const float *part_o,
+                                                          const float *part_ml, T *out, float *lse, int nq, int nkv, int hd,
+                                                          float scale) {
+  const SharedJoin j = joins[row_req[2 * blockIdx.x]];
+  if (j.own + j.pre < 2) return;                      // written as it was computed
+  const int G = nq / nkv, ch = hd / 8, n = j.own + j.pre;
+  const float c_log2 = scale * kLog2e;
+  for (int u = threadIdx.x; u < nq * ch; u += blockDim.x) {
+    const int head = u / ch, c0 = u % ch * 8, kvh = head / G;
+    const int f = (blockIdx.x - j.row0) * G + head % G;
+    auto slot = [&](int p) {
+      return p < j.own ? ((int64_t)j.own_at + ((int64_t)p * nkv + kvh) * j.own_tiles) * kTile + f
+                       : ((int64_t)j.pre_at + ((int64_t)(p - j.own) * nkv + kvh) * j.pre_tiles) * kTile + j.pre_row + f;
+    };
+    float m = -INFINITY, den = 0.f;
+    for (int p = 0; p < n; ++p) m = fmaxf(m, part_ml[slot(p) * 2]);
+    floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
+    for (int p = 0; p < n; ++p) {
+      const int64_t s = slot(p);
+      const float2 ml = *reinterpret_cast<const float2 *>(part_ml + s * 2);
+      if (ml.x == -INFINITY) {
+        den += ml.y;
+        continue;
+      }
+      const float w = __builtin_amdgcn_exp2f((ml.x - m) * c_log2);
+      den += ml.y * w;
+      y += *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0) * w;
+      z += *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0 + 4) * w;
+    }
+    const int64_t row = (int64_t)blockIdx.x * nq + head;
+    const float inv = 1.0f / den;
+    y *= inv;
+    z *= inv;
+    T *to = out + row * hd + c0;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]), pack2bf_rne(z[0], z[1]), pack2bf_rne(z[2], z[3]));
+    } else {
+      *reinterpret_cast<floatx4 *>(to) = y;
+      *reinterpret_cast<floatx4 *>(to + 4) = z;
+    }
+    if (lse && c0 == 0) lse[row] = m * scale + logf(den);
+  }
+}
+
+}  // namespace
+
+int shared_wgs_per_cu(int dtype, int hd) { return dtype == WISP_BF16 || hd <= 64 ? 2 : 1; }
+
+void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, void *out, float *lse, int *err, hipStream_t s) {
+  SharedArgs a{};
+  a.items = reinterpret_cast<const SharedItem *>(p.ws + p.w_items);
+  a.page_table = p.page_table;
+  a.k = c.k;
+  a.v = c.v;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.part_o = reinterpret_cast<float *>(p.ws + p.w_po);
+  a.part_ml = reinterpret_cast<float *>(p.ws + p.w_pml);
+  a.err = err;
+  a.pt_stride = p.pt_stride;
+  a.n_blocks = c.n_blocks;
+  a.nq = p.nq;
+  a.nkv = p.nkv;
+  a.scale = 1.0f / sqrtf((float)p.hd);
+  auto go = [&](auto kernel) { launch(kernel, p.n_items * p.nkv, 256, 0, s, a); };
+  if (p.dtype == WISP_BF16) {
+    if (p.hd == 128) go(shared_attn_kernel<uint16_t, 128>);
+    else go(shared_attn_kernel<uint16_t, 64>);
+  } else {
+    switch (p.hd) {
+      case 32: go(shared_attn_kernel<float, 32>); break;
+      case 64: go(shared_attn_kernel<float, 64>); break;
+      case 96: go(shared_attn_kernel<float, 96>); break;
+      case 128: go(shared_attn_kernel<float, 128>); break;
+      case 160: go(shared_attn_kernel<float, 160>); break;
+      case 192: go(shared_attn_kernel<float, 192>); break;
+      case 224: go(shared_attn_kernel<float, 224>); break;
+      default: go(shared_attn_kernel<float, 256>);
+    }
+  }
+  if (!p.joined) return;
+  const int32_t *row = reinterpret_cast<const int32_t *>(p.ws + p.w_row);
+  const SharedJoin *joins = reinterpret_cast<const SharedJoin *>(p.ws + p.w_join);
+  const int threads = std::min(512, (p.nq * p.hd / 8 + 63) / 64 * 64);
+  if (p.dtype == WISP_BF16)
+    launch(shared_join_kernel<uint16_t>, p.rows, threads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml,
+           static_cast<uint16_t *>(out), lse, p.nq, p.nkv, p.hd, a.scale);
+  else
+    launch(shared_join_kernel<float>, p.rows, threads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml,
+           static_cast<float *>(out), lse, p.nq, p.nkv, p.hd, a.scale);
+}
+
+}  // namespace wisp
