@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
     const int b = ids[min((tq >> 4) + ((lane >> 4) & 1), (it.t1 - 1) >> 4)];
     const T *kt = static_cast<const T *>(a.k) + ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * (kPage * HD);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_off(lane, kb));
+    for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_lane(lane) + k_op_step(kb));
   }
   const float c_log2 = a.scale * kLog2e;
   floatx16 acc;

@@ -1,6 +1,7 @@
 // Attention of a batch whose requests share prefixes: the rows of a group attend to their common tokens
 // together, each request's rows to its own, and the partial results of a row are joined.
 #include <algorithm>
+#include <climits>
 
 #include "../../include/wisp.h"
 #include "kernels.h"
@@ -68,12 +69,21 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 
   // Online softmax of a tile's scores to probabilities.  The running maximum rises only by more
   // than 2^8 in the probabilities, so the accumulators are rescaled on few tiles.
-  auto softmax = [&](floatx16 &s, int tp) __attribute__((always_inline)) {
-    if (tp + kTile > open) {
+  float mc = 0.f;                                     // m_run in base 2; 0 while the row has seen nothing
+  bool far = false;                                   // of some row it is so large that its rounding counts
+  auto exponentials = [&](floatx16 &s) __attribute__((always_inline)) {
+    float off = -mc;
+    if (far) {
+      // the rounding of m x log2(e) would be most of the scores' difference: that first
+      const float m = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (tp + reg_token(lane, i) >= lim) s[i] = -INFINITY;
+      for (int i = 0; i < 16; ++i) s[i] -= m;
+      off = 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, off));
+  };
+  auto softmax = [&](floatx16 &s) __attribute__((always_inline)) {
     float mx = max3(s[0], s[1], s[2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) mx = max3(mx, s[i], s[i + 1]);
@@ -85,81 +95,23 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       l_run *= alpha;
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
+      mc = m_run == -INFINITY ? 0.f : m_run * c_log2;
+      far = __builtin_amdgcn_ballot_w64(fabsf(mc) > kFarScore) != 0;
     }
-    const float m = m_run == -INFINITY ? 0.f : m_run, mc = m * c_log2;
-    if (__builtin_amdgcn_ballot_w64(fabsf(mc) > kFarScore)) {
-      // of large scores the rounding of m x log2(e) would be most of their difference
-#pragma clang fp contract(off)
+    exponentials(s);
+    float sum[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f((s[i] - m) * c_log2);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -mc));
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += s[i];
-    l_run += sum;                                     // this lane's tokens: the halves are added at the end
+    for (int i = 4; i < 16; ++i) sum[i & 3] += s[i];
+    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);   // this lane's tokens: the halves are added at the end
   };
-  // O += P V of a tile, V's operands from v(page, block); page_at(page): where its V lies
-  auto weigh = [&](const floatx16 &p, int tp, auto &&v, auto &&page_at) __attribute__((always_inline)) {
-    if (tp + kTile > open) {
-      // slots past the last token may hold anything; and a token that some rows do not see may be
-      // infinite or NaN, which a product with a probability of 0 would hand on to them
-      bool special = false;
+  // eight probabilities of a page as an operand
+  auto probs = [&](const floatx16 &p, int g) __attribute__((always_inline)) {
+    float e[8];
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          Op8<T> x = v(g, mb);
-          keep_first(x, it.t1 - (tp + 16 * g + 8 * hf));
-          special |= any_special(x);
-        }
-      if (__builtin_amdgcn_ballot_w64(special)) {
-#pragma unroll 1
-        for (int t = 0; t < kTile; ++t) {
-          float w = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) w = (t >> 4) * 8 + (t & 7) == i ? p[i] : w;
-          w = __shfl(w, lc + 32 * ((t >> 3) & 1));
-          if (tp + t >= it.t1) break;
-          const T *from = page_at(t >> 4);
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float x = as_float(from[v_page_off(t & 15, 32 * mb + 8 * (i >> 2) + 4 * hf + (i & 3))]);
-              o[mb][i] = tp + t < lim ? __builtin_fmaf(w, x, o[mb][i]) : o[mb][i];
-            }
-        }
-        return;
-      }
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = p[8 * g + i];
-        Op8<T> pb;
-        to_op(pb, e);
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          Op8<T> x = v(g, mb);
-          keep_first(x, it.t1 - (tp + 16 * g + 8 * hf));
-          o[mb] = mma(o[mb], x, pb);
-        }
-      }
-      return;
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = p[8 * g + i];
-      Op8<T> pb;
-      to_op(pb, e);
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], v(g, mb), pb);
-    }
+    for (int i = 0; i < 8; ++i) e[i] = p[8 * g + i];
+    Op8<T> pb;
+    to_op(pb, e);
+    return pb;
   };
 
   const_ids_t *ids = const_ids(a.page_table + (int64_t)it.table * a.pt_stride);
@@ -173,75 +125,85 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
   }
   const T *kp = static_cast<const T *>(a.k), *vp = static_cast<const T *>(a.v);
+  const int k_lane = k_op_lane(lane), v_lane = v_op_lane(lane);
   const int n_tiles = (it.t1 - it.t0 + kTile - 1) / kTile;
+  int x = part;                                        // the next tile of this wave
 
   if (wide) {
-    // pages go straight into LDS, one stage ahead; a page lies there as it does in memory
+    // The tiles that every row of the item sees, in whole stages: pages go straight into LDS, one stage
+    // ahead; a page lies there as it does in memory.
     constexpr int UNITS = STAGE * 2 / 4, CHUNKS = PAGE_BYTES / 1024;      // pages (K or V) of a wave a stage
     constexpr int TILES = STAGE / 2;
-    const int stages = (n_tiles + TILES - 1) / TILES;
+    const int stages = max(0, min(it.t1, it.ctx + it.tile0 * kTile / G + 1) - it.t0) / (TILES * kTile);
     auto id_of = [&](int s) __attribute__((always_inline)) { return ids[min(page0 + s * STAGE + (STAGE == 4 ? wave : wave >> 1), page_end)]; };
     auto bring = [&](int s, int id) __attribute__((always_inline)) {
       const int64_t at = place(id);
       char *to = smem + (s & 1) * G_::STAGE_BYTES;
 #pragma unroll
-      for (int x = 0; x < UNITS; ++x) {
-        const int u = wave * UNITS + x;               // page u / 2, K or V
+      for (int u0 = 0; u0 < UNITS; ++u0) {
+        const int u = wave * UNITS + u0;              // page u / 2, K or V
         const char *from = reinterpret_cast<const char *>((u & 1 ? vp : kp) + at) + lane * 16;
 #pragma unroll
         for (int y = 0; y < CHUNKS; ++y) lds_dma16(from + y * 1024, to + u * PAGE_BYTES + y * 1024);
       }
     };
-    bring(0, id_of(0));
+    if (stages > 0) bring(0, id_of(0));
     int next = id_of(1);
     for (int s = 0; s < stages; ++s) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (s + 1 < stages) bring(s + 1, next);
       next = id_of(s + 2);
       const T *buf = reinterpret_cast<const T *>(smem + (s & 1) * G_::STAGE_BYTES);
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        const int tp = it.t0 + (s * TILES + x) * kTile;
-        if (tp >= it.t1) break;
-        const T *kt = buf + (4 * x + 2 * ((lane >> 4) & 1)) * PAGE;      // this lane's K page: units are page, K or V
+#pragma unroll 1
+      for (int y = 0; y < TILES; ++y) {
+        // units of a stage: page, K or V; this lane's K page of the tile
+        const T *tile_at = buf + 4 * y * PAGE, *kt = tile_at + 2 * ((lane >> 4) & 1) * PAGE + k_lane;
         floatx16 sc;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sc = mma(sc, load_op(kt + k_op_off(lane, kb)), qf[kb]);
-        softmax(sc, tp);
-        weigh(sc, tp, [&](int g, int mb) __attribute__((always_inline)) { return load_op(buf + (4 * x + 2 * g + 1) * PAGE + v_op_off(lane, mb)); },
-              [&](int g) { return buf + (4 * x + 2 * g + 1) * PAGE; });
+        for (int kb = 0; kb < KB; ++kb) sc = mma(sc, load_op(kt + k_op_step(kb)), qf[kb]);
+        softmax(sc);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Op8<T> pb = probs(sc, g);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], load_op(tile_at + (2 * g + 1) * PAGE + v_lane + v_op_block(mb)), pb);
+        }
       }
     }
-  } else {
-    // the waves of a row tile take its token tiles in turn, operands straight from memory, a tile ahead
+    x = stages * TILES;
+  }
+
+  // A wave by itself, operands straight from memory, a tile ahead: the waves of a row tile take its token
+  // tiles in turn; of a wide item each its rows' last tiles.
+  {
     Op8<T> kf[KB], vf[2][MB];
     const T *vb[2];
-    int b0 = 0, b1 = 0;
-    auto ids_of = [&](int x) __attribute__((always_inline)) {
-      b0 = ids[min(page0 + 2 * x, page_end)];
-      b1 = ids[min(page0 + 2 * x + 1, page_end)];
+    int b0 = 0, b1 = 0, later = INT_MAX;
+    auto ids_of = [&](int t) __attribute__((always_inline)) {
+      b0 = ids[min(page0 + 2 * t, page_end)];
+      b1 = ids[min(page0 + 2 * t + 1, page_end)];
     };
     auto load_k = [&]() __attribute__((always_inline)) {
-      const T *kt = kp + ((lane >> 4) & 1 ? place(b1) : place(b0));
+      const T *kt = kp + ((lane >> 4) & 1 ? place(b1) : place(b0)) + k_lane;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_off(lane, kb));
+      for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_step(kb));
     };
     auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) vf[g][mb] = load_op(vb[g] + v_op_off(lane, mb));
+        for (int mb = 0; mb < MB; ++mb) vf[g][mb] = load_op(vb[g] + v_lane + v_op_block(mb));
     };
-    if (part < n_tiles) {
-      ids_of(part);
+    if (x < n_tiles) {
+      ids_of(x);
       if constexpr (G_::AHEAD) load_k();
       vb[0] = vp + place(b0);
       vb[1] = vp + place(b1);
       if constexpr (G_::AHEAD) load_v();
     }
-    for (int x = part; x < n_tiles; x += parts) {
+    for (; x < n_tiles; x += parts) {
       const int tp = it.t0 + x * kTile;
       if constexpr (!G_::AHEAD) {
         ids_of(x);
@@ -256,13 +218,74 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) sc = mma(sc, kf[kb], qf[kb]);
+      // operands are asked for where those before them have been used: sooner, they would take registers of their own
+      __builtin_amdgcn_sched_barrier(0);
       if constexpr (G_::AHEAD) load_k();               // past the end: the last pages once more
-      softmax(sc, tp);
+      __builtin_amdgcn_sched_barrier(0);
+      const bool masked = tp + kTile > open;
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = tp + reg_token(lane, i) < lim ? sc[i] : -INFINITY;
+      }
+      softmax(sc);
       if constexpr (!G_::AHEAD) load_v();
-      weigh(sc, tp, [&](int g, int mb) __attribute__((always_inline)) { return vf[g][mb]; }, [&](int g) { return vb[g]; });
+      if (masked) {
+        // Slots past the last token may hold anything.  And a token that is there, but not seen by every row, may be
+        // infinite or NaN, which a product with a probability of 0 would hand on: from such a tile on V is left for later
+        bool special = false;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Keep<T> keep(it.t1 - (tp + 16 * g + 8 * hf));
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) {
+            keep.apply(vf[g][mb]);
+            special |= any_special(vf[g][mb]);
+          }
+        }
+        if (__builtin_amdgcn_ballot_w64(special)) later = min(later, x);
+      }
+      if (later > x) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Op8<T> pb = probs(sc, g);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], vf[g][mb], pb);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
       vb[0] = vp + place(b0);
       vb[1] = vp + place(b1);
       if constexpr (G_::AHEAD) load_v();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // V of the tiles that hold what some rows must not touch, token by token
+#pragma unroll 1
+    for (x = later; x < n_tiles; x += parts) {
+      const int tp = it.t0 + x * kTile;
+      ids_of(x);
+      load_k();
+      floatx16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) sc = mma(sc, kf[kb], qf[kb]);
+      exponentials(sc);
+#pragma unroll 1
+      for (int t = 0; t < kTile && tp + t < it.t1; ++t) {
+        float w = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w = (t >> 4) * 8 + (t & 7) == i ? sc[i] : w;
+        w = __shfl(w, lc + 32 * ((t >> 3) & 1));
+        const T *from = vp + place(t < kPage ? b0 : b1) + v_page_off(t & 15, 4 * hf);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float v = as_float(from[512 * mb + (i >> 3) * 256 + ((i >> 2) & 1) * 64 + (i & 3) * 8]);
+            asm volatile("" : "+v"(v));                // loaded by every lane: no branch around each load
+            o[mb][i] = tp + t < lim ? __builtin_fmaf(w, v, o[mb][i]) : o[mb][i];
+          }
+      }
     }
   }
 
@@ -320,51 +343,69 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   }
 }
 
-// The partial results of a row, joined in order: its own segment's, then its group's.  A workgroup for
-// each row, a thread for 8 dims of a head.
+// The partial results of a row, joined in order: its own segment's, then its group's.  A thread for 8 dims of a
+// head; the loads of kJoinParts results are in flight at once.
+constexpr int kJoinParts = 8, kJoinThreads = 256;
 template <typename T>
-__global__ __launch_bounds__(512) void shared_join_kernel(const int32_t *row_req, const SharedJoin *joins, const float *part_o,
-                                                          const float *part_ml, T *out, float *lse, int nq, int nkv, int hd,
-                                                          float scale) {
-  const SharedJoin j = joins[row_req[2 * blockIdx.x]];
+__global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const int32_t *row_req, const SharedJoin *joins, const float *part_o,
+                                                                   const float *part_ml, T *out, float *lse, int nq, int nkv, int hd,
+                                                                   float scale) {
+  const int r = blockIdx.x;
+  const SharedJoin j = joins[row_req[2 * (int64_t)r]];
   if (j.own + j.pre < 2) return;                      // written as it was computed
-  const int G = nq / nkv, ch = hd / 8, n = j.own + j.pre;
+  const int G = nq / nkv, ch = hd / 8, n = j.own + j.pre, u = blockIdx.y * kJoinThreads + threadIdx.x;
+  if (u >= nq * ch) return;
   const float c_log2 = scale * kLog2e;
-  for (int u = threadIdx.x; u < nq * ch; u += blockDim.x) {
-    const int head = u / ch, c0 = u % ch * 8, kvh = head / G;
-    const int f = (blockIdx.x - j.row0) * G + head % G;
-    auto slot = [&](int p) {
-      return p < j.own ? ((int64_t)j.own_at + ((int64_t)p * nkv + kvh) * j.own_tiles) * kTile + f
-                       : ((int64_t)j.pre_at + ((int64_t)(p - j.own) * nkv + kvh) * j.pre_tiles) * kTile + j.pre_row + f;
-    };
-    float m = -INFINITY, den = 0.f;
-    for (int p = 0; p < n; ++p) m = fmaxf(m, part_ml[slot(p) * 2]);
-    floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
-    for (int p = 0; p < n; ++p) {
-      const int64_t s = slot(p);
-      const float2 ml = *reinterpret_cast<const float2 *>(part_ml + s * 2);
-      if (ml.x == -INFINITY) {
-        den += ml.y;
-        continue;
+  const int head = u / ch, c0 = u % ch * 8, kvh = head / G;
+  const int f = (r - j.row0) * G + head % G;
+  const int64_t own = ((int64_t)j.own_at + (int64_t)kvh * j.own_tiles) * kTile + f;
+  const int64_t pre = ((int64_t)j.pre_at + (int64_t)kvh * j.pre_tiles) * kTile + j.pre_row + f;
+  float m = -INFINITY, den = 0.f;
+  floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
+  for (int p0 = 0; p0 < n; p0 += kJoinParts) {
+    float2 ml[kJoinParts];
+    floatx4 a[kJoinParts], b[kJoinParts];
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.f);
+      a[i] = b[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (p0 + i < n) {                               // uniform
+        const int p = p0 + i, q = p - j.own;
+        const int64_t s = p < j.own ? own + (int64_t)p * nkv * j.own_tiles * kTile : pre + (int64_t)q * nkv * j.pre_tiles * kTile;
+        ml[i] = *reinterpret_cast<const float2 *>(part_ml + s * 2);
+        a[i] = *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0);
+        b[i] = *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0 + 4);
       }
-      const float w = __builtin_amdgcn_exp2f((ml.x - m) * c_log2);
-      den += ml.y * w;
-      y += *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0) * w;
-      z += *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0 + 4) * w;
     }
-    const int64_t row = (int64_t)blockIdx.x * nq + head;
-    const float inv = 1.0f / den;
-    y *= inv;
-    z *= inv;
-    T *to = out + row * hd + c0;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]), pack2bf_rne(z[0], z[1]), pack2bf_rne(z[2], z[3]));
-    } else {
-      *reinterpret_cast<floatx4 *>(to) = y;
-      *reinterpret_cast<floatx4 *>(to + 4) = z;
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) top = fmaxf(top, ml[i].x);
+    const float was = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c_log2);
+    m = top;
+    den *= was;
+    y *= was;
+    z *= was;
+#pragma unroll
+    for (int i = 0; i < kJoinParts; ++i) {
+      // of a part that saw no token the sum is 0, or NaN where the row's scores were
+      const float w = ml[i].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c_log2);
+      den += ml[i].y * w;
+      y += a[i] * w;
+      z += b[i] * w;
     }
-    if (lse && c0 == 0) lse[row] = m * scale + logf(den);
   }
+  const int64_t row = (int64_t)r * nq + head;
+  const float inv = 1.0f / den;
+  y *= inv;
+  z *= inv;
+  T *to = out + row * hd + c0;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4 *>(to) = make_uint4(pack2bf_rne(y[0], y[1]), pack2bf_rne(y[2], y[3]), pack2bf_rne(z[0], z[1]), pack2bf_rne(z[2], z[3]));
+  } else {
+    *reinterpret_cast<floatx4 *>(to) = y;
+    *reinterpret_cast<floatx4 *>(to + 4) = z;
+  }
+  if (lse && c0 == 0) lse[row] = m * scale + logf(den);
 }
 
 }  // namespace
@@ -407,13 +448,12 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
   if (!p.joined) return;
   const int32_t *row = reinterpret_cast<const int32_t *>(p.ws + p.w_row);
   const SharedJoin *joins = reinterpret_cast<const SharedJoin *>(p.ws + p.w_join);
-  const int threads = std::min(512, (p.nq * p.hd / 8 + 63) / 64 * 64);
-  if (p.dtype == WISP_BF16)
-    launch(shared_join_kernel<uint16_t>, p.rows, threads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml,
-           static_cast<uint16_t *>(out), lse, p.nq, p.nkv, p.hd, a.scale);
-  else
-    launch(shared_join_kernel<float>, p.rows, threads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml,
-           static_cast<float *>(out), lse, p.nq, p.nkv, p.hd, a.scale);
+  const dim3 grid(p.rows, (p.nq * p.hd / 8 + kJoinThreads - 1) / kJoinThreads);
+  auto join = [&](auto kernel, auto *to) {
+    launch(kernel, grid, kJoinThreads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml, to, lse, p.nq, p.nkv, p.hd, a.scale);
+  };
+  if (p.dtype == WISP_BF16) join(shared_join_kernel<uint16_t>, static_cast<uint16_t *>(out));
+  else join(shared_join_kernel<float>, static_cast<float *>(out));
 }
 
 }  // namespace wisp

@@ -48,17 +48,24 @@ __device__ __forceinline__ void to_op(Op8<float> &o, const float *p) {
   for (int x = 0; x < 2; ++x)
     o.v[x] = make_uint4(__float_as_uint(p[4 * x]), __float_as_uint(p[4 * x + 1]), __float_as_uint(p[4 * x + 2]), __float_as_uint(p[4 * x + 3]));
 }
-// Elements from `n` on become zero: slots past a request's last token may hold anything
-__device__ __forceinline__ void keep_first(Op8<uint16_t> &o, int n) {
-  uint32_t *w = reinterpret_cast<uint32_t *>(&o.v[0]);
+// The first n of eight elements: what is not theirs becomes zero.  Slots past a request's last token may hold
+// anything.
+template <typename T>
+struct Keep {
+  uint32_t mask[2 * sizeof(T)];
+  __device__ __forceinline__ explicit Keep(int n) {
 #pragma unroll
-  for (int x = 0; x < 4; ++x) w[x] = n >= 2 * x + 2 ? w[x] : n == 2 * x + 1 ? w[x] & 0xFFFFu : 0u;
-}
-__device__ __forceinline__ void keep_first(Op8<float> &o, int n) {
-  uint32_t *w = reinterpret_cast<uint32_t *>(&o.v[0]);
+    for (int x = 0; x < 2 * (int)sizeof(T); ++x) {
+      const int bits = min(max((n * (int)sizeof(T) - 4 * x) * 8, 0), 32);
+      mask[x] = (uint32_t)((1ull << bits) - 1);
+    }
+  }
+  __device__ __forceinline__ void apply(Op8<T> &o) const {
 #pragma unroll
-  for (int x = 0; x < 8; ++x) w[x] = n > x ? w[x] : 0u;
-}
+    for (int x = 0; x < (int)sizeof(T) / 2; ++x)
+      o.v[x] = make_uint4(o.v[x].x & mask[4 * x], o.v[x].y & mask[4 * x + 1], o.v[x].z & mask[4 * x + 2], o.v[x].w & mask[4 * x + 3]);
+  }
+};
 // whether an element is infinite or NaN
 __device__ __forceinline__ bool any_special(const Op8<uint16_t> &o) {
   const uint32_t w[4] = {o.v[0].x, o.v[0].y, o.v[0].z, o.v[0].w};
@@ -78,15 +85,13 @@ __device__ __forceinline__ bool any_special(const Op8<float> &o) {
 __device__ __forceinline__ float as_float(uint16_t b) { return bf2f(b); }
 __device__ __forceinline__ float as_float(float f) { return f; }
 
-// A lane's operands inside a page.  K, 16-dim step kb: row r = lane % 32 of the product is slot
+// A lane's operands inside a page, in elements.  K, 16-dim step kb: row r = lane % 32 of the product is slot
 // 8 ((r / 4) % 2) + 4 ((r / 8) % 2) + r % 4 of page r / 16
-__device__ __forceinline__ int k_op_off(int lane, int kb) {
-  return (((kb >> 1) * 2 + ((lane >> 3) & 1)) * 4 + (kb & 1) * 2 + (lane >> 5)) * 64 + (lane & 7) * 8;
-}
+__device__ __forceinline__ int k_op_lane(int lane) { return ((lane >> 3) & 1) * 256 + (lane >> 5) * 64 + (lane & 7) * 8; }
+__device__ __forceinline__ constexpr int k_op_step(int kb) { return (kb >> 1) * 512 + (kb & 1) * 128; }
 // V, 32-dim block mb: dim 32 mb + lane % 32, slots 8 (lane / 32) ..
-__device__ __forceinline__ int v_op_off(int lane, int mb) {
-  return ((2 * mb + ((lane >> 4) & 1)) * 2 + (lane >> 5)) * 128 + (lane & 15) * 8;
-}
+__device__ __forceinline__ int v_op_lane(int lane) { return ((lane >> 4) & 1) * 256 + (lane >> 5) * 128 + (lane & 15) * 8; }
+__device__ __forceinline__ constexpr int v_op_block(int mb) { return mb * 512; }
 // token of register i, from the tile's first
 __device__ __forceinline__ int reg_token(int lane, int i) { return 16 * (i >> 3) + 8 * (lane >> 5) + (i & 7); }
 
