@@ -2,6 +2,7 @@
 // first and the last ones, and move together; a kept key is rotated from its old position to its new one.
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstring>
 #include <numeric>
 
@@ -26,11 +27,10 @@ struct EvictArgs {
   int32_t *kept;
   int *err;
   int64_t total;                       // kept tokens of all requests
-  int stride, to_stride, n_blocks, nkv, slices;
-  double base;                         // rope_base
+  int stride, to_stride, n_blocks, nkv, runs;
 };
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kSelectKeys = 16384;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kSelectHeld = 16, kSelectBins = 2048;
 
 // floats in the order of their values as unsigned integers, -0 as 0, NaN below everything
 __device__ __forceinline__ uint32_t key_of(float f) {
@@ -39,246 +39,316 @@ __device__ __forceinline__ uint32_t key_of(float f) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Which tokens stay: a workgroup for each layer, kv head and request.  A radix selection, 8 bits a
-// pass, finds the least key that stays and how many of that key do (the first ones); then the tokens
-// are listed in order, and their weights move.
-template <bool LDS>
+// Which tokens stay: a workgroup for each layer, kv head and request, a wave for a run of tokens.  A radix
+// selection finds the least key that stays and how many of that key do (the first ones): 11 bits (a float's
+// exponent and two more), 11 and 10; then the tokens are listed in order.  HELD: the keys stay in registers.
+// Bound by latency: two loads that depend on each other, and 13 barriers.
+template <bool HELD>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t keys[LDS ? kSelectKeys : 1];
-  __shared__ uint32_t hist[256];
+  __shared__ uint32_t hist[kSelectBins];
   __shared__ int more[kSelectWaves], same[kSelectWaves];
   __shared__ uint32_t sh_key;
   __shared__ int sh_left;
   const EvictReq r = a.reqs[blockIdx.x];
   const int kvh = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t *pt = a.table + (int64_t)r.req * a.stride, *to = a.to + (int64_t)r.req * a.to_stride;
-  float *mass = a.mass + (int64_t)layer * a.n_blocks * a.nkv * kPage;
+  const int32_t *pt = a.table + (int64_t)r.req * a.stride;
+  const float *mass = a.mass + (int64_t)layer * a.n_blocks * a.nkv * kPage;
   int32_t *kept = a.kept + ((int64_t)layer * a.nkv + kvh) * a.total + r.start;
-  auto at = [&](int b, int t) { return ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * kPage + (t & 15); };
-  for (int x = tid; x < (r.ctx + 15) / 16; x += kSelectThreads)
-    if (pt[x] < 0 || pt[x] >= a.n_blocks) flag_error(a.err, kErrBlock);
-  for (int x = tid; x < (r.keep + 15) / 16; x += kSelectThreads)
-    if (to[x] < 0 || to[x] >= a.n_blocks) flag_error(a.err, kErrBlock);
-
   if (r.keep == r.ctx) {
     for (int t = tid; t < r.keep; t += kSelectThreads) kept[t] = t;
-  } else {
-    const int n = r.ctx - r.sink - r.recent;           // tokens to choose from
-    auto key = [&](int x) { return LDS ? keys[x] : key_of(mass[at(pt[(r.sink + x) >> 4], r.sink + x)]); };
-    if constexpr (LDS) {
-      for (int x = tid; x < n; x += kSelectThreads) keys[x] = key_of(mass[at(pt[(r.sink + x) >> 4], r.sink + x)]);
-      __syncthreads();
-    }
-    uint32_t found = 0;
-    int left = r.keep - r.sink - r.recent;             // tokens with the key's bits so far that stay
-    for (int shift = 24; shift >= 0 && left > 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int x = tid; x < n; x += kSelectThreads) {
-        const uint32_t k = key(x);
-        if (shift == 24 || (k >> (shift + 8)) == (found >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {
-        // the digit at which the count from the top reaches `left`: four digits a lane
-        int c[4], sum = 0;
+    return;
+  }
+  const int n = r.ctx - r.sink - r.recent;             // tokens to choose from
+  const int steps = (n + kSelectThreads - 1) / kSelectThreads, x0 = wave * steps * 64 + lane;   // a wave's run, 64 a step
+  auto token = [&](int i) __attribute__((always_inline)) { return r.sink + min(x0 + 64 * i, n - 1); };
+  bool bad = false;
+  auto key = [&](int i, int b) __attribute__((always_inline)) {
+    bad |= b < 0 || b >= a.n_blocks;
+    return key_of(mass[((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * kPage + (token(i) & 15)]);
+  };
+  uint32_t held[HELD ? kSelectHeld : 1];
+  if constexpr (HELD) {
+    int b[kSelectHeld];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) sum += c[x] = hist[255 - 4 * lane - x];
-        int before = sum;
+    for (int i = 0; i < kSelectHeld; ++i) b[i] = i < steps ? pt[token(i) >> 4] : 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int v = __shfl_up(before, o);
-          before += lane >= o ? v : 0;
-        }
-        before -= sum;
+    for (int i = 0; i < kSelectHeld; ++i) held[i] = i < steps ? key(i, b[i]) : 0;
+  }
+  // f(key, whether there is one) for each of this lane's tokens, in order
+  auto each = [&](auto &&f) __attribute__((always_inline)) {
+    if constexpr (HELD) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          if (before < left && before + c[x] >= left) {
-            sh_key = found | (uint32_t)(255 - 4 * lane - x) << shift;
-            sh_left = left - before;
-          }
-          before += c[x];
-        }
-      }
-      __syncthreads();
-      found = sh_key;
-      left = sh_left;
+      for (int i = 0; i < kSelectHeld; ++i)
+        if (i < steps) f(held[i], x0 + 64 * i < n, i);
+    } else {
+      for (int i = 0; i < steps; ++i) f(key(i, pt[token(i) >> 4]), x0 + 64 * i < n, i);
     }
-    if (left == 0) found = UINT_MAX;                    // none of the middle stays (no key is above)
-    // each wave lists a run of tokens: first their number, then their places
-    const int run = (n + kSelectThreads - 1) / kSelectThreads * 64, x0 = wave * run, x1 = min(n, x0 + run);
-    int m = 0, s = 0;
-    for (int x = x0 + lane; x - lane < x1; x += 64) {
-      const uint32_t k = x < x1 ? key(x) : 0;
-      m += __popcll(__builtin_amdgcn_ballot_w64(x < x1 && k > found));
-      s += __popcll(__builtin_amdgcn_ballot_w64(x < x1 && k == found));
+  };
+  uint32_t found = 0;
+  int left = r.keep - r.sink - r.recent;               // tokens with the key's bits so far that stay
+  auto digit = [&](int shift, int bits, uint32_t above) __attribute__((always_inline)) {
+    if (left == 0) return;
+    for (int x = tid; x < kSelectBins; x += kSelectThreads) hist[x] = 0;
+    __syncthreads();
+    each([&](uint32_t k, bool on, int) __attribute__((always_inline)) {
+      if (on && (k & above) == found) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+    });
+    __syncthreads();
+    // the digit at which the count from the top reaches `left`: two digits a thread
+    const int top = kSelectBins - 1 - 2 * tid;
+    const int c0 = hist[top], c1 = hist[top - 1];
+    int before = c0 + c1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(before, o);
+      before += lane >= o ? v : 0;
     }
-    if (lane == 0) {
-      more[wave] = m;
-      same[wave] = s;
+    if (lane == 63) more[wave] = before;
+    __syncthreads();
+    before -= c0 + c1;
+    for (int w = 0; w < wave; ++w) before += more[w];
+    if (before < left && before + c0 + c1 >= left) {
+      const bool second = before + c0 < left;
+      sh_key = found | (uint32_t)(top - second) << shift;
+      sh_left = left - before - (second ? c0 : 0);
     }
     __syncthreads();
-    m = 0;                                              // tokens listed before this one's, with the key and above it
-    s = 0;
-    for (int w = 0; w < wave; ++w) {
-      m += more[w];
-      s += same[w];
-    }
-    const unsigned long long below = (1ull << lane) - 1;
-    for (int x = x0 + lane; x - lane < x1; x += 64) {
-      const uint32_t k = x < x1 ? key(x) : 0;
-      const unsigned long long gt = __builtin_amdgcn_ballot_w64(x < x1 && k > found), eq = __builtin_amdgcn_ballot_w64(x < x1 && k == found);
-      const int e = s + __popcll(eq & below), place = r.sink + m + __popcll(gt & below) + min(e, left);
-      if (x < x1 && (k > found || (k == found && e < left))) kept[place] = r.sink + x;
-      m += __popcll(gt);
-      s += __popcll(eq);
-    }
-    for (int t = tid; t < r.sink; t += kSelectThreads) kept[t] = t;
-    for (int t = tid; t < r.recent; t += kSelectThreads) kept[r.keep - r.recent + t] = r.ctx - r.recent + t;
+    found = sh_key;
+    left = sh_left;
+  };
+  digit(21, 11, 0u);
+  digit(10, 11, ~0u << 21);
+  digit(0, 10, ~0u << 10);
+  if (left == 0) found = UINT_MAX;                      // none of the middle stays (no key is above)
+  // first the runs' numbers of tokens, then their places
+  int m = 0, s = 0;
+  each([&](uint32_t k, bool on, int) __attribute__((always_inline)) {
+    m += __popcll(__builtin_amdgcn_ballot_w64(on && k > found));
+    s += __popcll(__builtin_amdgcn_ballot_w64(on && k == found));
+  });
+  __syncthreads();
+  if (lane == 0) {
+    more[wave] = m;
+    same[wave] = s;
   }
   __syncthreads();
-  // the weights: a token never moves up, so those still to be read lie past those written
-  for (int d0 = 0; d0 < r.keep; d0 += kSelectThreads) {
-    const int d = d0 + tid;
-    float w = 0.f;
-    int64_t dst = -1;
-    if (d < r.keep) {
-      const int t = kept[d], b = to[d >> 4];
-      w = mass[at(pt[t >> 4], t)];
-      if (b >= 0 && b < a.n_blocks) dst = at(b, d);
-    }
-    __syncthreads();
-    if (dst >= 0) mass[dst] = w;
+  m = 0;                                                // tokens listed before this one's, with the key and above it
+  s = 0;
+  for (int w = 0; w < wave; ++w) {
+    m += more[w];
+    s += same[w];
   }
+  const unsigned long long below = (1ull << lane) - 1;
+  each([&](uint32_t k, bool on, int i) __attribute__((always_inline)) {
+    const unsigned long long gt = __builtin_amdgcn_ballot_w64(on && k > found), eq = __builtin_amdgcn_ballot_w64(on && k == found);
+    const int e = s + __popcll(eq & below), place = r.sink + m + __popcll(gt & below) + min(e, left);
+    if (on && (k > found || (k == found && e < left))) kept[place] = r.sink + x0 + 64 * i;
+    m += __popcll(gt);
+    s += __popcll(eq);
+  });
+  if (bad) flag_error(a.err, kErrBlock);
+  for (int t = tid; t < r.sink; t += kSelectThreads) kept[t] = t;
+  for (int t = tid; t < r.recent; t += kSelectThreads) kept[r.keep - r.recent + t] = r.ctx - r.recent + t;
 }
 
-// Moves the kept tokens of a layer, kv head and request: dims in slices, a workgroup each, which takes the new
-// pages in order, some at a time.  All sources of a turn are read before its slots are written; those of
-// later turns lie past them, as a token never moves up.  So a cache can be compacted in its own pages.
-constexpr int kMoveThreads = 256;
-
-// cos and sin of 2 pi x
-__device__ __forceinline__ void turn_of(double x, float &c, float &s) {
-  const float f = (float)(x - __builtin_rint(x));
-  s = sinpif(2.0f * f);
-  c = cospif(2.0f * f);
-}
+// Moves the kept tokens of a layer, kv head and request: a workgroup for 8 dims of K with the 8 that turn with
+// them and for 16 dims of V, its `runs` waves for 64 tokens each a turn.  All sources of a turn are read before its slots are written; those of later turns lie past them, as a token never moves
+// up.  So a cache is compacted in its own pages.  What a turn's tokens are is looked up while the turn before
+// runs, their positions two turns ahead.
+//
+// A page holds V by dims, eight slots of one in a row: the half pages that have kept tokens are read whole, and
+// their slots put in their new order in LDS (read one by one, at 2 bytes a lane, the cache's ports were the
+// bound: 32 requests of 2-8k tokens back to half, two layers, 496 us).
+struct MoveArgs {
+  EvictArgs e;
+  double freq[128];                    // turns of a position's angle, of each dim below HD / 2
+};
+// Where a token lies: page of its kv head x 16 + slot; kStill: there it stays; kNone: there is none
+constexpr uint32_t kStill = 1u << 31, kNone = ~0u;
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
-  constexpr int OCT = HD / 16;                          // octets of dims that turn with the octet HD / 2 above; blocks of 16 dims of V
-  constexpr int PAGES = 16;                             // of a turn
-  struct Src {
-    int blk, pos;
-  };
-  __shared__ Src src[PAGES * kPage];
-  __shared__ int dst[PAGES];
-  const EvictReq r = a.reqs[blockIdx.x / a.slices];
-  const int slice = blockIdx.x % a.slices, kvh = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x;
-  const int o0 = OCT * slice / a.slices, no = OCT * (slice + 1) / a.slices - o0;
+__global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
+  constexpr int OCT = HD / 16, VEC = 8 * (int)sizeof(T) / 16;       // 16-byte pieces of eight elements
+  constexpr int PAGE = kPage * HD;
+  const EvictArgs &a = m.e;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tid = threadIdx.x;
+  const int tokens = 64 * a.runs;                       // of a turn
+  uint32_t *codes = reinterpret_cast<uint32_t *>(smem);              // [2][tokens]
+  int *places = reinterpret_cast<int *>(smem) + 2 * tokens;          // [2][tokens]
+  // [2][runs][64]: the half pages of a run's tokens: page x 2 + half; the first token's place, its slots' bits << 8
+  uint2 *halves = reinterpret_cast<uint2 *>(places + 2 * tokens);
+  int *news = reinterpret_cast<int *>(halves + 2 * tokens), *n_halves = news + 2 * tokens / 16;   // [2][tokens / 16]; [2][runs]
+  T *tile = reinterpret_cast<T *>(smem + ((2 * tokens * 16 + 10 * a.runs * 4 + 15) & ~15)) + wave * 1024;   // this wave's V, as in the new pages
+  const EvictReq r = a.reqs[blockIdx.x / OCT];
+  const int oct = blockIdx.x % OCT, t0 = wave * 64, kvh = blockIdx.y, layer = blockIdx.z;
   const int32_t *pt = a.table + (int64_t)r.req * a.stride, *to = a.to + (int64_t)r.req * a.to_stride;
   const int32_t *kept = a.kept + ((int64_t)layer * a.nkv + kvh) * a.total + r.start;
-  T *kp = static_cast<T *>(a.k) + (int64_t)layer * a.n_blocks * a.nkv * (kPage * HD);
-  T *vp = static_cast<T *>(a.v) + (int64_t)layer * a.n_blocks * a.nkv * (kPage * HD);
-  auto page = [&](int b) { return ((int64_t)b * a.nkv + kvh) * (kPage * HD); };
-  const int pages = (r.keep + 15) / 16;
-  const int per_turn = min(PAGES, max(1, kMoveThreads / (16 * no)));   // pages: a thread one K unit at most, two of V
-  // K: a slot's octet and its partner, in the order of the new page; the turns of a position's angle
-  const int kx = tid % 16, ko = o0 + tid / 16 % no, kpg = tid / (16 * no);
-  const int ks = (kx % 8 / 4) * 8 + kx / 8 * 4 + kx % 4;
-  double freq[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) freq[e] = exp2(-2.0 * (8 * ko + e) / HD * log2(a.base)) * 0.15915494309189533577;
-  for (int p0 = 0; p0 < pages; p0 += per_turn) {
-    const int n = min(per_turn, pages - p0);
-    __syncthreads();                                    // the list before has been read
-    for (int x = tid; x < n * kPage; x += kMoveThreads) {
-      const int d = p0 * kPage + x;
-      Src s{-1, -1};
-      if (d < r.keep) {
-        s.pos = kept[d];
-        s.blk = min(max(pt[s.pos >> 4], 0), a.n_blocks - 1);
-      }
-      src[x] = s;
-    }
-    if (tid < n) {
-      const int b = to[p0 + tid];
-      dst[tid] = b >= 0 && b < a.n_blocks ? b : -1;
-    }
-    __syncthreads();
-    float lo[8], hi[8];
-    Src sk{-1, -1};
-    if (kpg < n) sk = src[kpg * kPage + ks];
-    if (sk.pos >= 0) {
-      const T *from = kp + page(sk.blk);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (sizeof(T) == 2) {
-          lo[e] = bf2f(from[k_page_off(sk.pos & 15, 8 * ko) + e]);
-          hi[e] = bf2f(from[k_page_off(sk.pos & 15, 8 * ko + HD / 2) + e]);
-        } else {
-          lo[e] = from[k_page_off(sk.pos & 15, 8 * ko) + e];
-          hi[e] = from[k_page_off(sk.pos & 15, 8 * ko + HD / 2) + e];
-        }
-      }
-    }
-    // V: a dim of eight slots
-    T val[2][8];
-    bool full[2], moved[2];
+  const int64_t layer_at = (int64_t)layer * a.n_blocks * a.nkv * PAGE;
+  // this lane's slot of K, in the order of the new page, and its octet's place there
+  const int ks = (lane % 8 / 4) * 8 + lane % 16 / 8 * 4 + lane % 4;
+  T *kp = static_cast<T *>(a.k) + layer_at + k_page_off(0, 8 * oct);
+  const int partner = k_page_off(0, 8 * oct + HD / 2) - k_page_off(0, 8 * oct);
+  // of V: dim lane % 16 of the octets' block, slots 8 (lane / 16 % 2) .. of pages lane / 32 and 2 more
+  T *vp = static_cast<T *>(a.v) + layer_at + v_page_off(0, 16 * oct + lane % 16);
+  const int v_half = lane / 16 % 2;
+
+  const int turns = (r.keep + tokens - 1) / tokens;
+    auto position = [&](int x) __attribute__((always_inline)) { return x * tokens + tid < r.keep ? kept[x * tokens + tid] : -1; };
+  int pos = position(0), blk = pos >= 0 ? pt[pos >> 4] : 0, new_page = pos >= 0 ? to[tid >> 4] : -1;
+  float *mass = a.mass + (int64_t)layer * a.n_blocks * a.nkv * kPage;
+  const bool weighs = oct == 0;                         // with one workgroup the weights move too
+  float weight = 0.f, moving = 0.f;
+  int put_to = -1, put_next = -1;                      // the new place (a page of the head), if it is another one
+  auto list = [&](int x) __attribute__((always_inline)) {
+    const int at = (x & 1) * tokens + tid, b = min(max(blk, 0), a.n_blocks - 1);
+    if (pos >= 0 && (blk != b || new_page < 0 || new_page >= a.n_blocks)) flag_error(a.err, kErrBlock);
+    put_next = pos >= 0 && new_page >= 0 && new_page < a.n_blocks && (pos != x * tokens + tid || b != new_page) ? new_page * a.nkv + kvh : -1;
+    if (weighs && put_next >= 0) weight = mass[((int64_t)b * a.nkv + kvh) * kPage + (pos & 15)];
+    codes[at] = pos < 0 ? kNone : (uint32_t)(b * a.nkv + kvh) << 4 | (pos & 15) | (pos == x * tokens + tid && b == new_page ? kStill : 0);
+    places[at] = pos;
+    // the first of a half page's tokens: they are in order
+    const int before = __shfl_up(pos, 1);
+    const bool first = pos >= 0 && (lane == 0 || before >> 3 != pos >> 3);
+    const unsigned long long all = __builtin_amdgcn_ballot_w64(first);
+    uint2 *half = halves + (at & ~63) + __popcll(all & ((2ull << lane) - 1)) - 1;
+    if (first) *half = make_uint2((uint32_t)(b * a.nkv + kvh) << 1 | (pos >> 3 & 1), lane);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (pos >= 0) atomicOr(&half->y, 256u << (pos & 7));
+    if (lane == 0) n_halves[at >> 6] = __popcll(all);
+    if (tid % 16 == 0) news[((x & 1) * tokens + tid) / 16] = new_page >= 0 && new_page < a.n_blocks ? new_page * a.nkv + kvh : -1;
+  };
+  list(0);
+  moving = weight;
+  put_to = put_next;
+  pos = position(1);
+  __syncthreads();
+  for (int x = 0; x < turns; ++x) {
+    const int at = (x & 1) * tokens + t0, d0 = x * tokens + t0;
+    const uint32_t ck = codes[at + (lane & ~15) + ks];
+    const int delta = d0 + (lane & ~15) + ks - places[at + (lane & ~15) + ks], kd = news[(at + lane) / 16];
+    uint32_t cv[2][8];
+    int vd[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int u = tid + y * kMoveThreads, vx = u % 32, vo = o0 + u / 32 % no, vpg = u / (32 * no);
-      full[y] = true;
-      moved[y] = false;
+      const int from = at + 32 * y + 16 * (lane / 32) + 8 * v_half;
+      __builtin_memcpy(cv[y], __builtin_assume_aligned(&codes[from], 32), 32);
+      vd[y] = news[from / 16];
+    }
+    // of no token: the pool's first one, not used
+    uint4 lo[VEC], hi[VEC];
+    {
+      const uint32_t c = ck == kNone ? 0 : ck & ~kStill;
+      const T *from = kp + (int64_t)(c >> 4) * PAGE + k_page_off(c & 15, 0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        val[y][e] = 0;
-        Src s{-1, -1};
-        if (vpg < n) s = src[vpg * kPage + vx / 16 * 8 + e];
-        if (s.pos >= 0) {
-          val[y][e] = vp[page(s.blk) + v_page_off(s.pos & 15, 16 * vo + vx % 16)];
-          moved[y] |= s.pos != (p0 + vpg) * kPage + vx / 16 * 8 + e || s.blk != dst[vpg];
-        } else {
-          full[y] = false;
+      for (int v = 0; v < VEC; ++v) {
+        lo[v] = ld16(reinterpret_cast<const char *>(from) + 16 * v);
+        hi[v] = ld16(reinterpret_cast<const char *>(from + partner) + 16 * v);
+      }
+    }
+    {
+      const uint2 *half = halves + at;
+      const int n = __builtin_amdgcn_readfirstlane(n_halves[at >> 6]);
+      for (int h0 = 0; h0 < n; h0 += 16) {
+        uint2 g[4];
+        uint4 w[4][VEC];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int h = h0 + 4 * i + lane / 16;
+          g[i] = h < n ? half[h] : make_uint2(0, 0);
+          const T *from = vp + (int64_t)(g[i].x >> 1) * PAGE + (g[i].x & 1) * 128;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) w[i][v] = ld16(reinterpret_cast<const char *>(from) + 16 * v);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          T val[8];
+          __builtin_memcpy(val, w[i], sizeof(val));
+          int d = g[i].y & 63;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (g[i].y >> (8 + e) & 1) {
+              tile[(d >> 3) * 128 + lane % 16 * 8 + (d & 7)] = val[e];
+              ++d;
+            }
         }
       }
     }
+    if (x + 1 < turns) {
+      blk = pos >= 0 ? pt[pos >> 4] : 0;
+      new_page = pos >= 0 ? to[((x + 1) * tokens + tid) >> 4] : -1;
+      const int after = position(x + 2);
+      list(x + 1);
+      pos = after;
+    }
+    // every load of the turn has returned, to every wave
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    if (sk.pos >= 0 && dst[kpg] >= 0) {
-      const int d = (p0 + kpg) * kPage + ks;
-      if (d != sk.pos || sk.blk != dst[kpg]) {
-        T *put = kp + page(dst[kpg]);
-        if (d != sk.pos) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float c, s;
-            turn_of((double)(d - sk.pos) * freq[e], c, s);
-            const float x = lo[e], y = hi[e];
-            lo[e] = __builtin_fmaf(x, c, -(y * s));
-            hi[e] = __builtin_fmaf(y, c, x * s);
-          }
-        }
+    if (weighs && put_to >= 0) mass[(int64_t)put_to * kPage + (tid & 15)] = moving;
+    moving = weight;
+    put_to = put_next;
+    if (!(ck & kStill) && kd >= 0) {
+      if (delta != 0) {
+        uint32_t wl[4 * VEC], wh[4 * VEC];
+        __builtin_memcpy(wl, lo, sizeof(wl));
+        __builtin_memcpy(wh, hi, sizeof(wh));
+        float l[8], h[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+          // the angle in turns, its whole ones taken off in 64 bits; sine and cosine of it are within 2.2 x 2^-24
+          const double turn = (double)delta * m.freq[8 * oct + e];
+          const float f = (float)(turn - __builtin_rint(turn)), c = __builtin_amdgcn_cosf(f), n = __builtin_amdgcn_sinf(f);
+          float p, q;
           if constexpr (sizeof(T) == 2) {
-            put[k_page_off(ks, 8 * ko) + e] = __builtin_bit_cast(uint16_t, (__bf16)lo[e]);
-            put[k_page_off(ks, 8 * ko + HD / 2) + e] = __builtin_bit_cast(uint16_t, (__bf16)hi[e]);
+            p = e & 1 ? __uint_as_float(wl[e / 2] & 0xFFFF0000u) : __uint_as_float(wl[e / 2] << 16);
+            q = e & 1 ? __uint_as_float(wh[e / 2] & 0xFFFF0000u) : __uint_as_float(wh[e / 2] << 16);
           } else {
-            put[k_page_off(ks, 8 * ko) + e] = lo[e];
-            put[k_page_off(ks, 8 * ko + HD / 2) + e] = hi[e];
+            p = __uint_as_float(wl[e]);
+            q = __uint_as_float(wh[e]);
+          }
+          l[e] = __builtin_fmaf(p, c, -(q * n));
+          h[e] = __builtin_fmaf(q, c, p * n);
+        }
+        if constexpr (sizeof(T) == 2) {
+          lo[0] = make_uint4(pack2bf_rne(l[0], l[1]), pack2bf_rne(l[2], l[3]), pack2bf_rne(l[4], l[5]), pack2bf_rne(l[6], l[7]));
+          hi[0] = make_uint4(pack2bf_rne(h[0], h[1]), pack2bf_rne(h[2], h[3]), pack2bf_rne(h[4], h[5]), pack2bf_rne(h[6], h[7]));
+        } else {
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            lo[v] = make_uint4(__float_as_uint(l[4 * v]), __float_as_uint(l[4 * v + 1]), __float_as_uint(l[4 * v + 2]), __float_as_uint(l[4 * v + 3]));
+            hi[v] = make_uint4(__float_as_uint(h[4 * v]), __float_as_uint(h[4 * v + 1]), __float_as_uint(h[4 * v + 2]), __float_as_uint(h[4 * v + 3]));
           }
         }
+      }
+      T *put = kp + (int64_t)kd * PAGE + k_page_off(ks, 0);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(put) + 16 * v) = lo[v];
+        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(put + partner) + 16 * v) = hi[v];
       }
     }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int u = tid + y * kMoveThreads, vx = u % 32, vo = o0 + u / 32 % no, vpg = u / (32 * no);
-      if (vpg >= n || !moved[y] || dst[vpg] < 0) continue;
-      T *put = vp + page(dst[vpg]) + v_page_off(vx / 16 * 8, 16 * vo + vx % 16);
+      if (vd[y] < 0) continue;
+      T *put = vp + (int64_t)vd[y] * PAGE + 128 * v_half;
+      const T *val = tile + (lane + 64 * y) * 8;
+      uint32_t none = 0, still = kStill;                // of some; of all (a slot of no token does not move)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (full[y] || src[vpg * kPage + vx / 16 * 8 + e].pos >= 0) put[e] = val[y][e];
+      for (int e = 0; e < 8; ++e) {
+        none |= cv[y][e] == kNone;
+        still &= cv[y][e];
+      }
+      if (still) continue;
+      if (!none) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(put) + 16 * v) = ld16(reinterpret_cast<const char *>(val) + 16 * v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (cv[y][e] != kNone) put[e] = val[e];
+      }
     }
   }
 }
@@ -362,6 +432,7 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
       if ((int64_t)stride * WISP_PAGE < r.keep)
         return fail(WISP_E_CAPACITY, "request %d keeps %d tokens but its new pages hold %d", r.req, r.keep, stride * WISP_PAGE);
     }
+    if ((int64_t)kv->n_blocks * model->n_kv_heads >= 1 << 27) return fail(WISP_E_UNSUPPORTED, "n_blocks x n_kv_heads of 2^27 or more");
     if (model->n_layers > 65535 || model->n_kv_heads > 65535) return fail(WISP_E_UNSUPPORTED, "more than 65535 layers or kv heads");
     if (!workspace) return fail(WISP_E_INVALID, "NULL workspace");
     if ((uintptr_t)workspace & 255) return fail(WISP_E_INVALID, "workspace must be 256-byte aligned");
@@ -390,15 +461,22 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     a.to_stride = stride;
     a.n_blocks = kv->n_blocks;
     a.nkv = model->n_kv_heads;
-    a.base = model->rope_base;
     const int n = (int)e.reqs.size();
-    launch(e.most <= kSelectKeys ? evict_select_kernel<true> : evict_select_kernel<false>, dim3(n, a.nkv, model->n_layers),
-           kSelectThreads, 0, s, a);
-    const int64_t units = (int64_t)n * a.nkv * model->n_layers, wgs = 4 * (int64_t)device_cus();
-    a.slices = 1;
-    while (a.slices < model->head_dim / 16 && units * a.slices < wgs) a.slices *= 2;
-    a.slices = std::min(a.slices, model->head_dim / 16);
-    auto go = [&](auto kernel) { launch(kernel, dim3((unsigned)n * a.slices, a.nkv, model->n_layers), kMoveThreads, 0, s, a); };
+    launch(e.most <= kSelectHeld * kSelectThreads ? evict_select_kernel<true> : evict_select_kernel<false>,
+           dim3(n, a.nkv, model->n_layers), kSelectThreads, 0, s, a);
+    // Tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half, two
+    // layers (4096 workgroups), 449 us with 8 waves and 475 with 16; one of 8000 back to a quarter (64) 53 and 45.
+    const int oct = model->head_dim / 16, most_waves = (int64_t)n * a.nkv * model->n_layers * oct < device_cus() ? 16 : 8;
+    int most_kept = 0;
+    for (const EvictReq &r : e.reqs) most_kept = std::max(most_kept, r.keep);
+    a.runs = std::max(1, std::min(most_waves, (most_kept + 63) / 64));
+    MoveArgs move{a, {}};
+    for (int i = 0; i < model->head_dim / 2; ++i)
+      move.freq[i] = std::pow((double)model->rope_base, -2.0 * i / model->head_dim) / (2 * 3.14159265358979323846);
+    const uint32_t shm = ((2 * 64 * a.runs * 16 + 10 * a.runs * 4 + 15) & ~15) + (uint32_t)a.runs * 1024 * (model->dtype == WISP_BF16 ? 2 : 4);
+    auto go = [&](auto kernel) {
+      launch(kernel, dim3((unsigned)n * oct, a.nkv, model->n_layers), 64 * a.runs, shm, s, move);
+    };
     if (model->dtype == WISP_BF16) {
       if (model->head_dim == 128) go(evict_move_kernel<uint16_t, 128>);
       else go(evict_move_kernel<uint16_t, 64>);
