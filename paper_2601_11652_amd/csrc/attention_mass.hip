@@ -1,6 +1,7 @@
 // The attention weight that every cached token gets from a batch's rows: for token t and kv head h the sum
 // over rows r that see t, and query heads g of h, of exp(q . k_t / sqrt(head_dim) - lse).
 #include <algorithm>
+#include <climits>
 
 #include "../../include/wisp.h"
 #include "kernels.h"
@@ -39,8 +40,10 @@ __device__ __forceinline__ void put_mass(const int32_t *page_table, int pt_strid
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mass_kernel(MassArgs a) {
-  constexpr int KB = HD / 16, PIECES = KB * (int)sizeof(T) / 2;   // 1 KiB pieces of a row tile in operand order
-  __shared__ uint4 rows_of[2][PIECES][64];
+  constexpr int KB = HD / 16, UNITS = HD * (int)sizeof(T) / 16, PIECES = UNITS / 2;   // 16-byte units of a row; 1 KiB pieces of a row tile
+  constexpr int TILES = PIECES <= 8 ? 4 : PIECES <= 16 ? 2 : 1;     // row tiles of a stage
+  constexpr int SWIZZLE = UNITS % 16 ? 7 : 15;
+  __shared__ uint4 rows_of[2][TILES][kTile * UNITS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lc = lane & 31, hf = lane >> 5;
   const int kvh = blockIdx.x % a.nkv;
@@ -63,68 +66,102 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
   floatx16 acc;
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  // a row tile's operands straight into LDS; its rows' lse and how far they see, in registers
+  // Row tiles go straight into LDS, whole rows at a time: unit u of row r lies at u ^ (r % 16 or 8), so that the rows' operands
+  // are read without bank conflicts (in operand order, each load took 32 bytes of 32 rows: 115 us for a prompt of
+  // 4096 rows).  Its rows' lse and how far they see are in registers.
   struct Rows {
     float lse;
-    int lim;                             // tokens that the lane's row sees; 0: it does not count
+    int lim, row, count;                 // tokens that the lane's row sees; it counts if its row is below count
   };
+  constexpr int WAVES = 4 / TILES, MINE = PIECES / WAVES;           // waves of a row tile's pieces; each one's
+  static_assert(PIECES % WAVES == 0, "a tile's pieces are shared equally");
+  const Divisor by_g(G);
   auto bring = [&](int r, int b) __attribute__((always_inline)) {
-    const int f = min(r + lc, rows - 1);
-    const T *from = static_cast<const T *>(a.q) + ((int64_t)(it.row0 + f / G) * a.nq + kvh * G + f % G) * HD + 8 * hf;
+    const int tile = wave / WAVES, p0 = wave % WAVES * MINE;
 #pragma unroll
-    for (int x = 0; x < (PIECES + 3) / 4; ++x) {
-      const int u = wave + 4 * x;
-      if (PIECES % 4 == 0 || u < PIECES)
-        lds_dma16(reinterpret_cast<const char *>(from + 16 * (u / ((int)sizeof(T) / 2))) + 16 * (u % ((int)sizeof(T) / 2)), &rows_of[b][u][0]);
+    for (int x = 0; x < MINE; ++x) {
+      const int at = (p0 + x) * 64 + lane, row = at / UNITS, unit = at % UNITS ^ (row & SWIZZLE);
+      const int f = min(r + tile * kTile + row, rows - 1), j = by_g.of(f);
+      const T *from = static_cast<const T *>(a.q) + ((int64_t)(it.row0 + j) * a.nq + kvh * G + f - j * G) * HD;
+      lds_dma16(reinterpret_cast<const char *>(from) + 16 * unit, &rows_of[b][tile][(p0 + x) * 64]);
     }
   };
-  auto figures = [&](int r) __attribute__((always_inline)) {
-    const int f = min(r + lc, rows - 1), j = f / G;
+  // A group's rows count by their requests: (request, row in it) is asked for two stages ahead, the request's
+  // count one, so that nothing waits for what is on its way
+  const bool by_request = a.count && it.req < 0;
+  auto request = [&](int r) __attribute__((always_inline)) {
+    return by_request ? *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + by_g.of(min(r + lc, rows - 1)))) : make_int2(0, 0);
+  };
+  auto figures = [&](int r, int2 of) __attribute__((always_inline)) {
+    const int f = min(r + lc, rows - 1), j = by_g.of(f);
     Rows w;
-    w.lse = a.lse[(int64_t)(it.row0 + j) * a.nq + kvh * G + f % G];
-    bool on = r + lc < r_end;
-    if (a.count && it.req < 0) {
-      const int2 of = *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + j));
-      on = on && of.y < a.count[of.x];
-    }
-    w.lim = on ? it.ctx + j + 1 : 0;
+    w.lse = a.lse[(int64_t)(it.row0 + j) * a.nq + kvh * G + f - j * G];
+    w.count = by_request ? a.count[of.x] : INT_MAX;
+    w.row = of.y;
+    w.lim = r + lc < r_end ? it.ctx + j + 1 : 0;
     return w;
   };
   if (it.r0 < r_end) {
+    loads_done();                        // K
+    constexpr int STAGE = TILES * kTile;
+    Rows w[TILES];
+    int2 of[TILES];
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) of[x] = request(it.r0 + x * kTile);
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) {
+      w[x] = figures(it.r0 + x * kTile, of[x]);
+      of[x] = request(it.r0 + STAGE + x * kTile);
+    }
     bring(it.r0, 0);
-    Rows w = figures(it.r0);
     int b = 0;
-    for (int r = it.r0; r < r_end; r += kTile, b ^= 1) {
+    for (int r0 = it.r0; r0 < r_end; r0 += STAGE, b ^= 1) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      const Rows now = w;
-      if (r + kTile < r_end) {
-        bring(r + kTile, b ^ 1);
-        w = figures(r + kTile);
+      Rows now[TILES];
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        now[x] = w[x];
+        now[x].lim = w[x].row < w[x].count ? w[x].lim : 0;
       }
-      floatx16 s;
+      if (r0 + STAGE < r_end) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        Op8<T> x;
-#pragma unroll
-        for (int y = 0; y < (int)sizeof(T) / 2; ++y) x.v[y] = rows_of[b][kb * ((int)sizeof(T) / 2) + y][lane];
-        s = mma(s, kf[kb], x);
-      }
-      const float l2 = now.lse * kLog2e;
-      if (__builtin_amdgcn_ballot_w64(now.lim < tp + kTile || fabsf(l2) > kFarScore)) {
-        // rows that do not see a token, or do not count; and scores so large that the roundings on both sides
-        // of the difference may make it positive
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e = __builtin_fmaf(s[i], c_log2, -l2);
-          if (fabsf(l2) > kFarScore) e = e > 0.f ? 0.f : e;
-          e = __builtin_amdgcn_exp2f(e);
-          acc[i] += tp + reg_token(lane, i) < now.lim ? e : 0.f;
+        for (int x = 0; x < TILES; ++x) {
+          w[x] = figures(r0 + STAGE + x * kTile, of[x]);
+          of[x] = request(r0 + 2 * STAGE + x * kTile);
         }
-      } else {
+        bring(r0 + STAGE, b ^ 1);
+      }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -l2));
+      for (int y = 0; y < TILES; ++y) {
+        if (r0 + y * kTile >= r_end) break;
+        floatx16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        // all operands asked for, then the products: a pair at a time, each pair waited for LDS
+        Op8<T> q[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int z = 0; z < (int)sizeof(T) / 2; ++z)
+            q[kb].v[z] = rows_of[b][y][lc * UNITS + (((2 * kb + hf) * ((int)sizeof(T) / 2) + z) ^ (lc & SWIZZLE))];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s = mma(s, kf[kb], q[kb]);
+        const float l2 = now[y].lse * kLog2e;
+        if (__builtin_amdgcn_ballot_w64(now[y].lim < tp + kTile || fabsf(l2) > kFarScore)) {
+          // rows that do not see a token, or do not count; and scores so large that the roundings on both sides
+          // of the difference may make it positive
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float e = __builtin_fmaf(s[i], c_log2, -l2);
+            if (fabsf(l2) > kFarScore) e = e > 0.f ? 0.f : e;
+            e = __builtin_amdgcn_exp2f(e);
+            acc[i] += tp + reg_token(lane, i) < now[y].lim ? e : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -l2));
+        }
       }
     }
   }

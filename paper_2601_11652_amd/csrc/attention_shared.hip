@@ -27,10 +27,10 @@ template <typename T, int HD>
 struct Geo {
   static constexpr int KB = HD / 16, MB = HD / 32;            // steps of the contraction; blocks of output dims
   static constexpr int PAGE = kPage * HD, PAGE_BYTES = PAGE * (int)sizeof(T);
-  static constexpr int STAGE = PAGE_BYTES <= 4096 ? 4 : 2;    // pages staged at a time
-  static constexpr int STAGE_BYTES = STAGE * 2 * PAGE_BYTES;
+  static constexpr int STAGES = PAGE_BYTES <= 4096 ? 4 : 2;   // tiles of K and V in LDS: the one in use and those ahead
+  static constexpr int STAGE_BYTES = 2 * 2 * PAGE_BYTES;
   static constexpr int LDJ = HD + 4;                          // a row of accumulators in LDS, in floats
-  static constexpr int SMEM = std::max(2 * STAGE_BYTES, 4 * kTile * LDJ * 4);
+  static constexpr int SMEM = std::max(STAGES * STAGE_BYTES, 4 * kTile * LDJ * 4);
   static constexpr bool AHEAD = sizeof(T) == 2 || HD <= 64;   // registers hold the operands of a tile ahead
   static constexpr int WGS = AHEAD ? 2 : 1;
 };
@@ -41,7 +41,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(
 template <typename T, int HD>
 __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(SharedArgs a) {
   using G_ = Geo<T, HD>;
-  constexpr int KB = G_::KB, MB = G_::MB, PAGE = G_::PAGE, PAGE_BYTES = G_::PAGE_BYTES, STAGE = G_::STAGE, LDJ = G_::LDJ;
+  constexpr int KB = G_::KB, MB = G_::MB, PAGE = G_::PAGE, STAGES = G_::STAGES, LDJ = G_::LDJ;
   __shared__ __attribute__((aligned(1024))) char smem[G_::SMEM];
   __shared__ float2 sh_ml[4][kTile];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -130,49 +130,73 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   int x = part;                                        // the next tile of this wave
 
   if (wide) {
-    // The tiles that every row of the item sees, in whole stages: pages go straight into LDS, one stage
-    // ahead; a page lies there as it does in memory.
-    constexpr int UNITS = STAGE * 2 / 4, CHUNKS = PAGE_BYTES / 1024;      // pages (K or V) of a wave a stage
-    constexpr int TILES = STAGE / 2;
-    const int stages = max(0, min(it.t1, it.ctx + it.tile0 * kTile / G + 1) - it.t0) / (TILES * kTile);
-    auto id_of = [&](int s) __attribute__((always_inline)) { return ids[min(page0 + s * STAGE + (STAGE == 4 ? wave : wave >> 1), page_end)]; };
-    auto bring = [&](int s, int id) __attribute__((always_inline)) {
-      const int64_t at = place(id);
-      char *to = smem + (s & 1) * G_::STAGE_BYTES;
+    // The tiles that every row of the item sees: pages go straight into LDS, STAGES - 1 tiles ahead, and lie
+    // there in operand order (as they do in memory, a third of the LDS cycles were conflicts).
+    constexpr int PIECE = (int)sizeof(T) / 2, OPS = KB / 2;              // 16-byte pieces of an operand; operands that a wave brings
+    constexpr int LOADS = OPS * PIECE;                                  // its loads for a tile: half of K or of V
+    const int n = max(0, min(it.t1, it.ctx + it.tile0 * kTile / G + 1) - it.t0) / kTile;
+    const int my_op = (wave >> 1) * OPS, my_v = wave & 1;
+    int b0 = 0, b1 = 0;
+    auto ids_of = [&](int t) __attribute__((always_inline)) {
+      b0 = ids[min(page0 + 2 * t, page_end)];
+      b1 = ids[min(page0 + 2 * t + 1, page_end)];
+    };
+    uint4(*stage)[2][KB][PIECE][64] = reinterpret_cast<uint4(*)[2][KB][PIECE][64]>(smem);   // [buffer][K, V]
+    // V's operands are of a page and a block of dims, KB / 2 blocks: a wave brings a page's.  K's, of a 16-dim step, are
+    // of both pages
+    auto bring = [&](int t) __attribute__((always_inline)) {
+      const T *from = my_v ? vp + place(my_op ? b1 : b0) + v_lane : kp + ((lane >> 4) & 1 ? place(b1) : place(b0)) + k_lane;
 #pragma unroll
-      for (int u0 = 0; u0 < UNITS; ++u0) {
-        const int u = wave * UNITS + u0;              // page u / 2, K or V
-        const char *from = reinterpret_cast<const char *>((u & 1 ? vp : kp) + at) + lane * 16;
+      for (int x = 0; x < OPS; ++x) {
+        const T *op = from + (my_v ? v_op_block(x) : k_op_step(my_op + x));
 #pragma unroll
-        for (int y = 0; y < CHUNKS; ++y) lds_dma16(from + y * 1024, to + u * PAGE_BYTES + y * 1024);
+        for (int y = 0; y < PIECE; ++y) lds_dma16(reinterpret_cast<const char *>(op) + 16 * y, &stage[t % STAGES][my_v][my_op + x][y][0]);
       }
     };
-    if (stages > 0) bring(0, id_of(0));
-    int next = id_of(1);
-    for (int s = 0; s < stages; ++s) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (s + 1 < stages) bring(s + 1, next);
-      next = id_of(s + 2);
-      const T *buf = reinterpret_cast<const T *>(smem + (s & 1) * G_::STAGE_BYTES);
-#pragma unroll 1
-      for (int y = 0; y < TILES; ++y) {
-        // units of a stage: page, K or V; this lane's K page of the tile
-        const T *tile_at = buf + 4 * y * PAGE, *kt = tile_at + 2 * ((lane >> 4) & 1) * PAGE + k_lane;
-        floatx16 sc;
+    auto operand = [&](const uint4 (&at)[PIECE][64]) __attribute__((always_inline)) {
+      Op8<T> r;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      for (int y = 0; y < PIECE; ++y) r.v[y] = at[y][lane];
+      return r;
+    };
+    loads_done();                                      // the queries
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sc = mma(sc, load_op(kt + k_op_step(kb)), qf[kb]);
-        softmax(sc);
+    for (int t = 0; t < STAGES - 1; ++t) {
+      ids_of(t);
+      if (n > 0) bring(t);                             // past the end: pages of the item, not used
+    }
+    ids_of(STAGES - 1);
+    for (int t = 0; t < n; ++t) {
+      // this wave's loads of the tile have landed, those of the STAGES - 2 after it may be on their way
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
+      bring(t + STAGES - 1);
+      ids_of(t + STAGES);
+      const auto &at = stage[t % STAGES];
+      // K's operands all asked for before the first product, V's before the exponentials: a pair at a time, each pair
+      // waited for LDS
+      Op8<T> op[KB];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const Op8<T> pb = probs(sc, g);
+      for (int kb = 0; kb < KB; ++kb) op[kb] = operand(at[0][kb]);
+      __builtin_amdgcn_sched_barrier(0);
+      floatx16 sc;
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], load_op(tile_at + (2 * g + 1) * PAGE + v_lane + v_op_block(mb)), pb);
-        }
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) sc = mma(sc, op[kb], qf[kb]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) op[kb] = operand(at[1][kb]);
+      __builtin_amdgcn_sched_barrier(0);
+      softmax(sc);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const Op8<T> pb = probs(sc, g);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], op[g * MB + mb], pb);
       }
     }
-    x = stages * TILES;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what was brought past the end has landed before LDS is used again
+    x = n;
   }
 
   // A wave by itself, operands straight from memory, a tile ahead: the waves of a row tile take its token

@@ -4,6 +4,7 @@
 #include <climits>
 #include <cstring>
 #include <numeric>
+#include <queue>
 
 #include "api.h"
 #include "host_guard.h"
@@ -75,32 +76,82 @@ wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedJoin> &joi
 }
 
 // Row tiles go in bundles of four, one a wave; one or two that are left share their tokens among four waves.
-// A tile's pass over 32 tokens is a turn: kTurn[tiles of the bundle] is a workgroup's for its share of them.
-int64_t turns(const Segment &s, int tiles) {
-  const int64_t n = (s.t1 - s.t0 + kTile - 1) / kTile;
-  return tiles > 2 ? n : (n * tiles + 3) / 4;
+// What a workgroup's pass over 32 tokens (a turn) costs, by the bundle's tiles, what starting and ending an
+// item does, and a row tile's partial result, written and read again; in ns.
+constexpr int64_t kTurnCost[5] = {0, 700, 800, 450, 450}, kStartCost = 4000, kPartCost = 1500;
+
+struct Tokens {                                     // of a segment, in tiles
+  int64_t tiles, full, rest;                        // and its bundles: of four row tiles; the row tiles left
+  int64_t turns(int row_tiles) const { return row_tiles > 2 ? tiles : (tiles * row_tiles + 3) / 4; }
+  int64_t cost(int row_tiles) const { return turns(row_tiles) * kTurnCost[row_tiles]; }
+};
+Tokens tokens_of(const Segment &s) { return Tokens{(s.t1 - s.t0 + kTile - 1) / kTile, s.tiles / 4, s.tiles % 4}; }
+// parts of a segment's tokens, for items of at most about `share`
+int32_t parts_of(const Segment &s, int64_t share) {
+  const Tokens t = tokens_of(s);
+  const int most = t.full ? 4 : (int)t.rest;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(t.turns(most), (t.cost(most) + share - 1) / share));
 }
-constexpr int64_t kCost[5] = {0, 3, 3, 2, 2}, kStart = 16;
+// When the last workgroup ends, the longest items first, and what the join adds
+int64_t time_of(const std::vector<Segment> &segs, int64_t share, int64_t slots) {
+  std::vector<int64_t> cost;
+  int64_t joined = 0;
+  for (const Segment &s : segs) {
+    const Tokens t = tokens_of(s);
+    const int64_t n = parts_of(s, share);
+    for (int64_t x = 0; x < n; ++x) {
+      cost.insert(cost.end(), t.full, kStartCost + (t.cost(4) + n - 1) / n);
+      if (t.rest) cost.push_back(kStartCost + (t.cost((int)t.rest) + n - 1) / n);
+    }
+    if (n > 1) joined += n * s.tiles;
+  }
+  std::sort(cost.begin(), cost.end(), std::greater<int64_t>());
+  std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> ends;
+  int64_t last = 0;
+  for (int64_t c : cost) {
+    int64_t at = 0;
+    if ((int64_t)ends.size() == slots) {
+      at = ends.top();
+      ends.pop();
+    }
+    ends.push(at + c);
+    last = std::max(last, at + c);
+  }
+  return last + joined * kPartCost / slots;
+}
 
 wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<SharedJoin> &joins, const std::vector<int32_t> &pre_seg, int G) {
   SharedPlan &p = b.p;
-  const int64_t slots = (int64_t)device_cus() * shared_wgs_per_cu(p.dtype, p.hd);
+  // every kv head has its part of the workgroups that run at once
+  const int64_t slots = std::max<int64_t>(1, (int64_t)device_cus() * shared_wgs_per_cu(p.dtype, p.hd) / p.nkv);
   int64_t total = 0, bundles = 0;
   for (Segment &s : segs) {
     s.tiles = (int32_t)(((int64_t)s.nrow * G + kTile - 1) / kTile);
-    const int64_t full = s.tiles / 4, rest = s.tiles % 4;
-    total += full * turns(s, 4) * kCost[4] + (rest ? turns(s, (int)rest) * kCost[rest] : 0);
-    bundles += full + (rest > 0);
+    const Tokens t = tokens_of(s);
+    total += t.full * t.cost(4) + t.cost((int)t.rest);
+    bundles += t.full + (t.rest > 0);
   }
   if (bundles > kSharedMaxItems / p.nkv) return too_many(bundles * p.nkv);
-  const int64_t share = std::max<int64_t>(total * p.nkv / slots, kStart);
+  // Items of an equal share of the work leave a last round of few, smaller ones more to start and to join: the
+  // best of some sizes.  With many more bundles than workgroups the rounds are short by themselves.
+  int64_t share = std::max<int64_t>(total / slots + 1, kStartCost);
+  if (bundles < 8 * slots) {
+    int64_t best = INT64_MAX, at = share;
+    for (int64_t f = 3; f <= 16; ++f) {
+      const int64_t c = std::max<int64_t>(share * f / 12, 1), t = time_of(segs, c, slots);
+      if (t < best) {
+        best = t;
+        at = c;
+      }
+    }
+    share = at;
+  }
   std::vector<SharedItem> items;
   std::vector<int64_t> cost;
   int64_t tiles_at = 0, n_items = 0;
   for (Segment &s : segs) {
-    const int most = s.tiles >= 4 ? 4 : s.tiles;
-    const int64_t t = turns(s, most), n = (s.t1 - s.t0 + kTile - 1) / kTile;
-    s.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({t, n, (t * kCost[most] + share / 2) / share}));
+    const int64_t n = tokens_of(s).tiles;
+    s.parts = parts_of(s, share);
     const bool alone = s.parts == 1 && s.req >= 0 && pre_seg[s.req] < 0;
     s.at = (int32_t)tiles_at;
     if (!alone) tiles_at += (int64_t)s.tiles * s.parts * p.nkv;
@@ -112,7 +163,7 @@ wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<Sha
         const int32_t m = std::min(4, s.tiles - k);
         items.push_back(SharedItem{s.table, s.t0 + from * kTile, std::min(s.t1, s.t0 + to * kTile), s.ctx, s.row0, s.nrow, k, m,
                                    alone ? -1 : (int32_t)(s.at + (int64_t)x * p.nkv * s.tiles + k), s.tiles, {0, 0}});
-        cost.push_back(kCost[m] * (m > 2 ? to - from : ((to - from) * m + 3) / 4));
+        cost.push_back(kTurnCost[m] * (m > 2 ? to - from : ((to - from) * m + 3) / 4));
       }
     }
     if (s.req >= 0) {
@@ -157,7 +208,8 @@ wisp_status plan_mass(Build &b, const std::vector<Segment> &segs, int G) {
   if (blocks > kSharedMaxItems / p.nkv) return too_many(blocks * p.nkv);
   for (const Segment &s : segs)
     for (int64_t t = s.t0; t < s.t1; t += kMassBlock) total += ((int64_t)s.nrow * G - first_row(s, t) + kTile - 1) / kTile;
-  const int64_t share = std::max<int64_t>(total * p.nkv / slots, kShort);
+  // three items for a workgroup that runs at once: the last ones to end are short
+  const int64_t share = std::max<int64_t>(total * p.nkv / (3 * slots), kShort);
   std::vector<MassItem> items;
   std::vector<MassJoin> joins;
   for (const Segment &s : segs)

@@ -95,6 +95,20 @@ __device__ __forceinline__ constexpr int v_op_block(int mb) { return mb * 512; }
 // token of register i, from the tile's first
 __device__ __forceinline__ int reg_token(int lane, int i) { return 16 * (i >> 3) + 8 * (lane >> 5) + (i & 7); }
 
+// Every load so far has returned, and the compiler knows it: operands that are first used inside a loop would make it
+// wait there, in every turn, for whatever has been asked for since.
+__device__ __forceinline__ void loads_done() {
+  __builtin_amdgcn_s_waitcnt(0 | 7 << 4 | 15 << 8);
+  asm volatile("" ::: "memory");
+}
+
+// x / d for x below 2^26 and d of 1 .. 64: one product (the quotient of a variable takes twenty instructions)
+struct Divisor {
+  uint32_t d, m;
+  __device__ __forceinline__ explicit Divisor(int by) : d(by), m(0xFFFFFFFFu / (uint32_t)by + 1) {}
+  __device__ __forceinline__ int of(int x) const { return d == 1 ? x : (int)__umulhi((uint32_t)x, m); }
+};
+
 // block ids, read through the scalar cache: nothing writes them while a kernel runs
 typedef const int32_t __attribute__((address_space(4))) const_ids_t;
 __device__ __forceinline__ const_ids_t *const_ids(const int32_t *p) {
