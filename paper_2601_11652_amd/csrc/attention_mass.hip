@@ -76,14 +76,48 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
   constexpr int WAVES = 4 / TILES, MINE = PIECES / WAVES;           // waves of a row tile's pieces; each one's
   static_assert(PIECES % WAVES == 0, "a tile's pieces are shared equally");
   const Divisor by_g(G);
-  auto bring = [&](int r, int b) __attribute__((always_inline)) {
-    const int tile = wave / WAVES, p0 = wave % WAVES * MINE;
+  // Where the query heads of a kv head divide a stage's rows (and the stage is whole) its rows lie as those of the stage
+  // before, so many tokens on: their places are kept, and only a uniform address moves.
+  constexpr int STAGE = TILES * kTile;
+  const int my_tile = wave / WAVES, p0 = wave % WAVES * MINE;
+  const bool steady = STAGE % G == 0;
+  const int step = STAGE / G;            // rows of the batch, of a steady stage
+  auto row_at = [&](int f, int64_t &at) __attribute__((always_inline)) {   // of flat row f: its query's place, in heads
+    const int c = min(f, rows - 1), j = by_g.of(c);
+    at = (int64_t)(it.row0 + j) * a.nq + kvh * G + c - j * G;
+    return j;
+  };
+  uint32_t q_off[MINE], lse_off[TILES];
+  int first_row[TILES];
+  int64_t head0;                         // the first row's query
+  row_at(it.r0, head0);
 #pragma unroll
-    for (int x = 0; x < MINE; ++x) {
-      const int at = (p0 + x) * 64 + lane, row = at / UNITS, unit = at % UNITS ^ (row & SWIZZLE);
-      const int f = min(r + tile * kTile + row, rows - 1), j = by_g.of(f);
-      const T *from = static_cast<const T *>(a.q) + ((int64_t)(it.row0 + j) * a.nq + kvh * G + f - j * G) * HD;
-      lds_dma16(reinterpret_cast<const char *>(from) + 16 * unit, &rows_of[b][tile][(p0 + x) * 64]);
+  for (int x = 0; x < MINE; ++x) {
+    const int at = (p0 + x) * 64 + lane, row = at / UNITS;
+    int64_t head;
+    row_at(it.r0 + my_tile * kTile + row, head);
+    q_off[x] = (uint32_t)((head - head0) * (HD * (int)sizeof(T))) + 16 * (at % UNITS ^ (row & SWIZZLE));
+  }
+#pragma unroll
+  for (int x = 0; x < TILES; ++x) {
+    int64_t head;
+    first_row[x] = row_at(it.r0 + x * kTile + lc, head);
+    lse_off[x] = (uint32_t)(head - head0);
+  }
+  // stage n of the item, rows r ..
+  auto bring = [&](int n, int r, int b) __attribute__((always_inline)) {
+    if (steady && r + STAGE <= rows) {
+      const T *base = static_cast<const T *>(a.q) + (head0 + (int64_t)n * step * a.nq) * HD;
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], &rows_of[b][my_tile][(p0 + x) * 64]);
+    } else {
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) {
+        const int at = (p0 + x) * 64 + lane, row = at / UNITS;
+        int64_t head;
+        row_at(r + my_tile * kTile + row, head);
+        lds_dma16(reinterpret_cast<const char *>(static_cast<const T *>(a.q) + head * HD) + 16 * (at % UNITS ^ (row & SWIZZLE)), &rows_of[b][my_tile][(p0 + x) * 64]);
+      }
     }
   };
   // A group's rows count by their requests: (request, row in it) is asked for two stages ahead, the request's
@@ -92,10 +126,17 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
   auto request = [&](int r) __attribute__((always_inline)) {
     return by_request ? *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + by_g.of(min(r + lc, rows - 1)))) : make_int2(0, 0);
   };
-  auto figures = [&](int r, int2 of) __attribute__((always_inline)) {
-    const int f = min(r + lc, rows - 1), j = by_g.of(f);
+  auto figures = [&](int n, int x, int r, int2 of) __attribute__((always_inline)) {
     Rows w;
-    w.lse = a.lse[(int64_t)(it.row0 + j) * a.nq + kvh * G + f - j * G];
+    int j;
+    if (steady && r + kTile <= rows) {
+      w.lse = (a.lse + head0 + (int64_t)n * step * a.nq)[lse_off[x]];
+      j = first_row[x] + n * step;
+    } else {
+      int64_t head;
+      j = row_at(r + lc, head);
+      w.lse = a.lse[head];
+    }
     w.count = by_request ? a.count[of.x] : INT_MAX;
     w.row = of.y;
     w.lim = r + lc < r_end ? it.ctx + j + 1 : 0;
@@ -103,19 +144,18 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
   };
   if (it.r0 < r_end) {
     loads_done();                        // K
-    constexpr int STAGE = TILES * kTile;
     Rows w[TILES];
     int2 of[TILES];
 #pragma unroll
     for (int x = 0; x < TILES; ++x) of[x] = request(it.r0 + x * kTile);
 #pragma unroll
     for (int x = 0; x < TILES; ++x) {
-      w[x] = figures(it.r0 + x * kTile, of[x]);
+      w[x] = figures(0, x, it.r0 + x * kTile, of[x]);
       of[x] = request(it.r0 + STAGE + x * kTile);
     }
-    bring(it.r0, 0);
-    int b = 0;
-    for (int r0 = it.r0; r0 < r_end; r0 += STAGE, b ^= 1) {
+    bring(0, it.r0, 0);
+    int b = 0, n = 0;
+    for (int r0 = it.r0; r0 < r_end; r0 += STAGE, b ^= 1, ++n) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       Rows now[TILES];
 #pragma unroll
@@ -126,10 +166,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
       if (r0 + STAGE < r_end) {
 #pragma unroll
         for (int x = 0; x < TILES; ++x) {
-          w[x] = figures(r0 + STAGE + x * kTile, of[x]);
+          w[x] = figures(n + 1, x, r0 + STAGE + x * kTile, of[x]);
           of[x] = request(r0 + 2 * STAGE + x * kTile);
         }
-        bring(r0 + STAGE, b ^ 1);
+        bring(n + 1, r0 + STAGE, b ^ 1);
       }
 #pragma unroll
       for (int y = 0; y < TILES; ++y) {

@@ -27,7 +27,7 @@ template <typename T, int HD>
 struct Geo {
   static constexpr int KB = HD / 16, MB = HD / 32;            // steps of the contraction; blocks of output dims
   static constexpr int PAGE = kPage * HD, PAGE_BYTES = PAGE * (int)sizeof(T);
-  static constexpr int STAGES = PAGE_BYTES <= 4096 ? 4 : 2;   // tiles of K and V in LDS: the one in use and those ahead
+  static constexpr int STAGES = PAGE_BYTES <= 4096 ? 4 : PAGE_BYTES <= 12288 ? 3 : 2;   // tiles of K and V in LDS
   static constexpr int STAGE_BYTES = 2 * 2 * PAGE_BYTES;
   static constexpr int LDJ = HD + 4;                          // a row of accumulators in LDS, in floats
   static constexpr int SMEM = std::max(STAGES * STAGE_BYTES, 4 * kTile * LDJ * 4);
@@ -71,23 +71,13 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   // than 2^8 in the probabilities, so the accumulators are rescaled on few tiles.
   float mc = 0.f;                                     // m_run in base 2; 0 while the row has seen nothing
   bool far = false;                                   // of some row it is so large that its rounding counts
-  auto exponentials = [&](floatx16 &s) __attribute__((always_inline)) {
-    float off = -mc;
-    if (far) {
-      // the rounding of m x log2(e) would be most of the scores' difference: that first
-      const float m = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] -= m;
-      off = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, off));
-  };
-  auto softmax = [&](floatx16 &s) __attribute__((always_inline)) {
+  auto row_max = [&](const floatx16 &s) __attribute__((always_inline)) {
     float mx = max3(s[0], s[1], s[2]);
 #pragma unroll
     for (int i = 3; i < 15; i += 2) mx = max3(mx, s[i], s[i + 1]);
-    mx = xor32_max(fmaxf(mx, s[15]));
+    return xor32_max(fmaxf(mx, s[15]));
+  };
+  auto raise = [&](float mx) __attribute__((always_inline)) {
     const bool grow = mx > m_run + tau;
     if (__builtin_amdgcn_ballot_w64(grow)) {
       const float alpha = grow ? __builtin_amdgcn_exp2f((m_run - mx) * c_log2) : 1.0f;
@@ -98,11 +88,30 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       mc = m_run == -INFINITY ? 0.f : m_run * c_log2;
       far = __builtin_amdgcn_ballot_w64(fabsf(mc) > kFarScore) != 0;
     }
-    exponentials(s);
+  };
+  // what is added to a score x log2(e) / sqrt(head_dim)
+  auto offset = [&](floatx16 &s) __attribute__((always_inline)) {
+    if (!far) return -mc;
+    // the rounding of m x log2(e) would be most of the scores' difference: that first
+    const float m = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] -= m;
+    return 0.f;
+  };
+  auto exponentials = [&](floatx16 &s, float off) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, off));
+  };
+  auto add_up = [&](const floatx16 &s) __attribute__((always_inline)) {
     float sum[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
     for (int i = 4; i < 16; ++i) sum[i & 3] += s[i];
     l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);   // this lane's tokens: the halves are added at the end
+  };
+  auto softmax = [&](floatx16 &s) __attribute__((always_inline)) {
+    raise(row_max(s));
+    exponentials(s, offset(s));
+    add_up(s);
   };
   // eight probabilities of a page as an operand
   auto probs = [&](const floatx16 &p, int g) __attribute__((always_inline)) {
@@ -166,33 +175,79 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       if (n > 0) bring(t);                             // past the end: pages of the item, not used
     }
     ids_of(STAGES - 1);
-    for (int t = 0; t < n; ++t) {
-      // this wave's loads of the tile have landed, those of the STAGES - 2 after it may be on their way
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * LOADS) : "memory");
-      bring(t + STAGES - 1);
-      ids_of(t + STAGES);
-      const auto &at = stage[t % STAGES];
-      // K's operands all asked for before the first product, V's before the exponentials: a pair at a time, each pair
-      // waited for LDS
-      Op8<T> op[KB];
+    auto products = [&](const Op8<T> (&k)[KB]) __attribute__((always_inline)) {
+      floatx16 r;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) op[kb] = operand(at[0][kb]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < 16; ++i) r[i] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) r = mma(r, k[kb], qf[kb]);
+      return r;
+    };
+    // This wave's loads of a tile have landed (those of `behind` tiles after it may be on their way), and every wave's
+    auto landed = [&](auto behind) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(behind)::value * LOADS) : "memory");
+    };
+    Op8<T> op[KB], ov[KB];
+    if constexpr (STAGES > 2) {
+      // A turn computes the scores of the next tile beside this one's exponentials, then this one's products with V
+      // beside the next one's maximum: a wave's matrix and vector instructions run at the same time.
       floatx16 sc;
+      if (n > 0) {
+        landed(std::integral_constant<int, STAGES - 2>());
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[0][0][kb]);
+        sc = products(op);
+        raise(row_max(sc));
+      }
+      for (int t = 0; t < n; ++t) {
+        landed(std::integral_constant<int, STAGES - 3>());
+        bring(t + STAGES - 1);
+        ids_of(t + STAGES);
+        const float off = offset(sc);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) sc = mma(sc, op[kb], qf[kb]);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[(t + 1) % STAGES][0][kb]);
+        const floatx16 next = products(op);              // past the end: not used
+        exponentials(sc, off);
+        add_up(sc);
+        const Op8<T> p0 = probs(sc, 0), p1 = probs(sc, 1);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) op[kb] = operand(at[1][kb]);
-      __builtin_amdgcn_sched_barrier(0);
-      softmax(sc);
+        for (int kb = 0; kb < KB; ++kb) ov[kb] = operand(stage[t % STAGES][1][kb]);
+        if constexpr (sizeof(T) == 2) {
+          __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);          // LDS reads
+          __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);             // vector instructions
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const Op8<T> pb = probs(sc, g);
+          for (int kb = 0; kb < KB; ++kb) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);           // a product
+            __builtin_amdgcn_sched_group_barrier(0x2, 48 / KB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], op[g * MB + mb], pb);
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], ov[g * MB + mb], g ? p1 : p0);
+        const float mx = row_max(next);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 < n) raise(mx);
+        sc = next;
+      }
+    } else {
+      for (int t = 0; t < n; ++t) {
+        landed(std::integral_constant<int, 0>());
+        bring(t + 1);
+        ids_of(t + 2);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[t % STAGES][0][kb]);
+        floatx16 sc = products(op);
+        softmax(sc);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const Op8<T> pb = probs(sc, g);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], operand(stage[t % STAGES][1][g * MB + mb]), pb);
+        }
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what was brought past the end has landed before LDS is used again
@@ -293,7 +348,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) sc = mma(sc, kf[kb], qf[kb]);
-      exponentials(sc);
+      exponentials(sc, offset(sc));
 #pragma unroll 1
       for (int t = 0; t < kTile && tp + t < it.t1; ++t) {
         float w = 0.f;
