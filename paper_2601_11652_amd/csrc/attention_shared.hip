@@ -49,16 +49,18 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   const int kvh = blockIdx.x % a.nkv;                 // neighbouring workgroups, on other XCDs: other kv heads
   const SharedItem it = a.items[blockIdx.x / a.nkv];
   const int G = a.nq / a.nkv, rows = it.nrow * G;
+  const Divisor by_g(G);
   const bool wide = it.tiles > 2;                     // one tile of rows a wave; else the waves share the tokens
   const int parts = wide ? 1 : 4 / it.tiles, tile = wide ? min(wave, it.tiles - 1) : wave % it.tiles;
   const int part = wide ? 0 : wave / it.tiles;
   const int fr0 = (it.tile0 + tile) * kTile, fr = min(fr0 + lc, rows - 1);   // padding rows: a real one
-  const int64_t q_at = ((int64_t)(it.row0 + fr / G) * a.nq + kvh * G + fr % G) * HD + 8 * hf;
+  const int jr = by_g.of(fr);
+  const int64_t q_at = ((int64_t)(it.row0 + jr) * a.nq + kvh * G + fr - jr * G) * HD + 8 * hf;
   Op8<T> qf[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) qf[kb] = load_op(static_cast<const T *>(a.q) + q_at + 16 * kb);
-  const int lim = min(it.t1, it.ctx + fr / G + 1);    // tokens that this lane's row sees
-  const int open = min(it.t1, it.ctx + __builtin_amdgcn_readfirstlane(fr0 / G) + 1);   // that every row of the tile sees
+  const int lim = min(it.t1, it.ctx + jr + 1);        // tokens that this lane's row sees
+  const int open = min(it.t1, it.ctx + __builtin_amdgcn_readfirstlane(by_g.of(fr0)) + 1);   // that every row of the tile sees
   const float c_log2 = a.scale * kLog2e, tau = 8.0f / c_log2;
   float m_run = -INFINITY, l_run = 0.f;
   floatx16 o[MB];
@@ -128,11 +130,6 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   auto place = [&](int b) __attribute__((always_inline)) {
     return ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * PAGE;
   };
-  // block ids out of range are reported (and clamped above)
-  for (int x = page0 + threadIdx.x; x <= page_end; x += 256) {
-    const int b = a.page_table[(int64_t)it.table * a.pt_stride + x];
-    if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
-  }
   const T *kp = static_cast<const T *>(a.k), *vp = static_cast<const T *>(a.v);
   const int k_lane = k_op_lane(lane), v_lane = v_op_lane(lane);
   const int n_tiles = (it.t1 - it.t0 + kTile - 1) / kTile;
@@ -141,40 +138,55 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   if (wide) {
     // The tiles that every row of the item sees: pages go straight into LDS, STAGES - 1 tiles ahead, and lie
     // there in operand order (as they do in memory, a third of the LDS cycles were conflicts).
-    constexpr int PIECE = (int)sizeof(T) / 2, OPS = KB / 2;              // 16-byte pieces of an operand; operands that a wave brings
-    constexpr int LOADS = OPS * PIECE;                                  // its loads for a tile: half of K or of V
-    const int n = max(0, min(it.t1, it.ctx + it.tile0 * kTile / G + 1) - it.t0) / kTile;
-    const int my_op = (wave >> 1) * OPS, my_v = wave & 1;
-    int b0 = 0, b1 = 0;
-    auto ids_of = [&](int t) __attribute__((always_inline)) {
-      b0 = ids[min(page0 + 2 * t, page_end)];
-      b1 = ids[min(page0 + 2 * t + 1, page_end)];
-    };
-    uint4(*stage)[2][KB][PIECE][64] = reinterpret_cast<uint4(*)[2][KB][PIECE][64]>(smem);   // [buffer][K, V]
-    // V's operands are of a page and a block of dims, KB / 2 blocks: a wave brings a page's.  K's, of a 16-dim step, are
-    // of both pages
-    auto bring = [&](int t) __attribute__((always_inline)) {
-      const T *from = my_v ? vp + place(my_op ? b1 : b0) + v_lane : kp + ((lane >> 4) & 1 ? place(b1) : place(b0)) + k_lane;
-#pragma unroll
-      for (int x = 0; x < OPS; ++x) {
-        const T *op = from + (my_v ? v_op_block(x) : k_op_step(my_op + x));
-#pragma unroll
-        for (int y = 0; y < PIECE; ++y) lds_dma16(reinterpret_cast<const char *>(op) + 16 * y, &stage[t % STAGES][my_v][my_op + x][y][0]);
+    constexpr int PIECE = (int)sizeof(T) / 2, LOADS = G_::PAGE_BYTES / 1024;   // 16-byte pieces of an operand; a wave's loads for a tile
+    const int n = max(0, min(it.t1, it.ctx + by_g.of(it.tile0 * kTile) + 1) - it.t0) / kTile;
+    // Block ids of 32 tiles sit in the lanes, those of the next 32 are on their way.  (Scalar loads share their counter with
+    // LDS and return out of order: every operand read from LDS would wait for them.)
+    const int32_t *table = a.page_table + (int64_t)it.table * a.pt_stride;
+    auto window = [&](int w) __attribute__((always_inline)) { return table[min(page0 + 64 * w + lane, page_end)]; };
+    int blk = window(0), after = window(1), b0 = 0, b1 = 0;
+    auto ids_of = [&](int t) __attribute__((always_inline)) {          // of each tile in turn
+      if (t % 32 == 0 && t > 0) {
+        blk = after;
+        after = window(t / 32 + 1);
       }
+      b0 = __builtin_amdgcn_readlane(blk, 2 * t & 63);
+      b1 = __builtin_amdgcn_readlane(blk, (2 * t & 63) + 1);
     };
-    auto operand = [&](const uint4 (&at)[PIECE][64]) __attribute__((always_inline)) {
+    // A tile's buffer holds K's pages, then V's, each KiB of them as a load of 16 bytes a lane brings it: K's units in the
+    // order of the rows that read them, V's as an operand has them.  The address is uniform but for the lane's place.
+    constexpr int KIB = G_::PAGE_BYTES / 1024, OP_BYTES = 8 * (int)sizeof(T);
+    const uint32_t k_from = ((lane >> 3 & 1) * 32 + (lane >> 4) * 8 + (lane & 7)) * OP_BYTES, v_from = (uint32_t)v_lane * (uint32_t)sizeof(T);
+    auto bring = [&](int t) __attribute__((always_inline)) {
+      // a wave: one page of K or of V
+      const char *from = reinterpret_cast<const char *>((wave & 1 ? vp : kp) + place(wave & 2 ? b1 : b0));
+      char *to = smem + (t % STAGES) * G_::STAGE_BYTES + (2 * (wave & 1) + (wave >> 1)) * G_::PAGE_BYTES;
+#pragma unroll
+      for (int u = 0; u < KIB / PIECE; ++u)
+#pragma unroll
+        for (int y = 0; y < PIECE; ++y)
+          lds_dma16_at(from + u * 1024 * PIECE + 16 * y, wave & 1 ? v_from : k_from, to + (u * PIECE + y) * 1024);
+    };
+    const char *k_at = smem + (lane >> 4 & 1) * G_::PAGE_BYTES + ((lane >> 5) * 16 + (lane & 15)) * 16, *v_at = smem + 2 * G_::PAGE_BYTES + lane * 16;
+    auto k_operand = [&](int buf, int kb) __attribute__((always_inline)) {
       Op8<T> r;
 #pragma unroll
-      for (int y = 0; y < PIECE; ++y) r.v[y] = at[y][lane];
+      for (int y = 0; y < PIECE; ++y) r.v[y] = ld16(k_at + buf * G_::STAGE_BYTES + ((kb >> 1) * PIECE + y) * 1024 + (kb & 1) * 512);
       return r;
     };
-    loads_done();                                      // the queries
+    auto v_operand = [&](int buf, int g, int mb) __attribute__((always_inline)) {
+      Op8<T> r;
+#pragma unroll
+      for (int y = 0; y < PIECE; ++y) r.v[y] = ld16(v_at + buf * G_::STAGE_BYTES + g * G_::PAGE_BYTES + (mb * PIECE + y) * 1024);
+      return r;
+    };
 #pragma unroll
     for (int t = 0; t < STAGES - 1; ++t) {
       ids_of(t);
       if (n > 0) bring(t);                             // past the end: pages of the item, not used
     }
     ids_of(STAGES - 1);
+    loads_done();                                      // the queries
     auto products = [&](const Op8<T> (&k)[KB]) __attribute__((always_inline)) {
       floatx16 r;
 #pragma unroll
@@ -195,7 +207,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       if (n > 0) {
         landed(std::integral_constant<int, STAGES - 2>());
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[0][0][kb]);
+        for (int kb = 0; kb < KB; ++kb) op[kb] = k_operand(0, kb);
         sc = products(op);
         raise(row_max(sc));
       }
@@ -206,13 +218,13 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
         const float off = offset(sc);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[(t + 1) % STAGES][0][kb]);
+        for (int kb = 0; kb < KB; ++kb) op[kb] = k_operand((t + 1) % STAGES, kb);
         const floatx16 next = products(op);              // past the end: not used
         exponentials(sc, off);
         add_up(sc);
         const Op8<T> p0 = probs(sc, 0), p1 = probs(sc, 1);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) ov[kb] = operand(stage[t % STAGES][1][kb]);
+        for (int kb = 0; kb < KB; ++kb) ov[kb] = v_operand(t % STAGES, kb / MB, kb % MB);
         if constexpr (sizeof(T) == 2) {
           __builtin_amdgcn_sched_group_barrier(0x100, KB, 0);          // LDS reads
           __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);             // vector instructions
@@ -239,14 +251,14 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
         bring(t + 1);
         ids_of(t + 2);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) op[kb] = operand(stage[t % STAGES][0][kb]);
+        for (int kb = 0; kb < KB; ++kb) op[kb] = k_operand(t % STAGES, kb);
         floatx16 sc = products(op);
         softmax(sc);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const Op8<T> pb = probs(sc, g);
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], operand(stage[t % STAGES][1][g * MB + mb]), pb);
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], v_operand(t % STAGES, g, mb), pb);
         }
       }
     }
@@ -368,10 +380,32 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     }
   }
 
+  // block ids out of range are reported (they were clamped above)
+  for (int x = page0 + threadIdx.x; x <= page_end; x += 256) {
+    const int b = a.page_table[(int64_t)it.table * a.pt_stride + x];
+    if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
+  }
+  // A row tile of one wave goes out as it lies in the registers, partial results in that order: 16 bytes a lane
+  const float l = xor32_sum(l_run);
+  auto put_part = [&](int tile, int row_lane, int at, floatx4 v) __attribute__((always_inline)) {
+    *reinterpret_cast<floatx4 *>(a.part_o + ((int64_t)it.part + (int64_t)kvh * it.step + tile) * (kTile * HD) + (at * 64 + row_lane) * 4) = v;
+  };
+  auto put_ml = [&](int tile, int row, float m, float den) __attribute__((always_inline)) {
+    *reinterpret_cast<float2 *>(a.part_ml + (((int64_t)it.part + (int64_t)kvh * it.step + tile) * kTile + row) * 2) = make_float2(m, den);
+  };
+  if (wide && it.part >= 0) {
+    if (wave < it.tiles) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) put_part(wave, lane, 4 * mb + y, floatx4{o[mb][4 * y], o[mb][4 * y + 1], o[mb][4 * y + 2], o[mb][4 * y + 3]});
+      if (hf == 0) put_ml(wave, lc, m_run, l);
+    }
+    return;
+  }
   // through LDS: 8 dims of a row a thread, the waves of a row tile added in order
   __syncthreads();
   float(*jo)[kTile][LDJ] = reinterpret_cast<float(*)[kTile][LDJ]>(smem);
-  const float l = xor32_sum(l_run);
   if (hf == 0) sh_ml[wave][lc] = make_float2(m_run, l);
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
@@ -400,14 +434,13 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       z += *reinterpret_cast<const floatx4 *>(&jo[t + x * it.tiles][r][c0 + 4]) * w;
     }
     if (it.part >= 0) {
-      const int64_t slot = ((int64_t)it.part + (int64_t)kvh * it.step + t) * kTile + r;
-      float *to = a.part_o + slot * HD + c0;
-      *reinterpret_cast<floatx4 *>(to) = y;
-      *reinterpret_cast<floatx4 *>(to + 4) = z;
-      if (c0 == 0) *reinterpret_cast<float2 *>(a.part_ml + slot * 2) = make_float2(m, den);
+      put_part(t, r, c0 / 8, y);
+      put_part(t, r + 32, c0 / 8, z);
+      if (c0 == 0) put_ml(t, r, m, den);
       continue;
     }
-    const int64_t row = (int64_t)(it.row0 + f / G) * a.nq + kvh * G + f % G;
+    const int j = by_g.of(f);
+    const int64_t row = (int64_t)(it.row0 + j) * a.nq + kvh * G + f - j * G;
     const float inv = 1.0f / den;
     y *= inv;
     z *= inv;
@@ -426,19 +459,30 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 // head; the loads of kJoinParts results are in flight at once.
 constexpr int kJoinParts = 8, kJoinThreads = 256;
 template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const int32_t *row_req, const SharedJoin *joins, const float *part_o,
+__global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedRow *rows, const SharedBundle *bundles, const float *part_o,
                                                                    const float *part_ml, T *out, float *lse, int nq, int nkv, int hd,
-                                                                   float scale) {
-  const int r = blockIdx.x;
-  const SharedJoin j = joins[row_req[2 * (int64_t)r]];
-  if (j.own + j.pre < 2) return;                      // written as it was computed
-  const int G = nq / nkv, ch = hd / 8, n = j.own + j.pre, u = blockIdx.y * kJoinThreads + threadIdx.x;
-  if (u >= nq * ch) return;
+                                                                   int per_block, float scale) {
+  // per_block kv heads a workgroup; neighbouring threads have the heads of a kv head, whose results are neighbours
+  const int r = blockIdx.x, G = nq / nkv, ch = hd / 8;
+  const SharedRow j = rows[r];
+  const Divisor by_g(G), by_head(G * ch);
+  const int at = blockIdx.z * blockDim.x + threadIdx.x, local = by_head.of(at), u = at - local * G * ch, c = by_g.of(u), g = u - c * G;
+  const int kvh = blockIdx.y * per_block + local, c0 = 8 * c, head = kvh * G + g;
+  if (local >= per_block || kvh >= nkv) return;
   const float c_log2 = scale * kLog2e;
-  const int head = u / ch, c0 = u % ch * 8, kvh = head / G;
-  const int f = (r - j.row0) * G + head % G;
-  const int64_t own = ((int64_t)j.own_at + (int64_t)kvh * j.own_tiles) * kTile + f;
-  const int64_t pre = ((int64_t)j.pre_at + (int64_t)kvh * j.pre_tiles) * kTile + j.pre_row + f;
+  const int f = j.own_row + g, k = f / (kBundle * kTile);
+  const SharedBundle b0 = bundles[j.own + k];
+  SharedBundle b1{0, 0, 0, 0};
+  int f1 = 0;
+  if (j.pre >= 0) {
+    f1 = j.pre_row + g;
+    b1 = bundles[j.pre + f1 / (kBundle * kTile)];
+    f1 %= kBundle * kTile;
+  }
+  const int n = b0.parts + b1.parts;
+  if (n < 2) return;                                  // written as it was computed
+  const int64_t own = ((int64_t)b0.at + (int64_t)kvh * b0.tiles) * kTile + f % (kBundle * kTile), own_step = (int64_t)nkv * b0.tiles * kTile;
+  const int64_t pre = ((int64_t)b1.at + (int64_t)kvh * b1.tiles) * kTile + f1, pre_step = (int64_t)nkv * b1.tiles * kTile;
   float m = -INFINITY, den = 0.f;
   floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
   for (int p0 = 0; p0 < n; p0 += kJoinParts) {
@@ -448,12 +492,13 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const int32_t
     for (int i = 0; i < kJoinParts; ++i) {
       ml[i] = make_float2(-INFINITY, 0.f);
       a[i] = b[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (p0 + i < n) {                               // uniform
-        const int p = p0 + i, q = p - j.own;
-        const int64_t s = p < j.own ? own + (int64_t)p * nkv * j.own_tiles * kTile : pre + (int64_t)q * nkv * j.pre_tiles * kTile;
+      if (p0 + i < n) {
+        const int p = p0 + i;
+        const int64_t s = p < b0.parts ? own + p * own_step : pre + (p - b0.parts) * pre_step;
         ml[i] = *reinterpret_cast<const float2 *>(part_ml + s * 2);
-        a[i] = *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0);
-        b[i] = *reinterpret_cast<const floatx4 *>(part_o + s * hd + c0 + 4);
+        const float *o = part_o + (s >> 5) * kTile * hd + (c0 / 8 * 64 + (s & 31)) * 4;
+        a[i] = *reinterpret_cast<const floatx4 *>(o);
+        b[i] = *reinterpret_cast<const floatx4 *>(o + 32 * 4);
       }
     }
     float top = m;
@@ -525,11 +570,14 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
     }
   }
   if (!p.joined) return;
-  const int32_t *row = reinterpret_cast<const int32_t *>(p.ws + p.w_row);
-  const SharedJoin *joins = reinterpret_cast<const SharedJoin *>(p.ws + p.w_join);
-  const dim3 grid(p.rows, (p.nq * p.hd / 8 + kJoinThreads - 1) / kJoinThreads);
+  const SharedRow *rows = reinterpret_cast<const SharedRow *>(p.ws + p.w_join);
+  const SharedBundle *bundles = reinterpret_cast<const SharedBundle *>(p.ws + p.w_bundles);
+  const int of_head = p.nq / p.nkv * p.hd / 8, per_block = std::max(1, std::min(p.nkv, kJoinThreads / of_head));
+  const int threads = std::min(kJoinThreads, (per_block * of_head + 63) / 64 * 64);
+  const dim3 grid(p.rows, (p.nkv + per_block - 1) / per_block, (per_block * of_head + threads - 1) / threads);
   auto join = [&](auto kernel, auto *to) {
-    launch(kernel, grid, kJoinThreads, 0, s, row, joins, (const float *)a.part_o, (const float *)a.part_ml, to, lse, p.nq, p.nkv, p.hd, a.scale);
+    launch(kernel, grid, threads, 0, s, rows, bundles, (const float *)a.part_o, (const float *)a.part_ml, to, lse,
+           p.nq, p.nkv, p.hd, per_block, a.scale);
   };
   if (p.dtype == WISP_BF16) join(shared_join_kernel<uint16_t>, static_cast<uint16_t *>(out));
   else join(shared_join_kernel<float>, static_cast<float *>(out));

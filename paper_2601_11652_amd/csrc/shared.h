@@ -17,13 +17,16 @@ struct SharedItem {                    // up to four row tiles of a segment over
   int32_t row0, nrow, tile0, tiles;    // the segment's first row and rows; first row tile, row tiles
   int32_t part, step, pad[2];          // kv head 0's first partial result (a tile each), those of a head; -1: none
 };
-// The results of a request's row r x head g (flat row r * G + g): `own` partial results of its own
-// segment, then `pre` of its group's, in which its rows begin at flat row pre_row.  A segment's results
-// lie [part][kv head][tiles], from tile own_at (pre_at) on.
-struct SharedJoin {
-  int32_t row0, own_at, own, own_tiles;
-  int32_t pre_at, pre, pre_tiles, pre_row;
+// The partial results of a bundle of row tiles (four of a segment's, the last one's rest) lie [part][kv head][row tile]
+// from tile `at` on, a tile in the order of the accumulators.  A row has those of its own segment's
+// bundle, and of its group's; one in all was written as it was computed.
+struct SharedBundle {
+  int32_t at, parts, tiles, pad;
 };
+struct SharedRow {                     // of a row of the batch, head 0 of a kv head
+  int32_t own, own_row, pre, pre_row;  // first bundle of the request's segment, flat row there; of its group's (own -1: none)
+};
+
 // Column sums of a segment's probabilities: tokens t0 .. t1 - 1 (at most a block of them), flat rows r0 .. r1 - 1
 struct MassItem {
   int32_t table, t0, t1, ctx;
@@ -35,6 +38,7 @@ struct MassJoin {                      // a token block whose sums have several 
   int32_t part, parts, step, pad;
 };
 
+constexpr int kBundle = 4;             // row tiles of a workgroup
 constexpr int kMassBlock = 4 * kTile;  // tokens of a workgroup: a tile a wave
 constexpr int kSharedMaxItems = 1 << 22;
 
@@ -45,7 +49,7 @@ struct SharedPlan {                    // a wisp_shared_batch
   int32_t device, dtype, nq, nkv, hd, rows, B;
   int32_t pt_stride, n_items, n_parts, joined, n_mass, n_mass_join, pad;
   // byte offsets in the workspace; w_row: a row's request
-  uint64_t w_items, w_row, w_join, w_mass, w_mass_join, w_po, w_pml, w_pm, total;
+  uint64_t w_items, w_bundles, w_row, w_join, w_mass, w_mass_join, w_po, w_pml, w_pm, total;
 };
 
 struct SharedCache {                   // one layer's pools

@@ -20,13 +20,13 @@ constexpr int32_t kAll = 1 << 30;                   // ctx of a group's segment:
 
 struct Segment {
   int32_t table, t0, t1, ctx, row0, nrow, req;      // as in the items; req: -1 for a group's
-  int32_t tiles, parts, at;                         // row tiles; parts of the tokens; first partial result
+  int32_t tiles, bundle0;                           // row tiles; the first of its bundles
 };
 
 struct Build {
   SharedPlan p{};
   std::vector<int32_t> host;
-  size_t i_items = 0, i_row = 0, i_join = 0, i_mass = 0, i_mass_join = 0;
+  size_t i_items = 0, i_bundles = 0, i_row = 0, i_join = 0, i_mass = 0, i_mass_join = 0;
   int64_t mass_parts = 0;                           // floats
 };
 
@@ -42,7 +42,7 @@ wisp_status too_many(int64_t n) {
   return fail(WISP_E_UNSUPPORTED, "the batch needs %lld work items (at most %d)", (long long)n, kSharedMaxItems);
 }
 
-wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedJoin> &joins, std::vector<int32_t> &pre_seg,
+wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedRow> &joins, std::vector<int32_t> &pre_seg,
                         const wisp_batch_desc *d, int32_t n_groups, const int32_t *size, const int32_t *prefix) {
   if (n_groups < 0) return fail(WISP_E_INVALID, "n_groups < 0");
   if (n_groups > 0 && (!size || !prefix)) return fail(WISP_E_INVALID, "group_size / prefix_len is NULL");
@@ -57,15 +57,12 @@ wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedJoin> &joi
       if (d->ctx_len[r] < pre) return fail(WISP_E_INVALID, "request %d has %d cached tokens, its group shares %d", r, d->ctx_len[r], pre);
     const bool together = n > 1 && pre > 0;
     const int32_t shared = together ? (int32_t)segs.size() : -1, first = row;
-    if (together) segs.push_back(Segment{i, 0, pre, kAll, row, 0, -1, 0, 0, 0});
+    if (together) segs.push_back(Segment{i, 0, pre, kAll, row, 0, -1, 0, 0});
     for (int32_t r = i; r < i + n; ++r) {
       const int32_t nrow = rows_of(r), ctx = d->ctx_len[r];
-      SharedJoin j{};
-      j.row0 = row;
-      j.pre_row = row - first;
-      joins.push_back(j);
+      for (int32_t x = 0; x < nrow; ++x) joins.push_back(SharedRow{(int32_t)segs.size(), x, shared, row - first + x});   // of segments, yet
       pre_seg.push_back(shared);
-      segs.push_back(Segment{r, together ? pre : 0, ctx + nrow, ctx, row, nrow, r, 0, 0, 0});
+      segs.push_back(Segment{r, together ? pre : 0, ctx + nrow, ctx, row, nrow, r, 0, 0});
       row += nrow;
     }
     if (together) segs[shared].nrow = row - first;
@@ -75,35 +72,58 @@ wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedJoin> &joi
   return WISP_OK;
 }
 
-// Row tiles go in bundles of four, one a wave; one or two that are left share their tokens among four waves.
-// What a workgroup's pass over 32 tokens (a turn) costs, by the bundle's tiles, what starting and ending an
-// item does, and a row tile's partial result, written and read again; in ns.
-constexpr int64_t kTurnCost[5] = {0, 700, 800, 450, 450}, kStartCost = 4000, kPartCost = 1500;
-
-struct Tokens {                                     // of a segment, in tiles
-  int64_t tiles, full, rest;                        // and its bundles: of four row tiles; the row tiles left
-  int64_t turns(int row_tiles) const { return row_tiles > 2 ? tiles : (tiles * row_tiles + 3) / 4; }
-  int64_t cost(int row_tiles) const { return turns(row_tiles) * kTurnCost[row_tiles]; }
-};
-Tokens tokens_of(const Segment &s) { return Tokens{(s.t1 - s.t0 + kTile - 1) / kTile, s.tiles / 4, s.tiles % 4}; }
-// parts of a segment's tokens, for items of at most about `share`
-int32_t parts_of(const Segment &s, int64_t share) {
-  const Tokens t = tokens_of(s);
-  const int most = t.full ? 4 : (int)t.rest;
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(t.turns(most), (t.cost(most) + share - 1) / share));
+// Row tiles of a segment go in bundles of four, one a wave; of a bundle of one or two the four waves share the tokens.
+// What a workgroup's pass over 32 tokens (a turn) costs by the bundle's row tiles, what starting and ending an item
+// does, and a row tile's partial result, written and read again; in ns.
+constexpr int64_t kStartCost = 3500, kPartCost = 1500, kLeast = 2500;   // the least that a piece is cut to
+int64_t turn_cost(int dtype, int hd, int tiles) {
+  if (dtype != WISP_BF16) return (int64_t)hd * 27 * shared_wgs_per_cu(dtype, hd);   // its products
+  return (tiles > 2 ? 900 : 1200) * (hd + 64) / 192;
 }
-// When the last workgroup ends, the longest items first, and what the join adds
-int64_t time_of(const std::vector<Segment> &segs, int64_t share, int64_t slots) {
+
+struct Bundle {
+  int32_t seg, tile0, tiles, tokens;                // first row tile, row tiles; token tiles up to its last row's limit
+  int64_t turns, turn;                              // and the cost of one
+  bool joined;                                      // its rows have other results to be joined with
+};
+struct Piece {                                      // turns from .. to - 1 of a bundle, a bundle's in order
+  int32_t bundle;
+  int64_t from, to;
+};
+int64_t cost_of(const std::vector<Bundle> &bundles, const Piece &x) { return kStartCost + (x.to - x.from) * bundles[x.bundle].turn; }
+
+// Bundles longer than `share` (a start and the least of any, or more) are laid one behind another over shares of that length and cut at their borders; the
+// others stay whole.
+std::vector<Piece> pieces_of(const std::vector<Bundle> &bundles, int64_t share) {
+  std::vector<Piece> pieces;
+  int64_t room = share;
+  for (size_t k = 0; k < bundles.size(); ++k) {
+    const Bundle &u = bundles[k];
+    const int64_t least = std::max<int64_t>(1, (kLeast + u.turn / 2) / u.turn);
+    int64_t at = 0;
+    while (kStartCost + (u.turns - at) * u.turn > (at ? room : share)) {
+      int64_t n = (room - kStartCost) / u.turn;
+      if (n >= u.turns - at) break;
+      if (n >= least) {
+        n = std::min(n, std::max<int64_t>(u.turns - at - least, 1));
+        pieces.push_back(Piece{(int32_t)k, at, at + n});
+        at += n;
+      }
+      room = share;
+    }
+    pieces.push_back(Piece{(int32_t)k, at, u.turns});
+    if (at) room -= cost_of(bundles, pieces.back());
+  }
+  return pieces;
+}
+// When the last workgroup ends, the longest pieces first, and what the join adds
+int64_t time_of(const std::vector<Bundle> &bundles, const std::vector<Piece> &pieces, int64_t slots) {
   std::vector<int64_t> cost;
   int64_t joined = 0;
-  for (const Segment &s : segs) {
-    const Tokens t = tokens_of(s);
-    const int64_t n = parts_of(s, share);
-    for (int64_t x = 0; x < n; ++x) {
-      cost.insert(cost.end(), t.full, kStartCost + (t.cost(4) + n - 1) / n);
-      if (t.rest) cost.push_back(kStartCost + (t.cost((int)t.rest) + n - 1) / n);
-    }
-    if (n > 1) joined += n * s.tiles;
+  for (const Piece &x : pieces) {
+    const Bundle &u = bundles[x.bundle];
+    cost.push_back(cost_of(bundles, x));
+    if (u.joined || x.to - x.from < u.turns) joined += u.tiles;
   }
   std::sort(cost.begin(), cost.end(), std::greater<int64_t>());
   std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> ends;
@@ -120,78 +140,97 @@ int64_t time_of(const std::vector<Segment> &segs, int64_t share, int64_t slots) 
   return last + joined * kPartCost / slots;
 }
 
-wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<SharedJoin> &joins, const std::vector<int32_t> &pre_seg, int G) {
+wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<SharedRow> &joins, const std::vector<int32_t> &pre_seg, int G) {
   SharedPlan &p = b.p;
-  // every kv head has its part of the workgroups that run at once
-  const int64_t slots = std::max<int64_t>(1, (int64_t)device_cus() * shared_wgs_per_cu(p.dtype, p.hd) / p.nkv);
-  int64_t total = 0, bundles = 0;
+  int64_t count = 0;
   for (Segment &s : segs) {
     s.tiles = (int32_t)(((int64_t)s.nrow * G + kTile - 1) / kTile);
-    const Tokens t = tokens_of(s);
-    total += t.full * t.cost(4) + t.cost((int)t.rest);
-    bundles += t.full + (t.rest > 0);
+    count += (s.tiles + kBundle - 1) / kBundle;
   }
-  if (bundles > kSharedMaxItems / p.nkv) return too_many(bundles * p.nkv);
-  // Items of an equal share of the work leave a last round of few, smaller ones more to start and to join: the
-  // best of some sizes.  With many more bundles than workgroups the rounds are short by themselves.
-  int64_t share = std::max<int64_t>(total / slots + 1, kStartCost);
-  if (bundles < 8 * slots) {
-    int64_t best = INT64_MAX, at = share;
-    for (int64_t f = 3; f <= 16; ++f) {
-      const int64_t c = std::max<int64_t>(share * f / 12, 1), t = time_of(segs, c, slots);
+  if (count > kSharedMaxItems / p.nkv) return too_many(count * p.nkv);
+  std::vector<Bundle> bundles;
+  int64_t total = 0, longest = 0;
+  for (size_t k = 0; k < segs.size(); ++k) {
+    Segment &s = segs[k];
+    s.bundle0 = (int32_t)bundles.size();
+    for (int32_t t = 0; t < s.tiles; t += kBundle) {
+      Bundle u{};
+      u.seg = (int32_t)k;
+      u.tile0 = t;
+      u.tiles = std::min(kBundle, s.tiles - t);
+      const int64_t last = std::min<int64_t>((int64_t)s.nrow * G, (int64_t)(t + u.tiles) * kTile) - 1;
+      u.tokens = (int32_t)((std::min<int64_t>(s.t1, s.ctx + last / G + 1) - s.t0 + kTile - 1) / kTile);
+      u.turns = u.tiles > 2 ? u.tokens : (u.tokens * (int64_t)u.tiles + 3) / 4;
+      u.turn = turn_cost(p.dtype, p.hd, u.tiles);
+      longest = std::max(longest, u.turn);
+      u.joined = s.req < 0 || pre_seg[s.req] >= 0;
+      total += kStartCost + u.turns * u.turn;
+      bundles.push_back(u);
+    }
+  }
+  // Every kv head has its part of the workgroups that run at once.  Equal shares of the work, or longer ones, of which
+  // fewer bundles are cut, or shorter ones, of which the last round is shorter: the best by the costs above.  With many
+  // more bundles than workgroups none is cut.
+  const int64_t slots = std::max<int64_t>(1, (int64_t)device_cus() * shared_wgs_per_cu(p.dtype, p.hd) / p.nkv);
+  std::vector<Piece> pieces;
+  if ((int64_t)bundles.size() < 8 * slots) {
+    int64_t best = INT64_MAX;
+    for (int64_t f : {40, 50, 60, 70, 80, 90, 100, 110, 125, 150, 200, 300}) {
+      const int64_t share = std::max(total / slots * f / 100, kStartCost + kLeast + longest);
+      std::vector<Piece> x = pieces_of(bundles, share);
+      const int64_t t = time_of(bundles, x, slots);
       if (t < best) {
         best = t;
-        at = c;
+        pieces.swap(x);
       }
     }
-    share = at;
+  } else {
+    pieces = pieces_of(bundles, INT64_MAX);
   }
+  if ((int64_t)pieces.size() > kSharedMaxItems / p.nkv) return too_many((int64_t)pieces.size() * p.nkv);
   std::vector<SharedItem> items;
-  std::vector<int64_t> cost;
-  int64_t tiles_at = 0, n_items = 0;
-  for (Segment &s : segs) {
-    const int64_t n = tokens_of(s).tiles;
-    s.parts = parts_of(s, share);
-    const bool alone = s.parts == 1 && s.req >= 0 && pre_seg[s.req] < 0;
-    s.at = (int32_t)tiles_at;
-    if (!alone) tiles_at += (int64_t)s.tiles * s.parts * p.nkv;
-    n_items += (int64_t)((s.tiles + 3) / 4) * s.parts;
-    if (n_items > kSharedMaxItems / p.nkv || tiles_at > INT32_MAX) return too_many(n_items * p.nkv);
-    for (int32_t x = 0; x < s.parts; ++x) {
-      const int32_t from = (int32_t)(n * x / s.parts), to = (int32_t)(n * (x + 1) / s.parts);
-      for (int32_t k = 0; k < s.tiles; k += 4) {
-        const int32_t m = std::min(4, s.tiles - k);
-        items.push_back(SharedItem{s.table, s.t0 + from * kTile, std::min(s.t1, s.t0 + to * kTile), s.ctx, s.row0, s.nrow, k, m,
-                                   alone ? -1 : (int32_t)(s.at + (int64_t)x * p.nkv * s.tiles + k), s.tiles, {0, 0}});
-        cost.push_back(kTurnCost[m] * (m > 2 ? to - from : ((to - from) * m + 3) / 4));
-      }
+  std::vector<SharedBundle> table;
+  int64_t at = 0;
+  for (size_t k = 0; k < pieces.size();) {
+    const Bundle &u = bundles[pieces[k].bundle];
+    const Segment &s = segs[u.seg];
+    int32_t n = 0;
+    while (k + n < pieces.size() && pieces[k + n].bundle == pieces[k].bundle) ++n;
+    const bool alone = n == 1 && !u.joined;
+    if (at + (int64_t)n * p.nkv * u.tiles > INT32_MAX) return too_many(at);
+    for (int32_t x = 0; x < n; ++x) {
+      const Piece &y = pieces[k + x];
+      auto token = [&](int64_t turn) {              // of a turn's first tile; the waves that share tokens take 4 / tiles of them
+        const int64_t tile = u.tiles > 2 ? turn : turn * 4 / u.tiles;
+        return (int32_t)std::min<int64_t>((int64_t)u.tokens * kTile, tile * kTile);
+      };
+      items.push_back(SharedItem{s.table, s.t0 + token(y.from), std::min(s.t1, s.t0 + token(y.to)), s.ctx, s.row0, s.nrow, u.tile0, u.tiles,
+                                 alone ? -1 : (int32_t)(at + (int64_t)x * p.nkv * u.tiles), u.tiles, {0, 0}});
     }
-    if (s.req >= 0) {
-      SharedJoin &j = joins[s.req];
-      j.own_at = s.at;
-      j.own = s.parts;
-      j.own_tiles = s.tiles;
-      j.pre_row *= G;
-      if (!alone) p.joined = 1;
+    table.push_back(SharedBundle{(int32_t)at, n, u.tiles, 0});
+    if (!alone) {
+      at += (int64_t)n * p.nkv * u.tiles;
+      p.joined = 1;
     }
+    k += n;
   }
-  for (size_t r = 0; r < joins.size(); ++r)
-    if (pre_seg[r] >= 0) {
-      const Segment &s = segs[pre_seg[r]];
-      joins[r].pre_at = s.at;
-      joins[r].pre = s.parts;
-      joins[r].pre_tiles = s.tiles;
-    }
+  for (SharedRow &j : joins) {
+    j.own = segs[j.own].bundle0;
+    j.own_row *= G;
+    if (j.pre >= 0) j.pre = segs[j.pre].bundle0;
+    j.pre_row *= G;
+  }
   // the longest first: the last ones to start are short
   std::vector<int32_t> order(items.size());
   std::iota(order.begin(), order.end(), 0);
-  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return cost[x] > cost[y]; });
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return cost_of(bundles, pieces[x]) > cost_of(bundles, pieces[y]); });
   std::vector<SharedItem> sorted;
   sorted.reserve(items.size());
   for (int32_t x : order) sorted.push_back(items[x]);
   p.n_items = (int32_t)sorted.size();
-  p.n_parts = (int32_t)tiles_at;
+  p.n_parts = (int32_t)at;
   b.i_items = put(b.host, sorted);
+  b.i_bundles = put(b.host, table);
   return WISP_OK;
 }
 
@@ -250,7 +289,7 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   const int G = p.nq / p.nkv;
   if (G > 64) return fail(WISP_E_UNSUPPORTED, "GQA group > 64");
   std::vector<Segment> segs;
-  std::vector<SharedJoin> joins;
+  std::vector<SharedRow> joins;
   std::vector<int32_t> pre_seg, row;
   if ((st = segments_of(segs, joins, pre_seg, d, n_groups, size, prefix)) != WISP_OK) return st;
   for (const Segment &s : segs)
@@ -265,6 +304,7 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   b.i_join = put(b.host, joins);
   const size_t desc = 256;
   p.w_items = desc + b.i_items * 4;
+  p.w_bundles = desc + b.i_bundles * 4;
   p.w_row = desc + b.i_row * 4;
   p.w_join = desc + b.i_join * 4;
   p.w_mass = desc + b.i_mass * 4;

@@ -108,7 +108,7 @@ __device__ __forceinline__ void loads_done() {
   asm volatile("" ::: "memory");
 }
 
-// x / d for x below 2^26 and d of 1 .. 64: one product (the quotient of a variable takes twenty instructions)
+// x / d for x d below 2^32: one product (the quotient of a variable takes twenty instructions)
 struct Divisor {
   uint32_t d, m;
   __device__ __forceinline__ explicit Divisor(int by) : d(by), m(0xFFFFFFFFu / (uint32_t)by + 1) {}
