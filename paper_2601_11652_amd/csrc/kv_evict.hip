@@ -153,13 +153,19 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 }
 
 // Moves the kept tokens of a layer, kv head and request: a workgroup for 8 dims of K with the 8 that turn with
-// them and for 16 dims of V, its `runs` waves for 64 tokens each a turn.  All sources of a turn are read before its slots are written; those of later turns lie past them, as a token never moves
-// up.  So a cache is compacted in its own pages.  What a turn's tokens are is looked up while the turn before
-// runs, their positions two turns ahead.
+// them and for 16 dims of V, its `runs` waves for 64 tokens each a turn.  All sources of a turn are read before
+// its slots are written; those of later turns lie past them, as a token never moves up.  So a cache is compacted
+// in its own pages.  What a turn's tokens are is looked up while the turn before runs, their positions two turns
+// ahead.
 //
 // A page holds V by dims, eight slots of one in a row: the half pages that have kept tokens are read whole, and
 // their slots put in their new order in LDS (read one by one, at 2 bytes a lane, the cache's ports were the
 // bound: 32 requests of 2-8k tokens back to half, two layers, 496 us).
+//
+// Bound by HBM where there are many tokens: memory comes in lines of 128 bytes, which hold 8 slots of K or V, and
+// almost each has a token that stays.  That call reads 1306 MB (all of its old pages) and writes 617 in 409 us, 4.70
+// TB/s; a copy reaches 4.85.  kv heads are neighbours in the grid, one to an XCD: as its second index, 426 us.
+// A few requests are bound by latency: 2000 of 8000 tokens, one layer, 20 us.
 struct MoveArgs {
   EvictArgs e;
   double freq[128];                    // turns of a position's angle, of each dim below HD / 2
@@ -181,8 +187,9 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
   uint2 *halves = reinterpret_cast<uint2 *>(places + 2 * tokens);
   int *news = reinterpret_cast<int *>(halves + 2 * tokens), *n_halves = news + 2 * tokens / 16;   // [2][tokens / 16]; [2][runs]
   T *tile = reinterpret_cast<T *>(smem + ((2 * tokens * 16 + 10 * a.runs * 4 + 15) & ~15)) + wave * 1024;   // this wave's V, as in the new pages
-  const EvictReq r = a.reqs[blockIdx.x / OCT];
-  const int oct = blockIdx.x % OCT, t0 = wave * 64, kvh = blockIdx.y, layer = blockIdx.z;
+  const int rest = blockIdx.x / a.nkv;
+  const EvictReq r = a.reqs[rest / OCT];
+  const int oct = rest % OCT, t0 = wave * 64, kvh = blockIdx.x - rest * a.nkv, layer = blockIdx.z;
   const int32_t *pt = a.table + (int64_t)r.req * a.stride, *to = a.to + (int64_t)r.req * a.to_stride;
   const int32_t *kept = a.kept + ((int64_t)layer * a.nkv + kvh) * a.total + r.start;
   const int64_t layer_at = (int64_t)layer * a.n_blocks * a.nkv * PAGE;
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
   const int v_half = lane / 16 % 2;
 
   const int turns = (r.keep + tokens - 1) / tokens;
-    auto position = [&](int x) __attribute__((always_inline)) { return x * tokens + tid < r.keep ? kept[x * tokens + tid] : -1; };
+  auto position = [&](int x) __attribute__((always_inline)) { return x * tokens + tid < r.keep ? kept[x * tokens + tid] : -1; };
   int pos = position(0), blk = pos >= 0 ? pt[pos >> 4] : 0, new_page = pos >= 0 ? to[tid >> 4] : -1;
   float *mass = a.mass + (int64_t)layer * a.n_blocks * a.nkv * kPage;
   const bool weighs = oct == 0;                         // with one workgroup the weights move too
@@ -464,9 +471,10 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     const int n = (int)e.reqs.size();
     launch(e.most <= kSelectHeld * kSelectThreads ? evict_select_kernel<true> : evict_select_kernel<false>,
            dim3(n, a.nkv, model->n_layers), kSelectThreads, 0, s, a);
-    // Tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half, two
-    // layers (4096 workgroups), 449 us with 8 waves and 475 with 16; one of 8000 back to a quarter (64) 53 and 45.
-    const int oct = model->head_dim / 16, most_waves = (int64_t)n * a.nkv * model->n_layers * oct < device_cus() ? 16 : 8;
+    // Waves, of 64 tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half,
+    // two layers (4096 workgroups), 435 us with 8 waves, 438 with 4, 462 with 16; one of 8000 back to a quarter (64
+    // workgroups) 48 with 8 and 40 with 16, a small fp32 model's 12 requests (384) 40 and 36.
+    const int oct = model->head_dim / 16, most_waves = (int64_t)n * a.nkv * model->n_layers * oct < 2 * device_cus() ? 16 : 8;
     int most_kept = 0;
     for (const EvictReq &r : e.reqs) most_kept = std::max(most_kept, r.keep);
     a.runs = std::max(1, std::min(most_waves, (most_kept + 63) / 64));
@@ -475,7 +483,7 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
       move.freq[i] = std::pow((double)model->rope_base, -2.0 * i / model->head_dim) / (2 * 3.14159265358979323846);
     const uint32_t shm = ((2 * 64 * a.runs * 16 + 10 * a.runs * 4 + 15) & ~15) + (uint32_t)a.runs * 1024 * (model->dtype == WISP_BF16 ? 2 : 4);
     auto go = [&](auto kernel) {
-      launch(kernel, dim3((unsigned)n * oct, a.nkv, model->n_layers), 64 * a.runs, shm, s, move);
+      launch(kernel, dim3((unsigned)n * oct * a.nkv, 1, model->n_layers), 64 * a.runs, shm, s, move);
     };
     if (model->dtype == WISP_BF16) {
       if (model->head_dim == 128) go(evict_move_kernel<uint16_t, 128>);
