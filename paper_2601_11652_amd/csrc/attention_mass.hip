@@ -1,5 +1,15 @@
 // The attention weight that every cached token gets from a batch's rows: for token t and kv head h the sum
 // over rows r that see t, and query heads g of h, of exp(q . k_t / sqrt(head_dim) - lse).
+//
+// The scores are computed once more: they are one product and not two, and kept they would be the rows x tokens that the
+// attention does without.  A wave keeps the keys of 32 tokens in registers, as an operand, and adds up over the rows, which
+// stream through LDS for the four waves; sums of fp32 in registers, a row's place in them fixed, so results do not vary.
+//
+// For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: of a
+// row tile's 900 cycles a SIMD 256 are products and 424 vector instructions, 16 exponentials of 64 lanes among them.  Three
+// workgroups a CU hide most of the waits: 103 us, 680 TFLOP/s, where two took 105 (and for 32 sessions on a document 25 and
+// 32).  Two token tiles a wave, half the LDS reads, 118 us; the next tile's products beside a tile's exponentials, no
+// change.  A few rows over many tokens are bound by latency: 4000 tokens 8 us.
 #include <algorithm>
 #include <climits>
 
@@ -39,11 +49,14 @@ __device__ __forceinline__ void put_mass(const int32_t *page_table, int pt_strid
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mass_kernel(MassArgs a) {
+__global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mass_kernel(MassArgs a) {
   constexpr int KB = HD / 16, UNITS = HD * (int)sizeof(T) / 16, PIECES = UNITS / 2;   // 16-byte units of a row; 1 KiB pieces of a row tile
-  constexpr int TILES = PIECES <= 8 ? 4 : PIECES <= 16 ? 2 : 1;     // row tiles of a stage
+  constexpr int TILES = PIECES <= 8 ? 2 : 1, RING = 3;             // row tiles of a stage; stages in LDS
+  constexpr int STAGE = TILES * kTile;                              // its rows
   constexpr int SWIZZLE = UNITS % 16 ? 7 : 15;
-  __shared__ uint4 rows_of[2][TILES][kTile * UNITS];
+  __shared__ uint4 rows_of[RING][TILES][kTile * UNITS];
+  __shared__ float lse_of[RING][64];
+  __shared__ uint32_t counts[kMassTiles];                           // of a group: which rows count
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lc = lane & 31, hf = lane >> 5;
   const int kvh = blockIdx.x % a.nkv;
@@ -66,117 +79,73 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
   floatx16 acc;
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  // Row tiles go straight into LDS, whole rows at a time: unit u of row r lies at u ^ (r % 16 or 8), so that the rows' operands
-  // are read without bank conflicts (in operand order, each load took 32 bytes of 32 rows: 115 us for a prompt of
-  // 4096 rows).  Its rows' lse and how far they see are in registers.
-  struct Rows {
-    float lse;
-    int lim, row, count;                 // tokens that the lane's row sees; it counts if its row is below count
-  };
-  constexpr int WAVES = 4 / TILES, MINE = PIECES / WAVES;           // waves of a row tile's pieces; each one's
+  // Row tiles go straight into LDS, RING - 1 stages ahead, whole rows at a time: unit u of row r lies at u ^ (r % 16 or 8), so
+  // that the rows' operands are read without bank conflicts (in operand order, each load took 32 bytes of 32 rows: 115 us
+  // for a prompt of 4096 rows).  Their lse goes with them.
+  constexpr int WAVES = 4 / TILES, MINE = PIECES / WAVES, LOADS = MINE + 1;   // waves of a row tile's pieces; each one's; and the lse
   static_assert(PIECES % WAVES == 0, "a tile's pieces are shared equally");
   const Divisor by_g(G);
   // Where the query heads of a kv head divide a stage's rows (and the stage is whole) its rows lie as those of the stage
   // before, so many tokens on: their places are kept, and only a uniform address moves.
-  constexpr int STAGE = TILES * kTile;
   const int my_tile = wave / WAVES, p0 = wave % WAVES * MINE;
   const bool steady = STAGE % G == 0;
   const int step = STAGE / G;            // rows of the batch, of a steady stage
-  auto row_at = [&](int f, int64_t &at) __attribute__((always_inline)) {   // of flat row f: its query's place, in heads
+  auto row_at = [&](int f) __attribute__((always_inline)) {          // of flat row f: its query's place, in heads
     const int c = min(f, rows - 1), j = by_g.of(c);
-    at = (int64_t)(it.row0 + j) * a.nq + kvh * G + c - j * G;
-    return j;
+    return (int64_t)(it.row0 + j) * a.nq + kvh * G + c - j * G;
   };
-  uint32_t q_off[MINE], lse_off[TILES];
-  int first_row[TILES];
-  int64_t head0;                         // the first row's query
-  row_at(it.r0, head0);
+  uint32_t q_off[MINE];
+  const int64_t head0 = row_at(it.r0);   // the first row's query
+  const uint32_t lse_off = (uint32_t)(row_at(it.r0 + lane) - head0) * 4;
 #pragma unroll
   for (int x = 0; x < MINE; ++x) {
     const int at = (p0 + x) * 64 + lane, row = at / UNITS;
-    int64_t head;
-    row_at(it.r0 + my_tile * kTile + row, head);
-    q_off[x] = (uint32_t)((head - head0) * (HD * (int)sizeof(T))) + 16 * (at % UNITS ^ (row & SWIZZLE));
+    q_off[x] = (uint32_t)((row_at(it.r0 + my_tile * kTile + row) - head0) * (HD * (int)sizeof(T))) + 16 * (at % UNITS ^ (row & SWIZZLE));
   }
-#pragma unroll
-  for (int x = 0; x < TILES; ++x) {
-    int64_t head;
-    first_row[x] = row_at(it.r0 + x * kTile + lc, head);
-    lse_off[x] = (uint32_t)(head - head0);
-  }
-  // stage n of the item, rows r ..
-  auto bring = [&](int n, int r, int b) __attribute__((always_inline)) {
-    if (steady && r + STAGE <= rows) {
-      const T *base = static_cast<const T *>(a.q) + (head0 + (int64_t)n * step * a.nq) * HD;
+  auto bring = [&](int n) __attribute__((always_inline)) {           // stage n of the item
+    const int b = n % RING, r = it.r0 + n * STAGE;
+    if (steady && r + 64 <= rows) {
+      const int64_t head = head0 + (int64_t)n * step * a.nq;
+      const T *base = static_cast<const T *>(a.q) + head * HD;
 #pragma unroll
       for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], &rows_of[b][my_tile][(p0 + x) * 64]);
+      lds_dma4_at(a.lse + head, lse_off, &lse_of[b][0]);
     } else {
 #pragma unroll
       for (int x = 0; x < MINE; ++x) {
         const int at = (p0 + x) * 64 + lane, row = at / UNITS;
-        int64_t head;
-        row_at(r + my_tile * kTile + row, head);
-        lds_dma16(reinterpret_cast<const char *>(static_cast<const T *>(a.q) + head * HD) + 16 * (at % UNITS ^ (row & SWIZZLE)), &rows_of[b][my_tile][(p0 + x) * 64]);
+        lds_dma16(reinterpret_cast<const char *>(static_cast<const T *>(a.q) + row_at(r + my_tile * kTile + row) * HD) + 16 * (at % UNITS ^ (row & SWIZZLE)),
+                  &rows_of[b][my_tile][(p0 + x) * 64]);
       }
+      const int64_t first = row_at(r);
+      lds_dma4_at(a.lse + first, (uint32_t)(row_at(r + lane) - first) * 4, &lse_of[b][0]);
     }
   };
-  // A group's rows count by their requests: (request, row in it) is asked for two stages ahead, the request's
-  // count one, so that nothing waits for what is on its way
   const bool by_request = a.count && it.req < 0;
-  auto request = [&](int r) __attribute__((always_inline)) {
-    return by_request ? *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + by_g.of(min(r + lc, rows - 1)))) : make_int2(0, 0);
-  };
-  auto figures = [&](int n, int x, int r, int2 of) __attribute__((always_inline)) {
-    Rows w;
-    int j;
-    if (steady && r + kTile <= rows) {
-      w.lse = (a.lse + head0 + (int64_t)n * step * a.nq)[lse_off[x]];
-      j = first_row[x] + n * step;
-    } else {
-      int64_t head;
-      j = row_at(r + lc, head);
-      w.lse = a.lse[head];
-    }
-    w.count = by_request ? a.count[of.x] : INT_MAX;
-    w.row = of.y;
-    w.lim = r + lc < r_end ? it.ctx + j + 1 : 0;
-    return w;
-  };
+  const int stages = (r_end - it.r0 + STAGE - 1) / STAGE;
   if (it.r0 < r_end) {
-    loads_done();                        // K
-    Rows w[TILES];
-    int2 of[TILES];
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) of[x] = request(it.r0 + x * kTile);
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-      w[x] = figures(0, x, it.r0 + x * kTile, of[x]);
-      of[x] = request(it.r0 + STAGE + x * kTile);
+    for (int n = 0; n < min(stages, RING - 1); ++n) bring(n);
+    if (by_request) {
+      for (int f = it.r0 + threadIdx.x; f - lane < r_end; f += 256) {
+        const int2 of = *reinterpret_cast<const int2 *>(a.row + 2 * (int64_t)(it.row0 + by_g.of(min(f, rows - 1))));
+        const unsigned long long on = __builtin_amdgcn_ballot_w64(of.y < a.count[of.x]);
+        if (lane < 2 && (f - lane - it.r0) / kTile + lane < kMassTiles) counts[(f - lane - it.r0) / kTile + lane] = lane ? on >> 32 : on;
+      }
     }
-    bring(0, it.r0, 0);
-    int b = 0, n = 0;
-    for (int r0 = it.r0; r0 < r_end; r0 += STAGE, b ^= 1, ++n) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      Rows now[TILES];
+    loads_done();                        // K
+    floatx16 zero;                       // in registers: made anew for each tile, it would take 16 instructions
 #pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        now[x] = w[x];
-        now[x].lim = w[x].row < w[x].count ? w[x].lim : 0;
-      }
-      if (r0 + STAGE < r_end) {
-#pragma unroll
-        for (int x = 0; x < TILES; ++x) {
-          w[x] = figures(n + 1, x, r0 + STAGE + x * kTile, of[x]);
-          of[x] = request(r0 + 2 * STAGE + x * kTile);
-        }
-        bring(n + 1, r0 + STAGE, b ^ 1);
-      }
+    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+    asm volatile("" : "+v"(zero));
+    for (int n = 0; n < stages; ++n) {
+      const int r0 = it.r0 + n * STAGE, b = n % RING, behind = min(RING - 2, stages - 1 - n);
+      // this wave's loads of the stage have landed, and every wave's
+      if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (n + RING - 1 < stages) bring(n + RING - 1);
 #pragma unroll
       for (int y = 0; y < TILES; ++y) {
         if (r0 + y * kTile >= r_end) break;
-        floatx16 s;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
         // all operands asked for, then the products: a pair at a time, each pair waited for LDS
         Op8<T> q[KB];
 #pragma unroll
@@ -184,19 +153,26 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 2 : 1) void mas
 #pragma unroll
           for (int z = 0; z < (int)sizeof(T) / 2; ++z)
             q[kb].v[z] = rows_of[b][y][lc * UNITS + (((2 * kb + hf) * ((int)sizeof(T) / 2) + z) ^ (lc & SWIZZLE))];
+        const float lse = lse_of[b][y * kTile + lc];
+        const uint32_t on = by_request ? counts[n * TILES + y] : ~0u;
         __builtin_amdgcn_sched_barrier(0);
+        floatx16 s;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s = mma(s, kf[kb], q[kb]);
-        const float l2 = now[y].lse * kLog2e;
-        if (__builtin_amdgcn_ballot_w64(now[y].lim < tp + kTile || fabsf(l2) > kFarScore)) {
+        for (int kb = 0; kb < KB; ++kb) s = mma(kb ? s : zero, kf[kb], q[kb]);
+        const int f = r0 + y * kTile + lc;
+        // tokens that this lane's row sees: none where it does not count
+        const int lim = f < r_end && (on >> lc & 1) ? it.ctx + by_g.of(f) + 1 : 0;
+        const float l2 = lse * kLog2e;
+        if (__builtin_amdgcn_ballot_w64(lim < tp + kTile || fabsf(l2) > kFarScore)) {
           // rows that do not see a token, or do not count; and scores so large that the roundings on both sides
           // of the difference may make it positive
+          const int seen = lim - tp - 8 * hf;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float e = __builtin_fmaf(s[i], c_log2, -l2);
             if (fabsf(l2) > kFarScore) e = e > 0.f ? 0.f : e;
             e = __builtin_amdgcn_exp2f(e);
-            acc[i] += tp + reg_token(lane, i) < now[y].lim ? e : 0.f;
+            acc[i] += reg_token(0, i) < seen ? e : 0.f;
           }
         } else {
 #pragma unroll
@@ -239,6 +215,8 @@ __global__ __launch_bounds__(kMassBlock) void mass_join_kernel(const MassJoin *j
 }
 
 }  // namespace
+
+int mass_wgs_per_cu(int dtype, int hd) { return dtype == WISP_BF16 || hd <= 64 ? 3 : 1; }
 
 void shared_mass(const SharedPlan &p, const SharedCache &c, const void *q, const float *lse, const int32_t *count, float decay,
                  const float *prev, float *mass, int *err, hipStream_t s) {

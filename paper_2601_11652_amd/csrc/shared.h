@@ -40,6 +40,7 @@ struct MassJoin {                      // a token block whose sums have several 
 
 constexpr int kBundle = 4;             // row tiles of a workgroup
 constexpr int kMassBlock = 4 * kTile;  // tokens of a workgroup: a tile a wave
+constexpr int kMassTiles = 512;       // row tiles of an item at most
 constexpr int kSharedMaxItems = 1 << 22;
 
 struct SharedPlan {                    // a wisp_shared_batch
@@ -60,7 +61,8 @@ struct SharedCache {                   // one layer's pools
 void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, void *out, float *lse, int *err, hipStream_t s);
 void shared_mass(const SharedPlan &p, const SharedCache &c, const void *q, const float *lse, const int32_t *count, float decay,
                  const float *prev, float *mass, int *err, hipStream_t s);
-// workgroups of the attention that a CU holds
+// workgroups that a CU holds
 int shared_wgs_per_cu(int dtype, int hd);
+int mass_wgs_per_cu(int dtype, int hd);
 
 }  // namespace wisp

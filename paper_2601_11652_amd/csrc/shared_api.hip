@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <climits>
 #include <cstring>
+#include <map>
 #include <numeric>
 #include <queue>
 
@@ -234,27 +235,44 @@ wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<Sha
   return WISP_OK;
 }
 
-// A token block's sums over its rows, in parts where there are few blocks for many rows
+// A token block's sums over its rows, in parts where that ends sooner (sixteen row tiles in one item: 24 us; in parts of 4,
+// 13).  In ns: an item's start and end, one of its row tiles, the parts and their sum.
+constexpr int64_t kMassStart = 4000, kMassTile = 900, kMassJoin = 8000;
+
 wisp_status plan_mass(Build &b, const std::vector<Segment> &segs, int G) {
   SharedPlan &p = b.p;
-  constexpr int64_t kShort = 16;                    // row tiles that are not worth a part
-  const int64_t slots = (int64_t)device_cus() * 2;
-  int64_t total = 0, blocks = 0;
+  const int64_t slots = (int64_t)device_cus() * mass_wgs_per_cu(p.dtype, p.hd);
+  int64_t blocks = 0;
   auto first_row = [&](const Segment &s, int64_t t0) {   // of those that see token t0
     return s.req < 0 ? 0 : std::max<int64_t>(0, (t0 - s.ctx) * G) / kTile * kTile;
   };
   for (const Segment &s : segs) blocks += (s.t1 - s.t0 + kMassBlock - 1) / kMassBlock;
   if (blocks > kSharedMaxItems / p.nkv) return too_many(blocks * p.nkv);
+  std::map<int64_t, int64_t> sizes;                      // row tiles of a block; blocks
   for (const Segment &s : segs)
-    for (int64_t t = s.t0; t < s.t1; t += kMassBlock) total += ((int64_t)s.nrow * G - first_row(s, t) + kTile - 1) / kTile;
-  // three items for a workgroup that runs at once: the last ones to end are short
-  const int64_t share = std::max<int64_t>(total * p.nkv / (3 * slots), kShort);
+    for (int64_t t = s.t0; t < s.t1; t += kMassBlock) ++sizes[((int64_t)s.nrow * G - first_row(s, t) + kTile - 1) / kTile];
+  int64_t share = kMassTiles, best = INT64_MAX;
+  for (int64_t c : {4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 256, kMassTiles}) {
+    int64_t sum = 0, longest = 0;
+    bool cut = false;
+    for (auto [n, count] : sizes) {
+      const int64_t parts = std::max<int64_t>(1, n / c);
+      sum += count * (parts * kMassStart + n * kMassTile);
+      longest = std::max(longest, kMassStart + (n + parts - 1) / parts * kMassTile);
+      cut |= parts > 1;
+    }
+    const int64_t t = std::max(longest, sum * p.nkv / slots) + (cut ? kMassJoin : 0);
+    if (t < best) {
+      best = t;
+      share = c;
+    }
+  }
   std::vector<MassItem> items;
   std::vector<MassJoin> joins;
   for (const Segment &s : segs)
     for (int64_t t = s.t0; t < s.t1; t += kMassBlock) {
       const int64_t r0 = first_row(s, t), rows = (int64_t)s.nrow * G, n = (rows - r0 + kTile - 1) / kTile;
-      const int64_t parts = std::max<int64_t>(1, n / share);
+      const int64_t parts = std::max<int64_t>({1, n / share, (n + kMassTiles - 1) / kMassTiles});
       const int32_t t1 = (int32_t)std::min<int64_t>(s.t1, t + kMassBlock);
       if ((int64_t)items.size() + parts > kSharedMaxItems / p.nkv || b.mass_parts + parts * p.nkv * kMassBlock > INT32_MAX)
         return too_many(((int64_t)items.size() + parts) * p.nkv);

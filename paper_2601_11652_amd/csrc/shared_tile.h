@@ -101,6 +101,12 @@ __device__ __forceinline__ void lds_dma16_at(const void *base, uint32_t offset, 
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(m0) : "memory", "m0");
 }
 
+// four bytes a lane
+__device__ __forceinline__ void lds_dma4_at(const void *base, uint32_t offset, const void *dst) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)dst);
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(m0) : "memory", "m0");
+}
+
 // Every load so far has returned, and the compiler knows it: operands that are first used inside a loop would make it
 // wait there, in every turn, for whatever has been asked for since.
 __device__ __forceinline__ void loads_done() {
