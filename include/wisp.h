@@ -410,7 +410,8 @@ wisp_status wisp_attention_mass(const wisp_shared_batch *batch, const wisp_kv *k
  * aligned, wisp_kv_evict_workspace_size bytes; its first 256 bytes the fault record of wisp_check) may be used again by
  * a call on a stream ordered after this one.  Reads of block ids out of range are undefined, writes are left
  * out.  While `stream` is being captured the requests' figures travel as kernel arguments.
- * WISP_E_CAPACITY: a table too short for ctx_len or keep.
+ * WISP_E_CAPACITY: a table too short for ctx_len or keep.  WISP_E_UNSUPPORTED: requests x n_kv_heads x head_dim / 16 of
+ * 2^22 or more, n_blocks x n_kv_heads of 2^27 or more, more than 65535 layers or kv heads, or 2^31 tokens kept.
  */
 size_t wisp_kv_evict_workspace_size(const wisp_model *model, const wisp_batch_desc *desc);
 wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp_batch_desc *desc, const int32_t *keep,

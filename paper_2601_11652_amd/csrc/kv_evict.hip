@@ -440,6 +440,9 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
         return fail(WISP_E_CAPACITY, "request %d keeps %d tokens but its new pages hold %d", r.req, r.keep, stride * WISP_PAGE);
     }
     if ((int64_t)kv->n_blocks * model->n_kv_heads >= 1 << 27) return fail(WISP_E_UNSUPPORTED, "n_blocks x n_kv_heads of 2^27 or more");
+    const int oct = model->head_dim / 16;
+    if ((int64_t)e.reqs.size() * model->n_kv_heads * oct >= 1 << 22)   // a launch's threads fit in 32 bits
+      return fail(WISP_E_UNSUPPORTED, "requests x n_kv_heads x head_dim / 16 of 2^22 or more");
     if (model->n_layers > 65535 || model->n_kv_heads > 65535) return fail(WISP_E_UNSUPPORTED, "more than 65535 layers or kv heads");
     if (!workspace) return fail(WISP_E_INVALID, "NULL workspace");
     if ((uintptr_t)workspace & 255) return fail(WISP_E_INVALID, "workspace must be 256-byte aligned");
@@ -474,7 +477,7 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     // Waves, of 64 tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half,
     // two layers (4096 workgroups), 435 us with 8 waves, 438 with 4, 462 with 16; one of 8000 back to a quarter (64
     // workgroups) 48 with 8 and 40 with 16, a small fp32 model's 12 requests (384) 40 and 36.
-    const int oct = model->head_dim / 16, most_waves = (int64_t)n * a.nkv * model->n_layers * oct < 2 * device_cus() ? 16 : 8;
+    const int most_waves = (int64_t)n * a.nkv * model->n_layers * oct < 2 * device_cus() ? 16 : 8;
     int most_kept = 0;
     for (const EvictReq &r : e.reqs) most_kept = std::max(most_kept, r.keep);
     a.runs = std::max(1, std::min(most_waves, (most_kept + 63) / 64));

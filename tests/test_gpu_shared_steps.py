@@ -1,0 +1,191 @@
+"""Batches on shared prefixes as a server runs them: attention, the weights that it gives, eviction by them, the
+next step; and the shapes whose work is cut into many parts."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2601_11652_amd as W
+from gpu_harness import log, to_dev
+from oracle import shared
+from shared_harness import HALF, U, Case, bits, from_pages, to_pages
+from test_gpu_shared import check_attention, check_mass
+
+pytestmark = pytest.mark.gpu
+
+# groups of (prefix, [(own cached tokens, rows)]), query heads, kv heads, head_dim, bf16
+CUT = [
+    ([(64, [(3, 9)] * 40)], 64, 1, 64, True),               # 720 row tiles of one kv head
+    ([(0, [(9000, 1)]), (0, [(20000, 2)])], 6, 2, 128, True),   # long requests, one row tile each
+    ([(16000, [(0, 1), (40, 1)])], 8, 2, 64, True),
+    ([(128, [(1, 2)] * 70)], 12, 4, 128, True),              # three query heads per kv head: no tile starts with a row
+    ([(64, [(3, 2), (1, 1)])], 64, 1, 256, False),           # a row's heads take several workgroups of the join
+    ([(256, [(0, 300)]), (0, [(5, 1)])], 5, 1, 256, False),
+    ([(3200, [(17, 3), (33, 1)])], 7, 1, 32, False),
+    ([(16, [(2, 700)]), (0, [(900, 130)])], 4, 2, 128, True),
+    ([(2048, [(1, 1)] * 33)], 3, 3, 128, True),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CUT)))
+def test_work_that_is_cut_into_parts(case):
+    log(f"parts {CUT[case]}")
+    c = Case(*CUT[case], seed=500 + case)
+    kv, plan = c.pool(), c.plan()
+    out, lse = c.run(kv, plan)
+    check_attention(c, out, lse)
+    l = torch.from_numpy(lse).float().cuda()
+    shp = (c.k.shape[0], c.n_kv, 16)
+    before = c.rng.normal(0, 1, shp).astype(np.float32)
+    for count in (None, c.rng.integers(0, c.nrow + 1).astype(np.int32)):
+        m = to_dev(before)
+        W.wisp_attention_mass(plan, kv, c.dev_q(), l, m, None, 1.0, None if count is None else to_dev(count))
+        W.wisp_check(plan.ws)
+        check_mass(c, m.double().cpu().numpy(), lse, count, 1.0, None, before)
+        again = to_dev(before)
+        W.wisp_attention_mass(plan, kv, c.dev_q(), l, again, None, 1.0, None if count is None else to_dev(count))
+        assert torch.equal(m, again)
+
+
+def step(c, kv, mass, count, decay):
+    """Attention over one layer, checked, and the weights that its counting rows give, in place."""
+    plan = c.plan()
+    out, lse = c.run(kv, plan)
+    check_attention(c, out, lse)
+    before = mass.double().cpu().numpy()
+    W.wisp_attention_mass(plan, kv, c.dev_q(), torch.from_numpy(lse).float().cuda(), mass, mass, decay, to_dev(count))
+    W.wisp_check(plan.ws)
+    check_mass(c, mass.double().cpu().numpy(), lse, count, decay, before, before)
+
+
+def evict(c, kv, mass, keep, sink, recent):
+    """In place, checked; the case's host arrays then hold what the device does."""
+    desc = W.BatchDesc(c.ctx, np.zeros(len(c.ctx), np.int32), c.desc.page_table)
+    kept = torch.full((1, c.n_kv, int(np.minimum(keep, c.ctx).sum())), -9, dtype=torch.int32, device="cuda")
+    k, v, m = c.k[None].copy(), c.v[None].copy(), mass.cpu().numpy()[None]
+    want, pair = shared.evict(k, v, m, c.pt, c.ctx, keep, sink, recent, c.pt, 1e4)
+    ws = W.workspace(W.wisp_kv_evict_workspace_size(c.model, desc))
+    W.wisp_kv_evict(c.model, kv, desc, keep, mass, kept, ws, sink, recent)
+    W.wisp_check(ws)
+    np.testing.assert_array_equal(kept.cpu().numpy(), want)
+    np.testing.assert_array_equal(mass.cpu().numpy()[None].view(np.int32), m.view(np.int32))
+    got = from_pages(kv.k, "k", c.hd).double().numpy()
+    still, h = pair == 0, HALF[c.bf16]
+    np.testing.assert_array_equal(got[still], k[still])
+    # as in the tests of the eviction by itself: an angle, its sine and cosine, two products and their sum; one rounding
+    assert np.all((np.abs(got - k) <= h * np.abs(k) + 10 * U * (1 + h) * pair)[~still])
+    np.testing.assert_array_equal(bits(from_pages(kv.v, "v", c.hd)), bits(from_pages(to_pages(v, "v", c.bf16), "v", c.hd)))
+    c.k, c.v = got[0], v[0]
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_steps_with_evictions_between(bf16):
+    """Three requests on a common prefix (which stays, where it is) and one alone decode in steps; after each their
+    counting rows enter the cache, and the least attended tokens leave it."""
+    c = Case([(96, [(60, 4), (85, 3), (33, 6)]), (0, [(170, 2)])], 8, 2, 64, bf16, seed=71, spare=4)
+    for i, page in enumerate(np.setdiff1d(np.arange(c.k.shape[0]), c.pt)):   # a page more for each, for its next tokens
+        c.pt[i, np.argmax(c.pt[i] < 0)] = page
+    c.desc = W.BatchDesc(c.ctx, c.gamma, to_dev(c.pt))
+    kv = c.pool()
+    mass = torch.zeros(c.k.shape[0], 2, 16, device="cuda")
+    sink = np.array([96, 96, 96, 4], np.int32)
+    for turn in range(4):
+        count = np.minimum(c.nrow, [2, 3, 1, 2]).astype(np.int32)
+        step(c, kv, mass, count, 0.9)
+        c.ctx = c.ctx + count
+        if turn % 2:
+            keep = np.array([96 + 40, 96 + 50, 200, 90], np.int32)        # of the third all stay
+            evict(c, kv, mass, keep, sink, np.array([8, 16, 0, 20], np.int32))
+            c.ctx = np.minimum(c.ctx, keep).astype(np.int32)
+        # the next rows' keys and values, as the step would have stored them
+        c.nrow = c.rng.integers(1, 5, 4).astype(np.int32)
+        c.gamma = c.nrow - 1
+        for i in range(4):
+            for t in range(int(c.ctx[i]), int(c.ctx[i] + c.nrow[i])):
+                for pool in (c.k, c.v):
+                    pool[c.pt[i, t // 16], :, t % 16] = c.round(c.rng.normal(0, 1.15, (2, 64)))
+        c.M, c.off = int(c.nrow.sum()), np.concatenate([[0], np.cumsum(c.nrow)])
+        c.q = c.round(c.rng.normal(0, 1.15, (c.M, 8, 64)))
+        kv = c.pool()
+        c.desc = W.BatchDesc(c.ctx, c.gamma, to_dev(c.pt))
+    step(c, kv, mass, c.nrow, 0.9)
+
+
+def test_a_step_and_its_eviction_in_one_graph():
+    """Plan, attention, weights and eviction captured together and replayed, each time on what the last one left, beside the
+    same calls made eagerly."""
+    c = Case([(32, [(300, 4), (85, 3)]), (0, [(170, 2)])], 8, 2, 64, True, seed=72)
+    keep, sink, recent = [150, 80, 60], [32, 32, 0], [10, 3, 20]
+    desc = W.BatchDesc(c.ctx, np.zeros(3, np.int32), c.desc.page_table)
+    q = c.dev_q()
+
+    def state():
+        return dict(kv=c.pool(), out=torch.zeros(c.M, 8, 64, dtype=torch.bfloat16, device="cuda"), lse=torch.zeros(c.M, 8, device="cuda"),
+                    mass=torch.zeros(c.k.shape[0], 2, 16, device="cuda"), kept=torch.zeros(1, 2, 290, dtype=torch.int32, device="cuda"),
+                    ws=W.workspace(W.wisp_shared_workspace_size(c.model, c.desc, c.size, c.prefix)),
+                    ews=W.workspace(W.wisp_kv_evict_workspace_size(c.model, desc)))
+
+    def calls(s):
+        s["plan"] = plan = W.wisp_shared_plan(c.model, c.desc, c.size, c.prefix, s["ws"])
+        W.wisp_attention_shared(plan, s["kv"], q, s["out"], s["lse"])
+        W.wisp_attention_mass(plan, s["kv"], q, s["lse"], s["mass"], s["mass"], 0.9)
+        W.wisp_kv_evict(c.model, s["kv"], desc, keep, s["mass"], s["kept"], s["ews"], sink, recent)
+
+    one, two = state(), state()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls(one)
+    for i in range(4):
+        q.copy_(torch.from_numpy(c.round(c.rng.normal(0, 1, c.q.shape))).cuda())
+        g.replay()
+        torch.cuda.synchronize()
+        calls(two)
+        for name in ("out", "lse", "mass", "kept"):
+            assert torch.equal(one[name].nan_to_num(7.0) if name != "kept" else one[name], two[name].nan_to_num(7.0) if name != "kept" else two[name]), (i, name)
+        for a, b in ((one["kv"].k, two["kv"].k), (one["kv"].v, two["kv"].v)):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), i
+    for s in (one, two):
+        W.wisp_check(s["ws"])
+        W.wisp_check(s["ews"])
+
+
+def test_two_batches_at_once_on_streams_of_their_own():
+    cs = [Case([(512, [(20, 5), (3, 4), (77, 1)])], 32, 8, 128, True, seed=73), Case([(64, [(200, 30)] * 3)], 8, 2, 64, True, seed=74)]
+    runs = []
+    for c in cs:
+        kv, plan = c.pool(), c.plan()
+        out, lse = c.run(kv, plan)
+        mass = torch.zeros(c.k.shape[0], c.n_kv, 16, device="cuda")
+        l = torch.from_numpy(lse).float().cuda()
+        W.wisp_attention_mass(plan, kv, c.dev_q(), l, mass)
+        runs.append((c, kv, c.plan(), c.dev_q(), torch.from_numpy(out).cuda(), l, mass, torch.cuda.Stream()))
+    outs = [[(torch.zeros(c.M, c.n_q, c.hd, dtype=torch.bfloat16, device="cuda"), torch.zeros_like(l), torch.zeros_like(m)) for _ in range(5)]
+            for c, _, _, _, _, l, m, _ in runs]
+    torch.cuda.synchronize()
+    for i in range(5):
+        for (c, kv, plan, q, *_, s), o in zip(runs, outs):
+            W.wisp_attention_shared(plan, kv, q, o[i][0], o[i][1], s)
+            W.wisp_attention_mass(plan, kv, q, o[i][1], o[i][2], stream=s)
+    torch.cuda.synchronize()
+    for (c, _, _, _, out, l, mass, _), o in zip(runs, outs):
+        for a, b, m in o:
+            assert torch.equal(a.double(), out) and torch.equal(b, l) and torch.equal(m, mass)
+
+
+def test_an_eviction_on_a_stream_of_its_own():
+    c = Case([(0, [(300, 1)]), (0, [(90, 1)])], 2, 2, 64, True, seed=75)
+    desc = W.BatchDesc(c.ctx, np.zeros(2, np.int32), c.desc.page_table)
+    weights = torch.rand(c.k.shape[0], 2, 16, device="cuda")
+    got = []
+    for s in (None, torch.cuda.Stream()):
+        kv, mass = c.pool(), weights.clone()
+        kept = torch.zeros(1, 2, 130, dtype=torch.int32, device="cuda")
+        ws = W.workspace(W.wisp_kv_evict_workspace_size(c.model, desc))
+        torch.cuda.synchronize()
+        W.wisp_kv_evict(c.model, kv, desc, [100, 30], mass, kept, ws, [4, 4], [8, 8], stream=s)
+        if s is not None:
+            s.synchronize()
+        W.wisp_check(ws)
+        got.append((kv.k.view(torch.int16), kv.v.view(torch.int16), mass, kept))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

@@ -126,6 +126,18 @@ def test_evictions(args, status):
     assert _evict(**args) == status, W.wisp_last_error()
 
 
+@pytest.mark.parametrize("model,n,blocks", [
+    (_model(8, 8, 128), 1 << 16, 4),                         # 2^22 workgroups of 1024 threads
+    (_model(1 << 17, 1 << 17, 64), 1, 4),                    # kv heads
+    (_model(8, 8, 64), 1, 1 << 24),                          # places in a pool
+])
+def test_evictions_beyond_the_kernels(model, n, blocks):
+    call = lambda n, blocks: _evict(model, _desc([2] * n), [1] * n, kv=W.wisp_kv(FAKE, FAKE, blocks, 16), nbytes=256)
+    assert call(n, blocks) == W.WISP_E_UNSUPPORTED, W.wisp_last_error()
+    if model.n_kv_heads <= 65535:                            # one less is refused for its workspace only
+        assert call(max(n - 1, 1), min(blocks, (1 << 24) - 1)) == W.WISP_E_WORKSPACE
+
+
 def test_evictions_of_nothing():
     """No request, or none that keeps a token: nothing to do, and no pointer is needed."""
     assert _evict(desc=_desc([], table=None), keep=[], mass=None, kept=None, ws=None) == W.WISP_OK
