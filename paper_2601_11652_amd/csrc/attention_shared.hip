@@ -1,5 +1,21 @@
 // Attention of a batch whose requests share prefixes: the rows of a group attend to their common tokens
 // together, each request's rows to its own, and the partial results of a row are joined.
+//
+// A row's result over tokens A and B is that over each with its maximum m and sum l of exp(s - m):
+// m = max(mA, mB), l = lA e^(mA - m) + lB e^(mB - m), o likewise; out = o / l, lse = m + ln l.  So a group's tokens are
+// read once for all its rows (128 samples of a prompt: 512 rows of a kv head, that would each have read it), and
+// their products have full tiles.
+//
+// A workgroup takes four row tiles of 32 (a wave each, K and V through LDS for all of them) or one or two (whose tokens the
+// waves share) over a run of tokens.  The host cuts the runs so that the workgroups that run at once end together.
+//
+// Bounds.  64 requests of a 64-head model on 8192 common tokens: 134 us, 763 TFLOP/s (a large library product reaches 1203
+// on this card): a turn of four waves over 32 tokens is 512 cycles of products and takes 915, as the maxima, exponentials and
+// roundings of 16 x 64 scores a wave take some 400 that the other workgroup's products hide in part only.  Scores of the next
+// tile beside a tile's exponentials: 146 -> 137 us.  Two row tiles a wave (half the LDS reads, one workgroup a CU): 167 us.
+// 128 samples of a prompt of 16384 tokens: 62 us, of which a third is what starts and ends an item (5 us: the item, its
+// queries and block ids, the first pages, each waiting for the one before) and 11 the join of 36 MB of partial results.  4
+// requests on 1024 tokens: 14 us, latency.
 #include <algorithm>
 #include <climits>
 

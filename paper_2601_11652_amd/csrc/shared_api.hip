@@ -74,9 +74,11 @@ wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedRow> &join
 }
 
 // Row tiles of a segment go in bundles of four, one a wave; of a bundle of one or two the four waves share the tokens.
-// What a workgroup's pass over 32 tokens (a turn) costs by the bundle's row tiles, what starting and ending an item
-// does, and a row tile's partial result, written and read again; in ns.
-constexpr int64_t kStartCost = 3500, kPartCost = 1500, kLeast = 2500;   // the least that a piece is cut to
+// In ns, as measured with two workgroups a CU: what starting and ending an item costs, a row tile's partial result, written
+// and read again, the least that a piece is cut to, and a pass over 32 tokens (a turn) by the bundle's row tiles.  (With
+// starts of 2500 or 7000, or turns a fifth shorter or longer, seven batches of twelve change by less than 2%, the others by
+// up to 25% either way.)
+constexpr int64_t kStartCost = 3500, kPartCost = 1500, kLeast = 2500;
 int64_t turn_cost(int dtype, int hd, int tiles) {
   if (dtype != WISP_BF16) return (int64_t)hd * 27 * shared_wgs_per_cu(dtype, hd);   // its products
   return (tiles > 2 ? 900 : 1200) * (hd + 64) / 192;
