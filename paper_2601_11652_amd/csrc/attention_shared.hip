@@ -476,28 +476,30 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 constexpr int kJoinParts = 8, kJoinThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedRow *rows, const SharedBundle *bundles, const float *part_o,
-                                                                   const float *part_ml, T *out, float *lse, int nq, int nkv, int hd,
-                                                                   int per_block, float scale) {
-  // per_block kv heads a workgroup; neighbouring threads have the heads of a kv head, whose results are neighbours
-  const int r = blockIdx.x, G = nq / nkv, ch = hd / 8;
-  const SharedRow j = rows[r];
-  const Divisor by_g(G), by_head(G * ch);
-  const int at = blockIdx.z * blockDim.x + threadIdx.x, local = by_head.of(at), u = at - local * G * ch, c = by_g.of(u), g = u - c * G;
-  const int kvh = blockIdx.y * per_block + local, c0 = 8 * c, head = kvh * G + g;
-  if (local >= per_block || kvh >= nkv) return;
+                                                                   const float *part_ml, T *out, float *lse, int n_rows, int nq, int nkv, int hd,
+                                                                   int together, int per_block, float scale) {
+  // Neighbouring threads have the heads of a kv head and then those of the next of `together` rows, whose results are
+  // neighbours: 128 bytes at least, a line.  per_block kv heads a workgroup.
+  const int G = nq / nkv, ch = hd / 8;
+  const Divisor by_g(G), by_rows(G * together), by_head(G * together * ch);
+  const int at = blockIdx.z * blockDim.x + threadIdx.x, local = by_head.of(at), u = at - local * G * together * ch, c = by_rows.of(u);
+  const int in_row = u - c * G * together, sub = by_g.of(in_row), g = in_row - sub * G;
+  const int kvh = blockIdx.y * per_block + local, c0 = 8 * c, head = kvh * G + g, r = blockIdx.x * together + sub;
+  if (local >= per_block || kvh >= nkv || r >= n_rows) return;
   const float c_log2 = scale * kLog2e;
-  const int f = j.own_row + g, k = f / (kBundle * kTile);
-  const SharedBundle b0 = bundles[j.own + k];
-  SharedBundle b1{0, 0, 0, 0};
-  int f1 = 0;
-  if (j.pre >= 0) {
-    f1 = j.pre_row + g;
-    b1 = bundles[j.pre + f1 / (kBundle * kTile)];
-    f1 %= kBundle * kTile;
+  SharedBundle b0 = rows[r].own, b1 = rows[r].pre;
+  int f0 = b0.row + g, f1 = b1.row + g;
+  if (f0 >= kBundle * kTile) {
+    b0 = bundles[rows[r].own_next];
+    f0 -= kBundle * kTile;
+  }
+  if (f1 >= kBundle * kTile && b1.parts) {
+    b1 = bundles[rows[r].pre_next];
+    f1 -= kBundle * kTile;
   }
   const int n = b0.parts + b1.parts;
   if (n < 2) return;                                  // written as it was computed
-  const int64_t own = ((int64_t)b0.at + (int64_t)kvh * b0.tiles) * kTile + f % (kBundle * kTile), own_step = (int64_t)nkv * b0.tiles * kTile;
+  const int64_t own = ((int64_t)b0.at + (int64_t)kvh * b0.tiles) * kTile + f0, own_step = (int64_t)nkv * b0.tiles * kTile;
   const int64_t pre = ((int64_t)b1.at + (int64_t)kvh * b1.tiles) * kTile + f1, pre_step = (int64_t)nkv * b1.tiles * kTile;
   float m = -INFINITY, den = 0.f;
   floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
@@ -588,12 +590,12 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
   if (!p.joined) return;
   const SharedRow *rows = reinterpret_cast<const SharedRow *>(p.ws + p.w_join);
   const SharedBundle *bundles = reinterpret_cast<const SharedBundle *>(p.ws + p.w_bundles);
-  const int of_head = p.nq / p.nkv * p.hd / 8, per_block = std::max(1, std::min(p.nkv, kJoinThreads / of_head));
-  const int threads = std::min(kJoinThreads, (per_block * of_head + 63) / 64 * 64);
-  const dim3 grid(p.rows, (p.nkv + per_block - 1) / per_block, (per_block * of_head + threads - 1) / threads);
+  const int G = p.nq / p.nkv, together = std::max(1, 8 / G), of_head = together * G * p.hd / 8;
+  const int per_block = std::max(1, std::min(p.nkv, kJoinThreads / of_head)), threads = std::min(kJoinThreads, (per_block * of_head + 63) / 64 * 64);
+  const dim3 grid((p.rows + together - 1) / together, (p.nkv + per_block - 1) / per_block, (per_block * of_head + threads - 1) / threads);
   auto join = [&](auto kernel, auto *to) {
     launch(kernel, grid, threads, 0, s, rows, bundles, (const float *)a.part_o, (const float *)a.part_ml, to, lse,
-           p.nq, p.nkv, p.hd, per_block, a.scale);
+           p.rows, p.nq, p.nkv, p.hd, together, per_block, a.scale);
   };
   if (p.dtype == WISP_BF16) join(shared_join_kernel<uint16_t>, static_cast<uint16_t *>(out));
   else join(shared_join_kernel<float>, static_cast<float *>(out));

@@ -21,10 +21,11 @@ struct SharedItem {                    // up to four row tiles of a segment over
 // from tile `at` on, a tile in the order of the accumulators.  A row has those of its own segment's
 // bundle, and of its group's; one in all was written as it was computed.
 struct SharedBundle {
-  int32_t at, parts, tiles, pad;
+  int32_t at, parts, tiles, row;       // row: in a SharedRow, the flat row in it
 };
-struct SharedRow {                     // of a row of the batch, head 0 of a kv head
-  int32_t own, own_row, pre, pre_row;  // first bundle of the request's segment, flat row there; of its group's (own -1: none)
+struct SharedRow {                     // of a row of the batch: where head 0 of a kv head lies
+  SharedBundle own, pre;               // in the request's segment, in its group's (no parts: there is none)
+  int32_t own_next, pre_next;          // the bundles behind them, in which the last heads of a row may lie
 };
 
 // Column sums of a segment's probabilities: tokens t0 .. t1 - 1 (at most a block of them), flat rows r0 .. r1 - 1

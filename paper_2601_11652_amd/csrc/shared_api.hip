@@ -24,6 +24,10 @@ struct Segment {
   int32_t tiles, bundle0;                           // row tiles; the first of its bundles
 };
 
+struct RowAt {                                      // a row's segment and its row there, and its group's (-1: none)
+  int32_t own, own_row, pre, pre_row;
+};
+
 struct Build {
   SharedPlan p{};
   std::vector<int32_t> host;
@@ -43,7 +47,7 @@ wisp_status too_many(int64_t n) {
   return fail(WISP_E_UNSUPPORTED, "the batch needs %lld work items (at most %d)", (long long)n, kSharedMaxItems);
 }
 
-wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedRow> &joins, std::vector<int32_t> &pre_seg,
+wisp_status segments_of(std::vector<Segment> &segs, std::vector<RowAt> &joins, std::vector<int32_t> &pre_seg,
                         const wisp_batch_desc *d, int32_t n_groups, const int32_t *size, const int32_t *prefix) {
   if (n_groups < 0) return fail(WISP_E_INVALID, "n_groups < 0");
   if (n_groups > 0 && (!size || !prefix)) return fail(WISP_E_INVALID, "group_size / prefix_len is NULL");
@@ -61,7 +65,7 @@ wisp_status segments_of(std::vector<Segment> &segs, std::vector<SharedRow> &join
     if (together) segs.push_back(Segment{i, 0, pre, kAll, row, 0, -1, 0, 0});
     for (int32_t r = i; r < i + n; ++r) {
       const int32_t nrow = rows_of(r), ctx = d->ctx_len[r];
-      for (int32_t x = 0; x < nrow; ++x) joins.push_back(SharedRow{(int32_t)segs.size(), x, shared, row - first + x});   // of segments, yet
+      for (int32_t x = 0; x < nrow; ++x) joins.push_back(RowAt{(int32_t)segs.size(), x, shared, row - first + x});   // of segments, yet
       pre_seg.push_back(shared);
       segs.push_back(Segment{r, together ? pre : 0, ctx + nrow, ctx, row, nrow, r, 0, 0});
       row += nrow;
@@ -143,7 +147,7 @@ int64_t time_of(const std::vector<Bundle> &bundles, const std::vector<Piece> &pi
   return last + joined * kPartCost / slots;
 }
 
-wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<SharedRow> &joins, const std::vector<int32_t> &pre_seg, int G) {
+wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<RowAt> &joins, const std::vector<int32_t> &pre_seg, int G) {
   SharedPlan &p = b.p;
   int64_t count = 0;
   for (Segment &s : segs) {
@@ -193,6 +197,7 @@ wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<Sha
   if ((int64_t)pieces.size() > kSharedMaxItems / p.nkv) return too_many((int64_t)pieces.size() * p.nkv);
   std::vector<SharedItem> items;
   std::vector<SharedBundle> table;
+  std::vector<SharedRow> rows;
   int64_t at = 0;
   for (size_t k = 0; k < pieces.size();) {
     const Bundle &u = bundles[pieces[k].bundle];
@@ -217,12 +222,21 @@ wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<Sha
     }
     k += n;
   }
-  for (SharedRow &j : joins) {
-    j.own = segs[j.own].bundle0;
-    j.own_row *= G;
-    if (j.pre >= 0) j.pre = segs[j.pre].bundle0;
-    j.pre_row *= G;
-  }
+  if (p.joined)
+    for (RowAt &j : joins) {
+      auto place = [&](int32_t seg, int32_t row, int32_t &next) {
+        if (seg < 0) return SharedBundle{0, 0, 0, 0};
+        const int32_t f = row * G, k = segs[seg].bundle0 + f / (kBundle * kTile);
+        next = std::min(k + 1, (int32_t)table.size() - 1);
+        SharedBundle x = table[k];
+        x.row = f % (kBundle * kTile);
+        return x;
+      };
+      SharedRow r{};
+      r.own = place(j.own, j.own_row, r.own_next);
+      r.pre = place(j.pre, j.pre_row, r.pre_next);
+      rows.push_back(r);
+    }
   // the longest first: the last ones to start are short
   std::vector<int32_t> order(items.size());
   std::iota(order.begin(), order.end(), 0);
@@ -234,6 +248,7 @@ wisp_status plan_attention(Build &b, std::vector<Segment> &segs, std::vector<Sha
   p.n_parts = (int32_t)at;
   b.i_items = put(b.host, sorted);
   b.i_bundles = put(b.host, table);
+  b.i_join = put(b.host, rows);
   return WISP_OK;
 }
 
@@ -309,7 +324,7 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   const int G = p.nq / p.nkv;
   if (G > 64) return fail(WISP_E_UNSUPPORTED, "GQA group > 64");
   std::vector<Segment> segs;
-  std::vector<SharedRow> joins;
+  std::vector<RowAt> joins;
   std::vector<int32_t> pre_seg, row;
   if ((st = segments_of(segs, joins, pre_seg, d, n_groups, size, prefix)) != WISP_OK) return st;
   for (const Segment &s : segs)
@@ -321,7 +336,6 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   p.rows = (int32_t)(row.size() / 2);
   if ((st = plan_attention(b, segs, joins, pre_seg, G)) != WISP_OK || (st = plan_mass(b, segs, G)) != WISP_OK) return st;
   b.i_row = put(b.host, row);
-  b.i_join = put(b.host, joins);
   const size_t desc = 256;
   p.w_items = desc + b.i_items * 4;
   p.w_bundles = desc + b.i_bundles * 4;
