@@ -473,13 +473,13 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 
 // The partial results of a row, joined in order: its own segment's, then its group's.  A thread for 8 dims of a
 // head; the loads of kJoinParts results are in flight at once.
-constexpr int kJoinParts = 8, kJoinThreads = 256;
+constexpr int kJoinParts = 8, kJoinThreads = 128;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedRow *rows, const SharedBundle *bundles, const float *part_o,
                                                                    const float *part_ml, T *out, float *lse, int n_rows, int nq, int nkv, int hd,
                                                                    int together, int per_block, float scale) {
   // Neighbouring threads have the heads of a kv head and then those of the next of `together` rows, whose results are
-  // neighbours: 128 bytes at least, a line.  per_block kv heads a workgroup.
+  // neighbours: 256 bytes, two lines.  per_block kv heads a workgroup.
   const int G = nq / nkv, ch = hd / 8;
   const Divisor by_g(G), by_rows(G * together), by_head(G * together * ch);
   const int at = blockIdx.z * blockDim.x + threadIdx.x, local = by_head.of(at), u = at - local * G * together * ch, c = by_rows.of(u);
@@ -590,7 +590,7 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
   if (!p.joined) return;
   const SharedRow *rows = reinterpret_cast<const SharedRow *>(p.ws + p.w_join);
   const SharedBundle *bundles = reinterpret_cast<const SharedBundle *>(p.ws + p.w_bundles);
-  const int G = p.nq / p.nkv, together = std::max(1, 8 / G), of_head = together * G * p.hd / 8;
+  const int G = p.nq / p.nkv, together = std::max(1, 16 / G), of_head = together * G * p.hd / 8;
   const int per_block = std::max(1, std::min(p.nkv, kJoinThreads / of_head)), threads = std::min(kJoinThreads, (per_block * of_head + 63) / 64 * 64);
   const dim3 grid((p.rows + together - 1) / together, (p.nkv + per_block - 1) / per_block, (per_block * of_head + threads - 1) / threads);
   auto join = [&](auto kernel, auto *to) {
