@@ -90,36 +90,36 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
   const int my_tile = wave / WAVES, p0 = wave % WAVES * MINE;
   const bool steady = STAGE % G == 0;
   const int step = STAGE / G;            // rows of the batch, of a steady stage
-  auto row_at = [&](int f) __attribute__((always_inline)) {          // of flat row f: its query's place, in heads
-    const int c = min(f, rows - 1), j = by_g.of(c);
-    return (int64_t)(it.row0 + j) * a.nq + kvh * G + c - j * G;
+  // of flat row f's query from row r's, in heads; j0: the batch's row of r
+  auto behind = [&](int r, int j0, int f) __attribute__((always_inline)) {
+    const int c = min(f, rows - 1);
+    return (uint32_t)((by_g.of(c) - j0) * (a.nq - G) + c - r);
   };
-  uint32_t q_off[MINE];
-  const int64_t head0 = row_at(it.r0);   // the first row's query
-  const uint32_t lse_off = (uint32_t)(row_at(it.r0 + lane) - head0) * 4;
+  auto head_of = [&](int r, int j0) __attribute__((always_inline)) { return (int64_t)(it.row0 + j0) * a.nq + kvh * G + r - j0 * G; };
+  uint32_t q_off[MINE], lse_off;
+  auto places = [&](int r, int j0) __attribute__((always_inline)) {
 #pragma unroll
-  for (int x = 0; x < MINE; ++x) {
-    const int at = (p0 + x) * 64 + lane, row = at / UNITS;
-    q_off[x] = (uint32_t)((row_at(it.r0 + my_tile * kTile + row) - head0) * (HD * (int)sizeof(T))) + 16 * (at % UNITS ^ (row & SWIZZLE));
-  }
-  auto bring = [&](int n) __attribute__((always_inline)) {           // stage n of the item
-    const int b = n % RING, r = it.r0 + n * STAGE;
-    if (steady && r + 64 <= rows) {
-      const int64_t head = head0 + (int64_t)n * step * a.nq;
-      const T *base = static_cast<const T *>(a.q) + head * HD;
-#pragma unroll
-      for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], &rows_of[b][my_tile][(p0 + x) * 64]);
-      lds_dma4_at(a.lse + head, lse_off, &lse_of[b][0]);
-    } else {
-#pragma unroll
-      for (int x = 0; x < MINE; ++x) {
-        const int at = (p0 + x) * 64 + lane, row = at / UNITS;
-        lds_dma16(reinterpret_cast<const char *>(static_cast<const T *>(a.q) + row_at(r + my_tile * kTile + row) * HD) + 16 * (at % UNITS ^ (row & SWIZZLE)),
-                  &rows_of[b][my_tile][(p0 + x) * 64]);
-      }
-      const int64_t first = row_at(r);
-      lds_dma4_at(a.lse + first, (uint32_t)(row_at(r + lane) - first) * 4, &lse_of[b][0]);
+    for (int x = 0; x < MINE; ++x) {
+      const int at = (p0 + x) * 64 + lane, row = at / UNITS;
+      q_off[x] = behind(r, j0, r + my_tile * kTile + row) * (uint32_t)(HD * sizeof(T)) + 16 * (at % UNITS ^ (row & SWIZZLE));
     }
+    lse_off = behind(r, j0, r + lane) * 4;
+  };
+  const int first_j = by_g.of(it.r0);
+  const int64_t head0 = head_of(it.r0, first_j);
+  places(it.r0, first_j);
+  auto bring = [&](int n) __attribute__((always_inline)) {           // stage n of the item, each in turn
+    const int b = n % RING, r = it.r0 + n * STAGE;
+    int64_t head = head0 + (int64_t)n * step * a.nq;
+    if (n > 0 && !(steady && r + 64 <= rows)) {
+      const int j0 = by_g.of(min(r, rows - 1));
+      head = head_of(r, j0);
+      places(r, j0);
+    }
+    const T *base = static_cast<const T *>(a.q) + head * HD;
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], &rows_of[b][my_tile][(p0 + x) * 64]);
+    lds_dma4_at(a.lse + head, lse_off, &lse_of[b][0]);
   };
   const bool by_request = a.count && it.req < 0;
   const int stages = (r_end - it.r0 + STAGE - 1) / STAGE;
@@ -138,9 +138,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
     for (int i = 0; i < 16; ++i) zero[i] = 0.f;
     asm volatile("" : "+v"(zero));
     for (int n = 0; n < stages; ++n) {
-      const int r0 = it.r0 + n * STAGE, b = n % RING, behind = min(RING - 2, stages - 1 - n);
+      const int r0 = it.r0 + n * STAGE, b = n % RING, after = min(RING - 2, stages - 1 - n);
       // this wave's loads of the stage have landed, and every wave's
-      if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+      if (after == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (n + RING - 1 < stages) bring(n + RING - 1);
 #pragma unroll
