@@ -13,9 +13,9 @@
 // on this card): a turn of four waves over 32 tokens is 512 cycles of products and takes 915, as the maxima, exponentials and
 // roundings of 16 x 64 scores a wave take some 400 that the other workgroup's products hide in part only.  Scores of the next
 // tile beside a tile's exponentials: 146 -> 137 us.  Two row tiles a wave (half the LDS reads, one workgroup a CU): 167 us.
-// 128 samples of a prompt of 16384 tokens: 62 us, of which a third is what starts and ends an item (5 us: the item, its
-// queries and block ids, the first pages, each waiting for the one before) and 11 the join of 36 MB of partial results.  4
-// requests on 1024 tokens: 14 us, latency.
+// 128 samples of a prompt of 16384 tokens: 60 us, of which a third is what starts and ends an item (5 us: the item, its
+// queries and block ids, the first pages, each waiting for the one before) and 7 the join of 28 MB of partial results.  4
+// requests on 1024 tokens: 13 us, latency.
 #include <algorithm>
 #include <climits>
 
