@@ -350,8 +350,8 @@ wisp_status wisp_verify_kv8(const wisp_model *model, const wisp_kv8 *kv, const w
  * workspace's scratch, so calls on one plan must not overlap.  Pools, q and out are 16-byte aligned; outputs must not
  * overlap inputs unless stated.  Block ids outside [0, n_blocks) are recorded in the workspace for wisp_check; what
  * is read of such a page is undefined.
- * WISP_E_UNSUPPORTED (and a workspace size of 0): more than WISP_ROWS_MAX rows, more than 64 query heads per kv head, or
- * more than 2^22 work items (x kv heads: one per 128 rows x query heads of a kv head and part of the tokens;
+ * WISP_E_UNSUPPORTED (and a workspace size of 0): more than WISP_ROWS_MAX rows, more than 64 query heads per kv head, more
+ * than 65535 kv heads, n_q_heads x head_dim above 2^22, or more than 2^22 work items (x kv heads: one per 128 rows x query heads of a kv head and part of the tokens;
  * one per 128 tokens and part of the rows).
  */
 typedef struct { uint64_t opaque[32]; } wisp_shared_batch;
@@ -405,6 +405,7 @@ wisp_status wisp_attention_mass(const wisp_shared_batch *batch, const wisp_kv *k
  *           same index, or one that no request of the call has; NULL: desc's table (in place)
  *   mass    DEVICE fp32 [n_layers][n_blocks][n_kv_heads][16]
  *   kept    DEVICE int32 [n_layers][n_kv_heads][sum of min(keep, ctx_len)]: the old positions of the tokens kept
+ * After a call in place wisp_kvm_commit of min(keep, ctx_len) returns the pages behind.
  * A token that keeps its position and page is not written: pages of the first `sink` tokens may be shared.  Pages past the
  * kept tokens, and the last one's slots past them, are left as they were.  The workspace (DEVICE, 256-byte
  * aligned, wisp_kv_evict_workspace_size bytes; its first 256 bytes the fault record of wisp_check) may be used again by

@@ -323,6 +323,8 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   p.B = d->B;
   const int G = p.nq / p.nkv;
   if (G > 64) return fail(WISP_E_UNSUPPORTED, "GQA group > 64");
+  if (p.nkv > 65535 || (int64_t)p.nq * p.hd > 1 << 22)   // a grid's second index; 64 rows' places in 32 bits
+    return fail(WISP_E_UNSUPPORTED, "more than 65535 kv heads, or n_q_heads x head_dim above 2^22");
   std::vector<Segment> segs;
   std::vector<RowAt> joins;
   std::vector<int32_t> pre_seg, row;

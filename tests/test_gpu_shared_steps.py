@@ -7,7 +7,8 @@ import torch
 import paper_2601_11652_amd as W
 from gpu_harness import log, to_dev
 from oracle import shared
-from shared_harness import HALF, U, Case, bits, from_pages, to_pages
+from shared_harness import HALF, U, Case, attention_bounds, bits, from_pages, to_pages
+from test_gpu_evict import Cache
 from test_gpu_shared import check_attention, check_mass
 
 pytestmark = pytest.mark.gpu
@@ -189,3 +190,38 @@ def test_an_eviction_on_a_stream_of_its_own():
         got.append((kv.k.view(torch.int16), kv.v.view(torch.int16), mass, kept))
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_pages_behind_the_kept_tokens_return_to_the_manager():
+    """A session's eviction in place and wisp_kvm_commit of what it keeps: the next round's table starts with the same
+    pages, and attention over it sees the kept tokens."""
+    ctx, keep, stride = [500, 123], [100, 64], 40
+    mgr = W.KVManager(64)
+    table, _ = mgr.reserve([7, 9], ctx, stride)
+    c = Cache(ctx, 2, 64, False, 80, spare=22)
+    assert c.nb == 64
+    for name in ("k", "v", "mass"):
+        old = getattr(c, name)
+        new = np.full_like(old, np.nan)
+        for i, n in enumerate((32, 8)):
+            new[:, table[i, :n]] = old[:, c.pt[i, :n]]
+        setattr(c, name, new)
+    c.pt, c.desc = table, W.BatchDesc(np.array(ctx, np.int32), np.zeros(2, np.int32), to_dev(table))
+    c.to_dev()
+    c.check(c.run(keep, [4, 4], [30, 30]), keep, [4, 4], [30, 30])
+    mgr.commit([7, 9], keep)
+    assert mgr.stats()["free_pages"] == 64 - 7 - 4
+    np.testing.assert_array_equal(mgr.lookup([7, 9]), keep)
+    again, _ = mgr.reserve([7, 9], [k + 4 for k in keep], stride)
+    np.testing.assert_array_equal(again[0, :7], table[0, :7])
+    np.testing.assert_array_equal(again[1, :4], table[1, :4])
+    last = np.array(keep, np.int32) - 1                      # the last kept token stands for a new one
+    desc = W.BatchDesc(last, np.zeros(2, np.int32), to_dev(again))
+    q = c.rng.normal(0, 1, (2, 2, 64)).astype(np.float32)
+    out, lse = torch.empty(2, 2, 64, device="cuda"), torch.empty(2, 2, device="cuda")
+    plan = W.wisp_shared_plan(c.model, desc, None, None, W.workspace(W.wisp_shared_workspace_size(c.model, desc)))
+    W.wisp_attention_shared(plan, c.kv, to_dev(q), out, lse)
+    W.wisp_check(plan.ws)
+    ref, rl, mag, big = shared.attention(q.astype(np.float64), c.k[0], c.v[0], again, last, [1, 1])
+    bo, bl = attention_bounds(ref, rl, mag, big, 64, 100, False)
+    assert np.all(np.abs(out.cpu().numpy() - ref) <= bo) and np.all(np.abs(lse.cpu().numpy() - rl) <= bl)

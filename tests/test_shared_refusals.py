@@ -73,6 +73,10 @@ def test_workspaces_and_tables():
 def test_sizes_beyond_the_kernels():
     assert W.wisp_shared_workspace_size(_model(65, 1, 64, False), _desc([5])) == 0            # more than 64 query heads per kv head
     assert W.wisp_shared_workspace_size(_model(64, 1, 64, False), _desc([5])) > 0
+    assert W.wisp_shared_workspace_size(_model(1 << 16, 1 << 16, 32, False), _desc([5])) == 0  # more than 65535 kv heads
+    assert W.wisp_shared_workspace_size(_model(65535, 65535, 32, False), _desc([5])) > 0
+    assert W.wisp_shared_workspace_size(_model(32768, 1024, 128), _desc([5])) > 0
+    assert W.wisp_shared_workspace_size(_model(32768 + 32, 1024 + 1, 128), _desc([5])) == 0    # more than 2^22 values of q in a row
     rows = [32768] * 8
     assert W.wisp_shared_workspace_size(_model(), _desc([0] * 8, prefill=rows)) == 0           # more than WISP_ROWS_MAX rows
     # 2^30 - 1 tokens: more blocks of them than work items
