@@ -158,35 +158,37 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 // in its own pages.  What a turn's tokens are is looked up while the turn before runs, their positions two turns
 // ahead.
 //
-// A page holds V by dims, eight slots of one in a row: the half pages that have kept tokens are read whole, and
-// their slots put in their new order in LDS (read one by one, at 2 bytes a lane, the cache's ports were the
-// bound: 32 requests of 2-8k tokens back to half, two layers, 496 us).
+// A page holds V by dims, eight slots of one in a row: the half pages that have kept tokens are read whole into LDS, from
+// where each new slot takes its own (read one by one from memory, at 2 bytes a lane, the cache's ports were the bound: 32
+// requests of 2-8k tokens back to half, two layers, 496 us; put in order as they come, 435).
 //
 // Bound by HBM where there are many tokens: memory comes in lines of 128 bytes, which hold 8 slots of K or V, and
-// almost each has a token that stays.  That call reads 1306 MB (all of its old pages) and writes 617 in 409 us, 4.70
-// TB/s; a copy reaches 4.85.  kv heads are neighbours in the grid, one to an XCD: as its second index, 426 us.
-// A few requests are bound by latency: 2000 of 8000 tokens, one layer, 20 us.
+// almost each has a token that stays.  That call reads 1306 MB (all of its old pages) and writes 617 in 404 us, 4.76
+// TB/s; a copy reaches 4.85.  kv heads are neighbours in the grid, one to an XCD: as its second index, 4% more.
+// A few requests are bound by latency: 2000 of 8000 tokens, one layer, 18 us.
 struct MoveArgs {
   EvictArgs e;
   double freq[128];                    // turns of a position's angle, of each dim below HD / 2
 };
 // Where a token lies: page of its kv head x 16 + slot; kStill: there it stays; kNone: there is none
 constexpr uint32_t kStill = 1u << 31, kNone = ~0u;
+constexpr int kHalves = 32;            // half pages of bf16 in a wave's LDS, 256 bytes each
 
 template <typename T, int HD>
 __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
   constexpr int OCT = HD / 16, VEC = 8 * (int)sizeof(T) / 16;       // 16-byte pieces of eight elements
-  constexpr int PAGE = kPage * HD;
+  constexpr int PAGE = kPage * HD, IN = kHalves / VEC;              // half pages that LDS holds at a time
   const EvictArgs &a = m.e;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tid = threadIdx.x;
   const int tokens = 64 * a.runs;                       // of a turn
   uint32_t *codes = reinterpret_cast<uint32_t *>(smem);              // [2][tokens]
   int *places = reinterpret_cast<int *>(smem) + 2 * tokens;          // [2][tokens]
-  // [2][runs][64]: the half pages of a run's tokens: page x 2 + half; the first token's place, its slots' bits << 8
-  uint2 *halves = reinterpret_cast<uint2 *>(places + 2 * tokens);
-  int *news = reinterpret_cast<int *>(halves + 2 * tokens), *n_halves = news + 2 * tokens / 16;   // [2][tokens / 16]; [2][runs]
-  T *tile = reinterpret_cast<T *>(smem + ((2 * tokens * 16 + 10 * a.runs * 4 + 15) & ~15)) + wave * 1024;   // this wave's V, as in the new pages
+  uint32_t *halves = reinterpret_cast<uint32_t *>(places + 2 * tokens);   // [2][runs][64]: the half pages of a run's tokens: page x 2 + half
+  uint16_t *sources = reinterpret_cast<uint16_t *>(halves + 2 * tokens);   // [2][tokens]: a token's half page, of its run's, x 8 + slot there
+  int *news = reinterpret_cast<int *>(sources + 2 * tokens), *n_halves = news + 2 * tokens / 16;   // [2][tokens / 16]; [2][runs]
+  // this wave's half pages of V, 16 dims of 8 slots each
+  uint4 *raw = reinterpret_cast<uint4 *>(smem + ((2 * tokens * 14 + 10 * a.runs * 4 + 15) & ~15)) + wave * kHalves * 16;
   const int rest = blockIdx.x / a.nkv;
   const EvictReq r = a.reqs[rest / OCT];
   const int oct = rest % OCT, t0 = wave * 64, kvh = blockIdx.x - rest * a.nkv, layer = blockIdx.z;
@@ -219,11 +221,9 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
     const int before = __shfl_up(pos, 1);
     const bool first = pos >= 0 && (lane == 0 || before >> 3 != pos >> 3);
     const unsigned long long all = __builtin_amdgcn_ballot_w64(first);
-    uint2 *half = halves + (at & ~63) + __popcll(all & ((2ull << lane) - 1)) - 1;
-    if (first) *half = make_uint2((uint32_t)(b * a.nkv + kvh) << 1 | (pos >> 3 & 1), lane);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (pos >= 0) atomicOr(&half->y, 256u << (pos & 7));
+    const int in_run = __popcll(all & ((2ull << lane) - 1)) - 1;
+    if (first) halves[(at & ~63) + in_run] = (uint32_t)(b * a.nkv + kvh) << 1 | (pos >> 3 & 1);
+    sources[at] = pos < 0 ? 0 : in_run << 3 | (pos & 7);
     if (lane == 0) n_halves[at >> 6] = __popcll(all);
     if (tid % 16 == 0) news[((x & 1) * tokens + tid) / 16] = new_page >= 0 && new_page < a.n_blocks ? new_page * a.nkv + kvh : -1;
   };
@@ -244,6 +244,14 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
       __builtin_memcpy(cv[y], __builtin_assume_aligned(&codes[from], 32), 32);
       vd[y] = news[from / 16];
     }
+    T moved[2][8] = {};                                 // V in its new order
+    // the lookups of the next turn
+    int after = -1;
+    if (x + 1 < turns) {
+      blk = pos >= 0 ? pt[pos >> 4] : 0;
+      new_page = pos >= 0 ? to[((x + 1) * tokens + tid) >> 4] : -1;
+      after = position(x + 2);
+    }
     // of no token: the pool's first one, not used
     uint4 lo[VEC], hi[VEC];
     {
@@ -256,37 +264,36 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
       }
     }
     {
-      const uint2 *half = halves + at;
+      const uint32_t *half = halves + at;
       const int n = __builtin_amdgcn_readfirstlane(n_halves[at >> 6]);
-      for (int h0 = 0; h0 < n; h0 += 16) {
-        uint2 g[4];
-        uint4 w[4][VEC];
+      for (int h0 = 0; h0 < n; h0 += IN) {
+        uint4 w[IN / 4][VEC];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int h = h0 + 4 * i + lane / 16;
-          g[i] = h < n ? half[h] : make_uint2(0, 0);
-          const T *from = vp + (int64_t)(g[i].x >> 1) * PAGE + (g[i].x & 1) * 128;
+        for (int i = 0; i < IN / 4; ++i) {
+          const uint32_t c = half[min(h0 + 4 * i + lane / 16, n - 1)];
+          const T *from = vp + (int64_t)(c >> 1) * PAGE + (c & 1) * 128;
 #pragma unroll
           for (int v = 0; v < VEC; ++v) w[i][v] = ld16(reinterpret_cast<const char *>(from) + 16 * v);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          T val[8];
-          __builtin_memcpy(val, w[i], sizeof(val));
-          int d = g[i].y & 63;
+        for (int i = 0; i < IN / 4; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (g[i].y >> (8 + e) & 1) {
-              tile[(d >> 3) * 128 + lane % 16 * 8 + (d & 7)] = val[e];
-              ++d;
-            }
-        }
+          for (int v = 0; v < VEC; ++v) raw[((4 * i + lane / 16) * 16 + lane % 16) * VEC + v] = w[i][v];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int from = (int)sources[at + 32 * y + 16 * (lane / 32) + 8 * v_half + e] - 8 * h0;
+            const T got = reinterpret_cast<const T *>(raw)[(min(max(from >> 3, 0), IN - 1) * 16 + lane % 16) * 8 + (from & 7)];
+            moved[y][e] = (uint32_t)from < 8 * IN ? got : moved[y][e];
+          }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
       }
     }
     if (x + 1 < turns) {
-      blk = pos >= 0 ? pt[pos >> 4] : 0;
-      new_page = pos >= 0 ? to[((x + 1) * tokens + tid) >> 4] : -1;
-      const int after = position(x + 2);
       list(x + 1);
       pos = after;
     }
@@ -340,7 +347,6 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
     for (int y = 0; y < 2; ++y) {
       if (vd[y] < 0) continue;
       T *put = vp + (int64_t)vd[y] * PAGE + 128 * v_half;
-      const T *val = tile + (lane + 64 * y) * 8;
       uint32_t none = 0, still = kStill;                // of some; of all (a slot of no token does not move)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -350,11 +356,11 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
       if (still) continue;
       if (!none) {
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(put) + 16 * v) = ld16(reinterpret_cast<const char *>(val) + 16 * v);
+        for (int v = 0; v < VEC; ++v) __builtin_memcpy(reinterpret_cast<char *>(put) + 16 * v, reinterpret_cast<const char *>(moved[y]) + 16 * v, 16);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (cv[y][e] != kNone) put[e] = val[e];
+          if (cv[y][e] != kNone) put[e] = moved[y][e];
       }
     }
   }
@@ -475,8 +481,8 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     launch(e.most <= kSelectHeld * kSelectThreads ? evict_select_kernel<true> : evict_select_kernel<false>,
            dim3(n, a.nkv, model->n_layers), kSelectThreads, 0, s, a);
     // Waves, of 64 tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half,
-    // two layers (4096 workgroups), 435 us with 8 waves, 438 with 4, 462 with 16; one of 8000 back to a quarter (64
-    // workgroups) 48 with 8 and 40 with 16, a small fp32 model's 12 requests (384) 40 and 36.
+    // two layers (4096 workgroups), 428 us with 8 waves, some 1% and 6% more with 4 and 16; one of 8000 back to a quarter (64
+    // workgroups) a fifth more with 8 than the 38 with 16, a small fp32 model's 12 requests (384) a tenth.
     const int most_waves = (int64_t)n * a.nkv * model->n_layers * oct < 2 * device_cus() ? 16 : 8;
     int most_kept = 0;
     for (const EvictReq &r : e.reqs) most_kept = std::max(most_kept, r.keep);
@@ -484,7 +490,7 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     MoveArgs move{a, {}};
     for (int i = 0; i < model->head_dim / 2; ++i)
       move.freq[i] = std::pow((double)model->rope_base, -2.0 * i / model->head_dim) / (2 * 3.14159265358979323846);
-    const uint32_t shm = ((2 * 64 * a.runs * 16 + 10 * a.runs * 4 + 15) & ~15) + (uint32_t)a.runs * 1024 * (model->dtype == WISP_BF16 ? 2 : 4);
+    const uint32_t shm = ((2 * 64 * a.runs * 14 + 10 * a.runs * 4 + 15) & ~15) + (uint32_t)a.runs * kHalves * 256;
     auto go = [&](auto kernel) {
       launch(kernel, dim3((unsigned)n * oct * a.nkv, 1, model->n_layers), 64 * a.runs, shm, s, move);
     };
