@@ -225,3 +225,24 @@ def test_pages_behind_the_kept_tokens_return_to_the_manager():
     ref, rl, mag, big = shared.attention(q.astype(np.float64), c.k[0], c.v[0], again, last, [1, 1])
     bo, bl = attention_bounds(ref, rl, mag, big, 64, 100, False)
     assert np.all(np.abs(out.cpu().numpy() - ref) <= bo) and np.all(np.abs(lse.cpu().numpy() - rl) <= bl)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("n", [32, 33, 40])
+def test_evictions_of_many_requests(n, captured):
+    ctx = 20 + 7 * np.arange(n)
+    c = Cache(ctx, 2, 64, True, 81).to_dev()
+    keep, sink, recent = (ctx // 2).tolist(), [3] * n, (ctx // 8).tolist()
+    kept = torch.full((1, 2, int(np.sum(keep))), -9, dtype=torch.int32, device="cuda")
+    ws = W.workspace(W.wisp_kv_evict_workspace_size(c.model, c.desc))
+    call = lambda: W.wisp_kv_evict(c.model, c.kv, c.desc, keep, c.dm, kept, ws, sink, recent)
+    if captured:
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            call()
+        g.replay()
+    else:
+        call()
+    W.wisp_check(ws)
+    c.check(kept.cpu().numpy(), keep, sink, recent)
