@@ -163,16 +163,21 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
         // tokens that this lane's row sees: none where it does not count
         const int lim = f < r_end && (on >> lc & 1) ? it.ctx + by_g.of(f) + 1 : 0;
         const float l2 = lse * kLog2e;
-        if (__builtin_amdgcn_ballot_w64(lim < tp + kTile || fabsf(l2) > kFarScore)) {
-          // rows that do not see a token, or do not count; and scores so large that the roundings on both sides
-          // of the difference may make it positive
-          const int seen = lim - tp - 8 * hf;
+        const int seen = lim - tp - 8 * hf;
+        if (__builtin_amdgcn_ballot_w64(fabsf(l2) > kFarScore)) {
+          // scores so large that the roundings on both sides of the difference may make it positive
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            float e = __builtin_fmaf(s[i], c_log2, -l2);
-            if (fabsf(l2) > kFarScore) e = e > 0.f ? 0.f : e;
-            e = __builtin_amdgcn_exp2f(e);
-            acc[i] += reg_token(0, i) < seen ? e : 0.f;
+            const float e = __builtin_fmaf(s[i], c_log2, -l2);
+            const float p = __builtin_amdgcn_exp2f(fabsf(l2) > kFarScore && e > 0.f ? 0.f : e);
+            acc[i] += reg_token(0, i) < seen ? p : 0.f;
+          }
+        } else if (__builtin_amdgcn_ballot_w64(lim < tp + kTile)) {
+          // rows that do not see a token, or do not count
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c_log2, -l2));
+            acc[i] += reg_token(0, i) < seen ? p : 0.f;
           }
         } else {
 #pragma unroll

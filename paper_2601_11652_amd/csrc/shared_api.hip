@@ -99,8 +99,8 @@ struct Piece {                                      // turns from .. to - 1 of a
 };
 int64_t cost_of(const std::vector<Bundle> &bundles, const Piece &x) { return kStartCost + (x.to - x.from) * bundles[x.bundle].turn; }
 
-// Bundles longer than `share` (a start and the least of any, or more) are laid one behind another over shares of that length and cut at their borders; the
-// others stay whole.
+// Bundles longer than `share` (a start and the least of any, or more) are laid one behind another over shares of that
+// length and cut at their borders; the others stay whole.
 std::vector<Piece> pieces_of(const std::vector<Bundle> &bundles, int64_t share) {
   std::vector<Piece> pieces;
   int64_t room = share;
