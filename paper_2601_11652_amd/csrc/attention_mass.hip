@@ -5,11 +5,12 @@
 // attention does without.  A wave keeps the keys of 32 tokens in registers, as an operand, and adds up over the rows, which
 // stream through LDS for the four waves; sums of fp32 in registers, a row's place in them fixed, so results do not vary.
 //
-// For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: of a
-// row tile's 900 cycles a SIMD 256 are products and 424 vector instructions, 16 exponentials of 64 lanes among them.  Three
-// workgroups a CU hide most of the waits: 103 us, 680 TFLOP/s, where two took 105 (and for 32 sessions on a document 25 and
-// 32).  Two token tiles a wave, half the LDS reads, 118 us; the next tile's products beside a tile's exponentials, no
-// change.  A few rows over many tokens are bound by latency: 4000 tokens 8 us.
+// For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: 0.38 and
+// 0.66 of the cycles, 16 exponentials of 64 lanes to a row tile's 8 products.  Three workgroups a CU hide most of the waits:
+// 100 us, 695 TFLOP/s.  Two token tiles a wave, half the LDS reads, were 118 us where one took 106; the next tile's products
+// beside a tile's exponentials, no change.  32 sessions on a document of 4096 tokens: 22 us, 2600 short items whose
+// instructions before and after their one row tile are the most of it.  A few rows over many tokens are bound by latency:
+// 4000 tokens 8 us.
 #include <algorithm>
 #include <climits>
 

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 // requests of 2-8k tokens back to half, two layers, 496 us; put in order as they come, 435).
 //
 // Bound by HBM where there are many tokens: memory comes in lines of 128 bytes, which hold 8 slots of K or V, and
-// almost each has a token that stays.  That call reads 1306 MB (all of its old pages) and writes 617 in 404 us, 4.76
+// almost each has a token that stays.  That call reads 1306 MB (all of its old pages) and writes 617 in 403 us, 4.77
 // TB/s; a copy reaches 4.85.  kv heads are neighbours in the grid, one to an XCD: as its second index, 4% more.
 // A few requests are bound by latency: 2000 of 8000 tokens, one layer, 18 us.
 struct MoveArgs {
@@ -498,8 +498,8 @@ wisp_status wisp_kv_evict(const wisp_model *model, const wisp_kv *kv, const wisp
     launch(e.most <= kSelectHeld * kSelectThreads ? evict_select_kernel<true> : evict_select_kernel<false>,
            dim3(n, a.nkv, model->n_layers), kSelectThreads, 0, s, a);
     // Waves, of 64 tokens of a turn: a request's turns wait for one another.  32 requests of 2-8k tokens back to half,
-    // two layers (4096 workgroups), 428 us with 8 waves, some 1% and 6% more with 4 and 16; one of 8000 back to a quarter (64
-    // workgroups) a fifth more with 8 than the 38 with 16, a small fp32 model's 12 requests (384) a tenth.
+    // two layers (4096 workgroups), 425 us with 8 waves, some 1% and 6% more with 4 and 16; one of 8000 back to a quarter (64
+    // workgroups) a fifth more with 8 than the 33 with 16, a small fp32 model's 12 requests (384) a tenth.
     const int most_waves = (int64_t)n * a.nkv * model->n_layers * oct < 2 * device_cus() ? 16 : 8;
     int most_kept = 0;
     for (const EvictReq &r : e.reqs) most_kept = std::max(most_kept, r.keep);
