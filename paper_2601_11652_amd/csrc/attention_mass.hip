@@ -12,7 +12,6 @@
 // instructions before and after their one row tile are the most of it.  A few rows over many tokens are bound by latency:
 // 4000 tokens 8 us.
 #include <algorithm>
-#include <climits>
 
 #include "../../include/wisp.h"
 #include "kernels.h"

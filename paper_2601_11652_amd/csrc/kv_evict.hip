@@ -4,7 +4,6 @@
 #include <climits>
 #include <cmath>
 #include <cstring>
-#include <numeric>
 
 #include "api.h"
 #include "host_guard.h"

@@ -41,7 +41,7 @@ struct MassJoin {                      // a token block whose sums have several 
 
 constexpr int kBundle = 4;             // row tiles of a workgroup
 constexpr int kMassBlock = 4 * kTile;  // tokens of a workgroup: a tile a wave
-constexpr int kMassTiles = 512;       // row tiles of an item at most
+constexpr int kMassTiles = 512;        // row tiles of an item at most
 constexpr int kSharedMaxItems = 1 << 22;
 
 struct SharedPlan {                    // a wisp_shared_batch
