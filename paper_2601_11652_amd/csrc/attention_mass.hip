@@ -7,10 +7,9 @@
 //
 // For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: 0.38 and
 // 0.66 of the cycles, 16 exponentials of 64 lanes to a row tile's 8 products.  Three workgroups a CU hide most of the waits:
-// 100 us, 695 TFLOP/s.  Two token tiles a wave, half the LDS reads, were 118 us where one took 106; the next tile's products
-// beside a tile's exponentials, no change.  32 sessions on a document of 4096 tokens: 22 us, 2600 short items whose
-// instructions before and after their one row tile are the most of it.  A few rows over many tokens are bound by latency:
-// 4000 tokens 8 us.
+// 96 us, 730 TFLOP/s.  Two token tiles a wave, half the LDS reads, were 118 us where one took 106; the next tile's products
+// beside a tile's exponentials, no change.  32 sessions on a document of 4096 tokens: 21 us, blocks of one row tile whose
+// instructions before and after it are the most of it.  A few rows over many tokens are bound by latency: 4000 tokens 8 us.
 #include <algorithm>
 
 #include "../../include/wisp.h"
@@ -62,23 +61,20 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
   const int kvh = blockIdx.x % a.nkv;
   const MassItem it = a.items[blockIdx.x / a.nkv];
   const int G = a.nq / a.nkv, rows = it.nrow * G;
-  const int tp = it.t0 + wave * kTile, tq = min(tp, (it.t1 - 1) & ~15);   // this wave's tokens; past the end the last page
   // rows past those that count give nothing
   int counted = it.nrow;
   if (a.count && it.req >= 0) counted = min(max(a.count[it.req], 0), it.nrow);
   const int r_end = min(it.r1, counted * G);
   Op8<T> kf[KB];
-  {
+  auto load_k = [&](int t0) __attribute__((always_inline)) {         // this wave's tokens of a block; past the end the last page
     const int32_t *ids = a.page_table + (int64_t)it.table * a.pt_stride;
-    const int b = ids[min((tq >> 4) + ((lane >> 4) & 1), (it.t1 - 1) >> 4)];
+    const int b = ids[min((t0 >> 4) + 2 * wave + ((lane >> 4) & 1), (it.t1 - 1) >> 4)];
     const T *kt = static_cast<const T *>(a.k) + ((int64_t)min(max(b, 0), a.n_blocks - 1) * a.nkv + kvh) * (kPage * HD);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) kf[kb] = load_op(kt + k_op_lane(lane) + k_op_step(kb));
-  }
+  };
+  load_k(it.t0);
   const float c_log2 = a.scale * kLog2e;
-  floatx16 acc;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
   // Row tiles go straight into LDS, RING - 1 stages ahead, whole rows at a time: unit u of row r lies at u ^ (r % 16 or 8), so
   // that the rows' operands are read without bank conflicts (in operand order, each load took 32 bytes of 32 rows: 115 us
   // for a prompt of 4096 rows).  Their lse goes with them.
@@ -117,9 +113,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
       places(r, j0);
     }
     const T *base = static_cast<const T *>(a.q) + head * HD;
+    const uint32_t to = lds_address(rows_of) + ((b * TILES + my_tile) * kTile * UNITS + p0 * 64) * 16;
 #pragma unroll
-    for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], &rows_of[b][my_tile][(p0 + x) * 64]);
-    lds_dma4_at(a.lse + head, lse_off, &lse_of[b][0]);
+    for (int x = 0; x < MINE; ++x) lds_dma16_at(base, q_off[x], to + x * 1024);
+    lds_dma4_at(a.lse + head, lse_off, lds_address(lse_of) + b * 256);
   };
   const bool by_request = a.count && it.req < 0;
   const int stages = (r_end - it.r0 + STAGE - 1) / STAGE;
@@ -132,15 +129,23 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
         if (lane < 2 && (f - lane - it.r0) / kTile + lane < kMassTiles) counts[(f - lane - it.r0) / kTile + lane] = lane ? on >> 32 : on;
       }
     }
-    loads_done();                        // K
-    floatx16 zero;                       // in registers: made anew for each tile, it would take 16 instructions
+  }
+  floatx16 zero;                       // in registers: made anew for each tile, it would take 16 instructions
 #pragma unroll
-    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
-    asm volatile("" : "+v"(zero));
+  for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+  asm volatile("" : "+v"(zero));
+  // An item of one stage may have several blocks of tokens; the next one's keys are on their way while the sums go out.
+  for (int t0 = it.t0;; t0 += kMassBlock) {
+    const int tp = t0 + wave * kTile;
+    floatx16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    loads_done();                        // K
     for (int n = 0; n < stages; ++n) {
       const int r0 = it.r0 + n * STAGE, b = n % RING, after = min(RING - 2, stages - 1 - n);
       // this wave's loads of the stage have landed, and every wave's
-      if (after == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+      if (t0 > it.t0) ;                  // the only one: it is there
+      else if (after == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (n + RING - 1 < stages) bring(n + RING - 1);
 #pragma unroll
@@ -185,26 +190,27 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
         }
       }
     }
-  }
-  // over the rows: the lanes of a half
-  float sum = 0.f;
+    const bool more = t0 + kMassBlock < it.t1;
+    if (more) load_k(t0 + kMassBlock);
+    // over the rows: the lanes of a half
+    float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float v = acc[i];
-    v += dpp<kXor1>(v);
-    v += dpp<kXor2>(v);
-    v += dpp<kHalfMirror>(v);
-    v += dpp<kMirror>(v);
-    v = xor16_sum(v);
-    sum = lc == i ? v : sum;
+    for (int i = 0; i < 16; ++i) {
+      float v = acc[i];
+      v += dpp<kXor1>(v);
+      v += dpp<kXor2>(v);
+      v += dpp<kHalfMirror>(v);
+      v += dpp<kMirror>(v);
+      v = xor16_sum(v);
+      sum = lc == i ? v : sum;
+    }
+    const int t = tp + reg_token(lane, lc & 15);
+    if (lc < 16 && t < it.t1) {
+      if (it.part >= 0) a.part[(int64_t)it.part + (int64_t)kvh * it.step + t - it.t0] = sum;
+      else put_mass(a.page_table, a.pt_stride, a.n_blocks, a.nkv, kvh, it.table, t, t < it.ctx, a.decay, a.prev, sum, a.mass, a.err);
+    }
+    if (!more) break;
   }
-  const int t = tp + reg_token(lane, lc & 15);
-  if (lc >= 16 || t >= it.t1) return;
-  if (it.part >= 0) {
-    a.part[(int64_t)it.part + (int64_t)kvh * it.step + t - it.t0] = sum;
-    return;
-  }
-  put_mass(a.page_table, a.pt_stride, a.n_blocks, a.nkv, kvh, it.table, t, t < it.ctx, a.decay, a.prev, sum, a.mass, a.err);
 }
 
 __global__ __launch_bounds__(kMassBlock) void mass_join_kernel(const MassJoin *joins, const float *part, const int32_t *page_table,
@@ -221,6 +227,7 @@ __global__ __launch_bounds__(kMassBlock) void mass_join_kernel(const MassJoin *j
 
 }  // namespace
 
+int mass_stage_tiles(int dtype, int hd) { return dtype == WISP_BF16 || hd <= 64 ? 2 : 1; }
 int mass_wgs_per_cu(int dtype, int hd) { return dtype == WISP_BF16 || hd <= 64 ? 3 : 1; }
 
 void shared_mass(const SharedPlan &p, const SharedCache &c, const void *q, const float *lse, const int32_t *count, float decay,

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     auto bring = [&](int t) __attribute__((always_inline)) {
       // a wave: one page of K or of V
       const char *from = reinterpret_cast<const char *>((wave & 1 ? vp : kp) + place(wave & 2 ? b1 : b0));
-      char *to = smem + (t % STAGES) * G_::STAGE_BYTES + (2 * (wave & 1) + (wave >> 1)) * G_::PAGE_BYTES;
+      const uint32_t to = lds_address(smem) + (t % STAGES) * G_::STAGE_BYTES + (2 * (wave & 1) + (wave >> 1)) * G_::PAGE_BYTES;
 #pragma unroll
       for (int u = 0; u < KIB / PIECE; ++u)
 #pragma unroll

@@ -28,7 +28,8 @@ struct SharedRow {                     // of a row of the batch: where head 0 of
   int32_t own_next, pre_next;          // the bundles behind them, in which the last heads of a row may lie
 };
 
-// Column sums of a segment's probabilities: tokens t0 .. t1 - 1 (at most a block of them), flat rows r0 .. r1 - 1
+// Column sums of a segment's probabilities: tokens t0 .. t1 - 1 (a block of them; of one stage of rows some
+// blocks), flat rows r0 .. r1 - 1
 struct MassItem {
   int32_t table, t0, t1, ctx;
   int32_t row0, nrow, req, r0;         // req: the request whose rows these are, -1: a group's
@@ -65,5 +66,6 @@ void shared_mass(const SharedPlan &p, const SharedCache &c, const void *q, const
 // workgroups that a CU holds
 int shared_wgs_per_cu(int dtype, int hd);
 int mass_wgs_per_cu(int dtype, int hd);
+int mass_stage_tiles(int dtype, int hd);   // row tiles that the weights' kernel has at a time
 
 }  // namespace wisp

@@ -95,15 +95,17 @@ __device__ __forceinline__ constexpr int v_op_block(int mb) { return mb * 512; }
 // token of register i, from the tile's first
 __device__ __forceinline__ int reg_token(int lane, int i) { return 16 * (i >> 3) + 8 * (lane >> 5) + (i & 7); }
 
-// lds_dma16 from base + offset, base wave-uniform: no address to make for each lane
-__device__ __forceinline__ void lds_dma16_at(const void *base, uint32_t offset, const void *dst) {
-  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)dst);
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+// lds_dma16 from base + offset, base wave-uniform (no address to make for each lane), to an LDS address
+__device__ __forceinline__ void lds_dma16_at(const void *base, uint32_t offset, uint32_t to) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane(to);
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(m0) : "memory", "m0");
 }
-
 // four bytes a lane
-__device__ __forceinline__ void lds_dma4_at(const void *base, uint32_t offset, const void *dst) {
-  const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)dst);
+__device__ __forceinline__ void lds_dma4_at(const void *base, uint32_t offset, uint32_t to) {
+  const uint32_t m0 = __builtin_amdgcn_readfirstlane(to);
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(m0) : "memory", "m0");
 }
 

@@ -24,6 +24,8 @@ CUT = [
     ([(3200, [(17, 3), (33, 1)])], 7, 1, 32, False),
     ([(16, [(2, 700)]), (0, [(900, 130)])], 4, 2, 128, True),
     ([(2048, [(1, 1)] * 33)], 3, 3, 128, True),
+    ([(16, [(300 + 7 * i, 1 + i % 3) for i in range(48)])], 16, 8, 64, True),   # more blocks of few rows than run at once
+    ([(0, [(250 + 11 * i, 2)]) for i in range(40)], 4, 4, 96, False),
 ]
 
 
