@@ -387,6 +387,8 @@ wisp_status wisp_attention_shared(const wisp_shared_batch *batch, const wisp_kv 
  *           NULL (nothing before) or mass itself.  Slots of the batch's tokens are written, others left.
  * A page that is not common to a group belongs to one request; a group's common tokens get the sum over all its rows.
  * Sums are fp32, in a fixed order.  A row whose lse is NaN makes the tokens that it sees NaN; one of +infinity adds 0.
+ * Besides the score's own error, the roundings of lse and of its product put a weight's exponent off by 2^-21 |lse| at most.  Where
+ * |lse| is above 45426 a weight is 1 at most, and 1 for a token that has all of its row, at any size of the score.
  */
 wisp_status wisp_attention_mass(const wisp_shared_batch *batch, const wisp_kv *kv, const void *q, const float *lse,
                                 const int32_t *count, float decay, const float *prev, float *mass, void *stream);

@@ -47,6 +47,16 @@ __device__ __forceinline__ void put_mass(const int32_t *page_table, int pt_strid
   mass[at] = old && prev ? __builtin_fmaf(decay, prev[at], got) : got;
 }
 
+// A weight's exponent in base 2 where the row's scores are large: the difference first, so that what is rounded before it is lse and
+// the score, each as the attention rounded it (the product by itself, not in one with the difference), and a token that had all of its row
+// has 0.  Roundings may make it positive: a weight is 1 at most.
+__device__ __forceinline__ float far_exponent(float score, float scale, float lse) {
+#pragma clang fp contract(off)
+  const float scaled = score * scale;
+  const float e = (scaled - lse) * kLog2e;
+  return e > 0.f ? 0.f : e;                            // NaN stays
+}
+
 template <typename T, int HD>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mass_kernel(MassArgs a) {
   constexpr int KB = HD / 16, UNITS = HD * (int)sizeof(T) / 16, PIECES = UNITS / 2;   // 16-byte units of a row; 1 KiB pieces of a row tile
@@ -170,11 +180,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 || HD <= 64) ? 3 : 1) void mas
         const float l2 = lse * kLog2e;
         const int seen = lim - tp - 8 * hf;
         if (__builtin_amdgcn_ballot_w64(fabsf(l2) > kFarScore)) {
-          // scores so large that the roundings on both sides of the difference may make it positive
+          // scores so large that the roundings of both products with log2(e) would be most of their difference
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float e = __builtin_fmaf(s[i], c_log2, -l2);
-            const float p = __builtin_amdgcn_exp2f(fabsf(l2) > kFarScore && e > 0.f ? 0.f : e);
+            const float p = __builtin_amdgcn_exp2f(fabsf(l2) > kFarScore ? far_exponent(s[i], a.scale, lse) : __builtin_fmaf(s[i], c_log2, -l2));
             acc[i] += reg_token(0, i) < seen ? p : 0.f;
           }
         } else if (__builtin_amdgcn_ballot_w64(lim < tp + kTile)) {
