@@ -182,7 +182,7 @@ struct MoveArgs {
   EvictArgs e;
   double freq[128];                    // turns of a position's angle, of each dim below HD / 2
 };
-// Where a token lies: page of its kv head x 16 + slot; kStill: there it stays; kNone: there is none
+// Where a token lies: page of its kv head x 16 + slot; kStill: there it stays; kNone (kStill among its bits): there is none
 constexpr uint32_t kStill = 1u << 31, kNone = ~0u;
 constexpr int kHalves = 32;            // half pages of bf16 in a wave's LDS, 256 bytes each
 
@@ -359,20 +359,20 @@ __global__ __launch_bounds__(1024) void evict_move_kernel(MoveArgs m) {
     for (int y = 0; y < 2; ++y) {
       if (vd[y] < 0) continue;
       T *put = vp + (int64_t)vd[y] * PAGE + 128 * v_half;
-      uint32_t none = 0, still = kStill;                // of some; of all (a slot of no token does not move)
+      uint32_t some = 0, all = kStill;                  // slots that are not written: of tokens that stay, and of none
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        none |= cv[y][e] == kNone;
-        still &= cv[y][e];
+        some |= cv[y][e];
+        all &= cv[y][e];
       }
-      if (still) continue;
-      if (!none) {
+      if (all) continue;
+      if (!(some & kStill)) {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) __builtin_memcpy(reinterpret_cast<char *>(put) + 16 * v, reinterpret_cast<const char *>(moved[y]) + 16 * v, 16);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (cv[y][e] != kNone) put[e] = moved[y][e];
+          if (!(cv[y][e] & kStill)) put[e] = moved[y][e];
       }
     }
   }
