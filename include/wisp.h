@@ -370,7 +370,7 @@ wisp_status wisp_shared_plan(const wisp_model *model, const wisp_batch_desc *des
  * Row j of request i sees keys 0 .. ctx_len[i] + j; tokens that a row does not see do not touch it, whatever they
  * hold, nor do slots past a request's last token.  Contexts of any length.  Scores may be as large as fp32 holds; a
  * row with a NaN, or with a score of +infinity, is NaN.  For WISP_BF16 each probability is rounded to bf16 (2^-8 of it at
- * most) before it multiplies V; the sum that divides, and lse, add them in fp32.
+ * most) before it multiplies V and in the sum that divides, as wisp_attention does; lse adds them as they were.
  */
 wisp_status wisp_attention_shared(const wisp_shared_batch *batch, const wisp_kv *kv, const void *q, void *out,
                                   float *lse, void *stream);

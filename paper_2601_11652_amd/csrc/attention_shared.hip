@@ -33,7 +33,8 @@ struct SharedArgs {
   const int32_t *page_table;
   const void *k, *v, *q;
   void *out;
-  float *lse, *part_o, *part_ml;
+  float *lse, *part_o;
+  float4 *part_ml;                     // maximum, sum, sum of the probabilities as they multiply V
   int *err;
   int pt_stride, n_blocks, nq, nkv;
   float scale;
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   using G_ = Geo<T, HD>;
   constexpr int KB = G_::KB, MB = G_::MB, PAGE = G_::PAGE, STAGES = G_::STAGES, LDJ = G_::LDJ;
   __shared__ __attribute__((aligned(1024))) char smem[G_::SMEM];
-  __shared__ float2 sh_ml[4][kTile];
+  __shared__ float4 sh_ml[4][kTile];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lc = lane & 31, hf = lane >> 5;
   const int kvh = blockIdx.x % a.nkv;                 // neighbouring workgroups, on other XCDs: other kv heads
@@ -78,7 +79,10 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
   const int lim = min(it.t1, it.ctx + jr + 1);        // tokens that this lane's row sees
   const int open = min(it.t1, it.ctx + __builtin_amdgcn_readfirstlane(by_g.of(fr0)) + 1);   // that every row of the tile sees
   const float c_log2 = a.scale * kLog2e, tau = 8.0f / c_log2;
-  float m_run = -INFINITY, l_run = 0.f;
+  // Sums of the probabilities, for lse, and (bf16) as they multiply V, rounded, by which the result is divided: it is then a mean of V's
+  // rows, and a token with nearly all of a row gives its own, where the other sum leaves the rounding of its probability, as
+  // much as that of the result once more.  1 to 2% of a call.
+  float m_run = -INFINITY, l_run = 0.f, d_run = 0.f;
   floatx16 o[MB];
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
@@ -101,6 +105,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       const float alpha = grow ? __builtin_amdgcn_exp2f((m_run - mx) * c_log2) : 1.0f;
       m_run = grow ? mx : m_run;
       l_run *= alpha;
+      d_run *= alpha;
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
       mc = m_run == -INFINITY ? 0.f : m_run * c_log2;
@@ -124,12 +129,14 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     float sum[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
     for (int i = 4; i < 16; ++i) sum[i & 3] += s[i];
-    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);   // this lane's tokens: the halves are added at the end
+    const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    l_run += all;                                     // this lane's tokens: the halves are added at the end
+    return all;
   };
   auto softmax = [&](floatx16 &s) __attribute__((always_inline)) {
     raise(row_max(s));
     exponentials(s, offset(s));
-    add_up(s);
+    return add_up(s);
   };
   // eight probabilities of a page as an operand
   auto probs = [&](const floatx16 &p, int g) __attribute__((always_inline)) {
@@ -239,6 +246,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
         exponentials(sc, off);
         add_up(sc);
         const Op8<T> p0 = probs(sc, 0), p1 = probs(sc, 1);
+        d_run = op_sum(p0, p1, d_run);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) ov[kb] = v_operand(t % STAGES, kb / MB, kb % MB);
         if constexpr (sizeof(T) == 2) {
@@ -270,12 +278,12 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
         for (int kb = 0; kb < KB; ++kb) op[kb] = k_operand(t % STAGES, kb);
         floatx16 sc = products(op);
         softmax(sc);
+        const Op8<T> pb[2] = {probs(sc, 0), probs(sc, 1)};
+        d_run = op_sum(pb[0], pb[1], d_run);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const Op8<T> pb = probs(sc, g);
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], v_operand(t % STAGES, g, mb), pb);
-        }
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], v_operand(t % STAGES, g, mb), pb[g]);
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what was brought past the end has landed before LDS is used again
@@ -334,7 +342,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = tp + reg_token(lane, i) < lim ? sc[i] : -INFINITY;
       }
-      softmax(sc);
+      const float all = softmax(sc);
       if constexpr (!G_::AHEAD) load_v();
       if (masked) {
         // Slots past the last token may hold anything.  And a token that is there, but not seen by every row, may be
@@ -352,12 +360,14 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
         if (__builtin_amdgcn_ballot_w64(special)) later = min(later, x);
       }
       if (later > x) {
+        const Op8<T> pb[2] = {probs(sc, 0), probs(sc, 1)};
+        d_run = op_sum(pb[0], pb[1], d_run);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const Op8<T> pb = probs(sc, g);
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], vf[g][mb], pb);
-        }
+          for (int mb = 0; mb < MB; ++mb) o[mb] = mma(o[mb], vf[g][mb], pb[g]);
+      } else {
+        d_run += all;                                  // they multiply V as they are
       }
       __builtin_amdgcn_sched_barrier(0);
       vb[0] = vp + place(b0);
@@ -402,12 +412,12 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     if (b < 0 || b >= a.n_blocks) flag_error(a.err, kErrBlock);
   }
   // A row tile of one wave goes out as it lies in the registers, partial results in that order: 16 bytes a lane
-  const float l = xor32_sum(l_run);
+  const float l = xor32_sum(l_run), d = sizeof(T) == 2 ? xor32_sum(d_run) : l;
   auto put_part = [&](int tile, int row_lane, int at, floatx4 v) __attribute__((always_inline)) {
     *reinterpret_cast<floatx4 *>(a.part_o + ((int64_t)it.part + (int64_t)kvh * it.step + tile) * (kTile * HD) + (at * 64 + row_lane) * 4) = v;
   };
-  auto put_ml = [&](int tile, int row, float m, float den) __attribute__((always_inline)) {
-    *reinterpret_cast<float2 *>(a.part_ml + (((int64_t)it.part + (int64_t)kvh * it.step + tile) * kTile + row) * 2) = make_float2(m, den);
+  auto put_ml = [&](int tile, int row, float m, float l, float d) __attribute__((always_inline)) {
+    a.part_ml[((int64_t)it.part + (int64_t)kvh * it.step + tile) * kTile + row] = make_float4(m, l, d, 0.f);
   };
   if (wide && it.part >= 0) {
     if (wave < it.tiles) {
@@ -415,14 +425,14 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int y = 0; y < 4; ++y) put_part(wave, lane, 4 * mb + y, floatx4{o[mb][4 * y], o[mb][4 * y + 1], o[mb][4 * y + 2], o[mb][4 * y + 3]});
-      if (hf == 0) put_ml(wave, lc, m_run, l);
+      if (hf == 0) put_ml(wave, lc, m_run, l, d);
     }
     return;
   }
   // through LDS: 8 dims of a row a thread, the waves of a row tile added in order
   __syncthreads();
   float(*jo)[kTile][LDJ] = reinterpret_cast<float(*)[kTile][LDJ]>(smem);
-  if (hf == 0) sh_ml[wave][lc] = make_float2(m_run, l);
+  if (hf == 0) sh_ml[wave][lc] = make_float4(m_run, l, d, 0.f);
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -435,24 +445,26 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
     const int c0 = u % CH * 8, r = u / CH % kTile, t = u / CH / kTile;
     const int f = (it.tile0 + t) * kTile + r;
     if (f >= rows) continue;
-    float m = -INFINITY, den = 0.f;
+    float m = -INFINITY, sum = 0.f, den = 0.f;
     for (int x = 0; x < parts; ++x) m = fmaxf(m, sh_ml[t + x * it.tiles][r].x);
     floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
     for (int x = 0; x < parts; ++x) {
-      const float2 ml = sh_ml[t + x * it.tiles][r];
+      const float4 ml = sh_ml[t + x * it.tiles][r];
       if (ml.x == -INFINITY) {
-        den += ml.y;                                  // 0, or NaN of a row's NaN scores
+        sum += ml.y;                                  // 0, or NaN of a row's NaN scores
+        den += ml.z;
         continue;
       }
       const float w = __builtin_amdgcn_exp2f((ml.x - m) * c_log2);
-      den += ml.y * w;
+      sum += ml.y * w;
+      den += ml.z * w;
       y += *reinterpret_cast<const floatx4 *>(&jo[t + x * it.tiles][r][c0]) * w;
       z += *reinterpret_cast<const floatx4 *>(&jo[t + x * it.tiles][r][c0 + 4]) * w;
     }
     if (it.part >= 0) {
       put_part(t, r, c0 / 8, y);
       put_part(t, r + 32, c0 / 8, z);
-      if (c0 == 0) put_ml(t, r, m, den);
+      if (c0 == 0) put_ml(t, r, m, sum, den);
       continue;
     }
     const int j = by_g.of(f);
@@ -467,7 +479,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
       *reinterpret_cast<floatx4 *>(to) = y;
       *reinterpret_cast<floatx4 *>(to + 4) = z;
     }
-    if (a.lse && c0 == 0) a.lse[row] = m * a.scale + logf(den);
+    if (a.lse && c0 == 0) a.lse[row] = m * a.scale + logf(sum);
   }
 }
 
@@ -476,7 +488,7 @@ __global__ __launch_bounds__(256, (Geo<T, HD>::WGS)) void shared_attn_kernel(Sha
 constexpr int kJoinParts = 8, kJoinThreads = 128;
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedRow *rows, const SharedBundle *bundles, const float *part_o,
-                                                                   const float *part_ml, T *out, float *lse, int n_rows, int nq, int nkv, int hd,
+                                                                   const float4 *part_ml, T *out, float *lse, int n_rows, int nq, int nkv, int hd,
                                                                    int together, int per_block, float scale) {
   // Neighbouring threads have the heads of a kv head and then those of the next of `together` rows, whose results are
   // neighbours: 256 bytes, two lines.  per_block kv heads a workgroup.
@@ -501,19 +513,19 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedR
   if (n < 2) return;                                  // written as it was computed
   const int64_t own = ((int64_t)b0.at + (int64_t)kvh * b0.tiles) * kTile + f0, own_step = (int64_t)nkv * b0.tiles * kTile;
   const int64_t pre = ((int64_t)b1.at + (int64_t)kvh * b1.tiles) * kTile + f1, pre_step = (int64_t)nkv * b1.tiles * kTile;
-  float m = -INFINITY, den = 0.f;
+  float m = -INFINITY, sum = 0.f, den = 0.f;
   floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
   for (int p0 = 0; p0 < n; p0 += kJoinParts) {
-    float2 ml[kJoinParts];
+    float4 ml[kJoinParts];
     floatx4 a[kJoinParts], b[kJoinParts];
 #pragma unroll
     for (int i = 0; i < kJoinParts; ++i) {
-      ml[i] = make_float2(-INFINITY, 0.f);
+      ml[i] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
       a[i] = b[i] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (p0 + i < n) {
         const int p = p0 + i;
         const int64_t s = p < b0.parts ? own + p * own_step : pre + (p - b0.parts) * pre_step;
-        ml[i] = *reinterpret_cast<const float2 *>(part_ml + s * 2);
+        ml[i] = part_ml[s];
         const float *o = part_o + (s >> 5) * kTile * hd + (c0 / 8 * 64 + (s & 31)) * 4;
         a[i] = *reinterpret_cast<const floatx4 *>(o);
         b[i] = *reinterpret_cast<const floatx4 *>(o + 32 * 4);
@@ -524,6 +536,7 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedR
     for (int i = 0; i < kJoinParts; ++i) top = fmaxf(top, ml[i].x);
     const float was = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c_log2);
     m = top;
+    sum *= was;
     den *= was;
     y *= was;
     z *= was;
@@ -531,7 +544,8 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedR
     for (int i = 0; i < kJoinParts; ++i) {
       // of a part that saw no token the sum is 0, or NaN where the row's scores were
       const float w = ml[i].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[i].x - m) * c_log2);
-      den += ml[i].y * w;
+      sum += ml[i].y * w;
+      den += ml[i].z * w;
       y += a[i] * w;
       z += b[i] * w;
     }
@@ -547,7 +561,7 @@ __global__ __launch_bounds__(kJoinThreads) void shared_join_kernel(const SharedR
     *reinterpret_cast<floatx4 *>(to) = y;
     *reinterpret_cast<floatx4 *>(to + 4) = z;
   }
-  if (lse && c0 == 0) lse[row] = m * scale + logf(den);
+  if (lse && c0 == 0) lse[row] = m * scale + logf(sum);
 }
 
 }  // namespace
@@ -564,7 +578,7 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
   a.out = out;
   a.lse = lse;
   a.part_o = reinterpret_cast<float *>(p.ws + p.w_po);
-  a.part_ml = reinterpret_cast<float *>(p.ws + p.w_pml);
+  a.part_ml = reinterpret_cast<float4 *>(p.ws + p.w_pml);
   a.err = err;
   a.pt_stride = p.pt_stride;
   a.n_blocks = c.n_blocks;
@@ -594,7 +608,7 @@ void shared_attention(const SharedPlan &p, const SharedCache &c, const void *q, 
   const int per_block = std::max(1, std::min(p.nkv, kJoinThreads / of_head)), threads = std::min(kJoinThreads, (per_block * of_head + 63) / 64 * 64);
   const dim3 grid((p.rows + together - 1) / together, (p.nkv + per_block - 1) / per_block, (per_block * of_head + threads - 1) / threads);
   auto join = [&](auto kernel, auto *to) {
-    launch(kernel, grid, threads, 0, s, rows, bundles, (const float *)a.part_o, (const float *)a.part_ml, to, lse,
+    launch(kernel, grid, threads, 0, s, rows, bundles, (const float *)a.part_o, (const float4 *)a.part_ml, to, lse,
            p.rows, p.nq, p.nkv, p.hd, together, per_block, a.scale);
   };
   if (p.dtype == WISP_BF16) join(shared_join_kernel<uint16_t>, static_cast<uint16_t *>(out));

@@ -355,7 +355,7 @@ wisp_status shared_build(Build &b, const wisp_model *m, const wisp_batch_desc *d
   p.w_mass_join = desc + b.i_mass_join * 4;
   p.w_po = align256(desc + b.host.size() * 4);
   p.w_pml = p.w_po + align256((size_t)p.n_parts * kTile * p.hd * 4);
-  p.w_pm = p.w_pml + align256((size_t)p.n_parts * kTile * 8);
+  p.w_pm = p.w_pml + align256((size_t)p.n_parts * kTile * 16);
   p.total = p.w_pm + align256((size_t)b.mass_parts * 4);
   return WISP_OK;
 }

@@ -48,6 +48,19 @@ __device__ __forceinline__ void to_op(Op8<float> &o, const float *p) {
   for (int x = 0; x < 2; ++x)
     o.v[x] = make_uint4(__float_as_uint(p[4 * x]), __float_as_uint(p[4 * x + 1]), __float_as_uint(p[4 * x + 2]), __float_as_uint(p[4 * x + 3]));
 }
+// c and the sixteen probabilities of two operands, as they multiply V (fp32: as they are, and added already)
+__device__ __forceinline__ float op_sum(const Op8<uint16_t> &a, const Op8<uint16_t> &b, float c) {
+  const bf16x2_t one = {(__bf16)1.f, (__bf16)1.f};
+  const uint32_t w[8] = {a.v[0].x, a.v[0].y, a.v[0].z, a.v[0].w, b.v[0].x, b.v[0].y, b.v[0].z, b.v[0].w};
+  float s = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[x]), one, s, false);
+    c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[x + 4]), one, c, false);
+  }
+  return c + s;
+}
+__device__ __forceinline__ float op_sum(const Op8<float> &, const Op8<float> &, float c) { return c; }
 // The first n of eight elements: what is not theirs becomes zero.  Slots past a request's last token may hold
 // anything.
 template <typename T>
