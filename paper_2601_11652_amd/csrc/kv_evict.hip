@@ -18,7 +18,9 @@ struct EvictReq {                      // a request, the longest first
   int32_t recent, start, pad[2];       // start: of its tokens in a head's list
 };
 
-constexpr int kFew = 32;               // requests that travel as arguments (an upload first: 3 to 6 us more)
+// Requests travel as arguments where they fit: a launch's 4 KB hold 256 bytes of the runtime's, the angles and what else stands
+// below.  (40 requests of 500 tokens: 38.9 us, with an upload first 44.4; few requests are not slower for the larger block.)
+constexpr int kArgumentBytes = 4096 - 256, kAngles = 128, kFew = (kArgumentBytes - kAngles * 8 - 96) / 32;
 struct EvictArgs {
   const EvictReq *reqs;                // NULL: few
   const int32_t *table, *to;
@@ -53,8 +55,10 @@ __device__ __forceinline__ uint32_t key_of(float f) {
 
 // Which tokens stay: a workgroup for each layer, kv head and request, a wave for a run of tokens.  A radix
 // selection finds the least key that stays and how many of that key do (the first ones): 11 bits (a float's
-// exponent and two more), 11 and 10; then the tokens are listed in order.  HELD: the keys stay in registers.
-// Bound by latency: two loads that depend on each other, and 13 barriers.
+// exponent and two more), 11 and 10; then the tokens are listed in order.  HELD: the keys stay in registers, where the sixteen of
+// a thread are enough; else they are read again in each of five passes, without loads ahead (one request of 16384 tokens to choose
+// from, back to half: 68 us for the whole call, of 16385 90, of 32768 160; 32 such requests: 722, 752 and 1488).
+// Bound by latency: two loads that depend on each other, and 14 barriers.
 template <bool HELD>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kSelectBins];
@@ -180,8 +184,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 // A few requests are bound by latency: 2000 of 8000 tokens, one layer, 18 us.
 struct MoveArgs {
   EvictArgs e;
-  double freq[128];                    // turns of a position's angle, of each dim below HD / 2
+  double freq[kAngles];                // turns of a position's angle, of each dim below HD / 2
 };
+static_assert(sizeof(EvictReq) == 32 && sizeof(MoveArgs) <= kArgumentBytes, "a launch's arguments");
 // Where a token lies: page of its kv head x 16 + slot; kStill: there it stays; kNone (kStill among its bits): there is none
 constexpr uint32_t kStill = 1u << 31, kNone = ~0u;
 constexpr int kHalves = 32;            // half pages of bf16 in a wave's LDS, 256 bytes each

@@ -1,10 +1,11 @@
 """Evictions whose kept tokens take several turns of a workgroup, in every type and with 8 and 16 waves, in place and into other
-pages; tokens that stay beside tokens that move."""
+pages; tokens that stay beside tokens that move; more requests than travel as arguments."""
 import numpy as np
 import pytest
+import torch
 
 import paper_2601_11652_amd as W
-from gpu_harness import log, to_dev
+from gpu_harness import log
 from test_gpu_evict import Cache
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +56,32 @@ def test_tokens_that_stay_beside_tokens_that_move(bf16, stay):
     kept = c.run(keep)
     assert (kept[0, 0, :stay] == np.arange(stay)).all() and kept[0, 0, stay] == stay + 1
     c.check(kept, keep)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("n", [85, 86, 200])
+def test_as_many_requests_as_arguments_hold_and_more(n, captured):
+    log(f"requests {n} {captured}")
+    ctx = 9 + 3 * np.arange(n) % 61
+    c = Cache(ctx, 1, 64, True, 960 + n).to_dev()
+    keep, sink, recent = (ctx // 2).tolist(), [1] * n, (ctx // 8).tolist()
+    before = [t.clone() for t in (c.kv.k, c.kv.v, c.dm)]
+    kept = torch.full((1, 1, int(np.sum(keep))), -9, dtype=torch.int32, device="cuda")
+    ws = W.workspace(W.wisp_kv_evict_workspace_size(c.model, c.desc))
+    call = lambda: W.wisp_kv_evict(c.model, c.kv, c.desc, keep, c.dm, kept, ws, sink, recent)
+    if captured:
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            call()
+        for _ in range(3):
+            for t, x in zip((c.kv.k, c.kv.v, c.dm), before):
+                t.copy_(x)
+            kept.fill_(-9)
+            ws.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+    else:
+        call()
+    W.wisp_check(ws)
+    c.check(kept.cpu().numpy(), keep, sink, recent)
