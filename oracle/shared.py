@@ -38,10 +38,10 @@ def attention(q, k, v, page_table, ctx, nrow):
     return out, lse, mag, big
 
 
-def mass(q, k, lse, page_table, ctx, nrow, count, decay, prev, shared=None):
+def mass(q, k, lse, page_table, ctx, nrow, count, decay, prev):
     """(mass, sum of p x its relative error's unit, mask of the slots written) [blocks][n_kv][16]: prev is
-    what was there (None: nothing), shared[i] the tokens of request i that others of its group have
-    too, whose weights add up over the group.  The second is sum p (sum |q k| / sqrt(hd) + |lse|)."""
+    what was there (None: nothing); a page in several requests' tables gets all of theirs.  The second is sum
+    p (sum |q k| / sqrt(hd) + |lse|)."""
     n_blocks, n_kv, _, hd = k.shape
     M, n_q, _ = q.shape
     G = n_q // n_kv
