@@ -5,9 +5,9 @@
 // attention does without.  A wave keeps the keys of 32 tokens in registers, as an operand, and adds up over the rows, which
 // stream through LDS for the four waves; sums of fp32 in registers, a row's place in them fixed, so results do not vary.
 //
-// For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: 0.38 and
-// 0.66 of the cycles, 16 exponentials of 64 lanes to a row tile's 8 products.  Three workgroups a CU hide most of the waits:
-// 96 us, 730 TFLOP/s.  Two token tiles a wave, half the LDS reads, were 118 us where one took 106; the next tile's products
+// For a prompt (4096 rows x 32 heads over 4096 tokens, half of them seen) matrix and vector instructions take turns: 0.40 and
+// 0.71 of the cycles, 16 exponentials of 64 lanes to a row tile's 8 products.  Three workgroups a CU hide most of the waits:
+// 96 to 98 us, 720 TFLOP/s.  Two token tiles a wave, half the LDS reads, were 118 us where one took 106; the next tile's products
 // beside a tile's exponentials, no change.  32 sessions on a document of 4096 tokens: 21 us, blocks of one row tile whose
 // instructions before and after it are the most of it.  A few rows over many tokens are bound by latency: 4000 tokens 8 us.
 #include <algorithm>

@@ -9,13 +9,15 @@
 // A workgroup takes four row tiles of 32 (a wave each, K and V through LDS for all of them) or one or two (whose tokens the
 // waves share) over a run of tokens.  The host cuts the runs so that the workgroups that run at once end together.
 //
-// Bounds.  64 requests of a 64-head model on 8192 common tokens: 134 us, 763 TFLOP/s (a large library product reaches 1203
-// on this card): a turn of four waves over 32 tokens is 512 cycles of products and takes 915, as the maxima, exponentials and
-// roundings of 16 x 64 scores a wave take some 400 that the other workgroup's products hide in part only.  Scores of the next
-// tile beside a tile's exponentials: 146 -> 137 us.  Two row tiles a wave (half the LDS reads, one workgroup a CU): 167 us.
+// Bounds.  64 requests of a 64-head model on 8192 common tokens: 134 to 136 us, 755 TFLOP/s (a large library product reaches 1203
+// on this card): a turn of four waves over 32 tokens is 512 cycles of products and took 915 before the sum of rounded probabilities,
+// which is 2% of the call, as the maxima, exponentials and roundings of 16 x 64 scores a wave take some 400 that the other workgroup's
+// products hide in part only (matrix units busy 0.42 of the cycles, vector instructions 0.44).  Scores of the next tile beside a tile's
+// exponentials: 146 -> 137 us.  Two row tiles a wave (half the LDS reads, one workgroup a CU): 167 us.
 // 128 samples of a prompt of 16384 tokens: 60 us, of which a third is what starts and ends an item (5 us: the item, its
 // queries and block ids, the first pages, each waiting for the one before) and 7 the join of 28 MB of partial results.  4
-// requests on 1024 tokens: 13 us, latency.
+// requests on 1024 tokens: 13 us, latency.  With nothing shared those samples take 372 us; but 64 requests on 512 tokens take 38, and 50
+// as a group, whose partial results are written and read again.
 #include <algorithm>
 #include <climits>
 
